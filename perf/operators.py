@@ -191,6 +191,15 @@ def _gelu_grad(h):
     return 0.5 * torch.erfc(h * -math.sqrt(0.5)) + h * torch.exp(-0.5 * h * h) * (1.0 / math.sqrt(2.0 * math.pi))
 
 
+def _stored(w1, w2, n_in, variant):
+    """The weights with the entries of padded input columns, which have no effect, set to zero."""
+    D, _, bi = w1.shape
+    g = torch.arange(D, device=w1.device).view(D, 1, 1)
+    k = torch.arange(bi, device=w1.device)
+    return (torch.where(g * bi + k < n_in, w1, 0),
+            torch.where((k * D + g if variant in ("IT", "DT") else g * bi + k) < n_in, w2, 0))
+
+
 def _mult(x1, x2, w1, w2, b, n_out, variant):
     y = _join(torch.bmm(x1, w1.transpose(1, 2).contiguous()), n_out, False)
     return y + _join(torch.bmm(x2, w2.transpose(1, 2).contiguous()), n_out, variant in ("OT", "DT")) + b
@@ -254,7 +263,8 @@ def prepare(case, seed):
             from paper_2312_06881_amd import mx
             return {"case": case, "x": x, "bias": b,
                     "weights": mx.quantize_weights(w1, w2, case["variant"], case["n_in"], case["n_out"])}
-        return {"case": case, "x": x, "weights": (_grid3(w1.float()), _grid3(w2.float()), b)}
+        w1, w2 = _stored(w1.float(), w2.float(), case["n_in"], case["variant"])
+        return {"case": case, "x": x, "weights": (_grid3(w1), _grid3(w2), b)}
     if not own:
         return {"case": case, "x": x, "dy": dy, "params": params}
     from paper_2312_06881_amd.nn import DyadFF, DyadLinear
@@ -381,7 +391,8 @@ def exact(case, seed):
             return back[:, :n_in].contiguous()
 
         def weight(w, place):
-            r = _rounded(w.double().reshape(-1, bi), "fp4").view(w.shape)
+            real = torch.where(place % cols < n_in, w.double(), 0)       # not the padded input columns
+            r = _rounded(real.reshape(-1, bi), "fp4").view(w.shape)
             return _dense(r, place, rows, cols, n_in, n_out)
 
         h = block_order(False) @ weight(w1, p1).t()
