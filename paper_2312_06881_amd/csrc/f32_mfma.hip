@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(kFThreads, 2) f32_gemm_kernel(GemmPass p, int 
 #pragma unroll
         for (int i = 0; i < SM; ++i) acc[j][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     const int wm0 = (wave >> 1) * (BM / 2), wn0 = (wave & 1) * (BN / 2);
-    const bool perm = OUT_T;
+    const bool perm = step != 1;   // consecutive columns (n_dyad 1 too) leave in 16-byte pieces instead
     // kinds: weights read transposed run along the columns, D apart in
     // component 1 under an output transpose (whose component 2 columns start
     // anywhere, so they go one at a time too)
