@@ -84,10 +84,10 @@ typedef enum { DYAD_ACT_NONE = 0, DYAD_ACT_GELU = 1 } dyad_act; /* GELU(x) = x *
 typedef enum {
     DYAD_OK = 0,
     DYAD_ERR_INVALID_ARG = -1, /* unknown enum, size < 0 (M) or <= 0 (n_in, n_out, n_dyad), size overflow, NULL required pointer */
-    DYAD_ERR_SHAPE = -2,       /* only the _ex calls with an input activation: no kernel for this shape */
+    DYAD_ERR_SHAPE = -2,       /* only the _ex calls with an input activation and dyad_mx4_forward: no kernel for this shape */
     DYAD_ERR_ALIGN = -3,       /* a non-NULL pointer is not 16-byte aligned */
     DYAD_ERR_DTYPE = -4,       /* unknown dtype */
-    DYAD_ERR_WORKSPACE = -5,   /* dW workspace NULL or smaller than dyad_dw_workspace_bytes() */
+    DYAD_ERR_WORKSPACE = -5,   /* a workspace (or the packed weights) NULL or smaller than its _bytes() call says */
     DYAD_ERR_LAUNCH = -6,      /* the HIP runtime rejected a kernel launch */
 } dyad_status;
 
@@ -188,6 +188,91 @@ int dyad_backward_dw_ex(dyad_variant variant, int64_t n_in, int64_t n_out, int64
 /* Workspace bytes dyad_backward_dw_ex needs (0 if none, or if the arguments are invalid or unsupported). */
 size_t dyad_dw_workspace_bytes_ex(dyad_variant variant, int64_t n_in, int64_t n_out, int64_t n_dyad,
                                   int64_t M, dyad_dtype dtype, dyad_act act_in);
+
+/*
+ * ---- Microscaled formats -------------------------------------------------------
+ *
+ * OCP microscaling (MX): 32 consecutive values of a row share a scale byte s,
+ * the power of two 2^(s - 127), and each keeps an 8- or 4-bit element:
+ *   DYAD_MX_INT8  two's complement k, the value k / 64 * 2^(s - 127), |k| <= 127
+ *   DYAD_MX_FP4   sign and one of 0, .5, 1, 1.5, 2, 3, 4, 6, times 2^(s - 127)
+ * s - 127 is floor(log2) of the block's largest magnitude, less 2 for fp4;
+ * elements are rounded to nearest even and saturate.  A block of zeros reads
+ * back as zeros.  A block that holds an infinity or a NaN gets s = 255 and reads
+ * back as NaN throughout.  A row's last block may be short.
+ *
+ * The calls below take the same kinds of arguments and give the same
+ * guarantees as those above: they only enqueue work on `stream`, allocate
+ * nothing (every buffer, the workspaces too, is the caller's; a workspace's
+ * contents on entry do not matter), overwrite their outputs, and check every
+ * argument before any HIP call.  Only dyad_forward_mx8 and
+ * dyad_backward_dx_mx8 may use the per-stream buffer of dyad_forward.
+ */
+typedef enum { DYAD_MX_INT8 = 0, DYAD_MX_FP4 = 1 } dyad_mx_format;
+
+/*
+ * X [rows][cols] of dtype, row-major, into codes and scales [rows][ceil(cols/32)]
+ * (one byte each), and back.  int8 codes are [rows][cols]; fp4 codes
+ * [rows][ceil(cols/2)] bytes, an even column in the low nibble.  Reading back
+ * is exact in fp32, and in bf16 but for fp4 and int8 steps below bf16's
+ * smallest subnormal.  rows == 0 is valid.
+ */
+int dyad_mx_quantize(dyad_mx_format format, int64_t rows, int64_t cols, dyad_dtype dtype, const void *X, void *codes,
+                     void *scales, hipStream_t stream);
+int dyad_mx_dequantize(dyad_mx_format format, int64_t rows, int64_t cols, dyad_dtype dtype, const void *codes,
+                       const void *scales, void *Y, hipStream_t stream);
+
+/*
+ * Weights of one layer for dyad_mx4_forward: W1, W2 [n_dyad][bo][bi] of dtype
+ * quantised to fp4 along the reduction (each row of a block on its own; entries
+ * of padded rows or columns are zero), into dyad_mx4_weight_bytes() bytes whose
+ * layout is the library's own.  The variant is part of the result.
+ * dyad_mx4_weight_bytes is 0 for invalid arguments.
+ */
+size_t dyad_mx4_weight_bytes(dyad_variant variant, int64_t n_in, int64_t n_out, int64_t n_dyad);
+int dyad_mx4_quantize_weights(dyad_variant variant, int64_t n_in, int64_t n_out, int64_t n_dyad, dyad_dtype dtype,
+                              const void *W1, const void *W2, void *packed, size_t packed_bytes, hipStream_t stream);
+
+/*
+ * Forward pass on fp4 operands: Y[m] = act(W Q(X)[m] + bias), summed in fp32 and
+ * rounded once to dtype, where W holds the quantised entries and each component
+ * sees X quantised to fp4 in its own block order: component 1 the blocks
+ * X[m][i*bi + k], component 2 the same or, under an input transpose, the
+ * residues X[m][k*n_dyad + i], 32 consecutive k to a scale.  X is quantised within
+ * the call, each token on its own, into the workspace of
+ * dyad_mx4_workspace_bytes() bytes.  With Dyad-OT / -DT, n_dyad above 32 returns
+ * DYAD_ERR_SHAPE.
+ */
+size_t dyad_mx4_workspace_bytes(dyad_variant variant, int64_t n_in, int64_t n_out, int64_t n_dyad, int64_t M);
+int dyad_mx4_forward(dyad_variant variant, int64_t n_in, int64_t n_out, int64_t n_dyad, int64_t M, dyad_dtype dtype,
+                     const void *X, const void *packed, size_t packed_bytes, const void *bias, dyad_act act, void *Y,
+                     void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Training with activations checkpointed in DYAD_MX_INT8 (codes and scales as
+ * dyad_mx_quantize writes them, along each token's row):
+ *   dyad_forward_mx8      dyad_forward with GELU, whose pre-activation H is kept as
+ *                         H8 / Hs, the quantised value of what H would hold
+ *   dyad_backward_dx_mx8  dyad_backward_dx with act_in GELU at the kept H:
+ *                         dX = (W^T dZ) * GELU'(H8)
+ *   dyad_backward_dw_mx8  dyad_backward_dw with X read from X8 / Xs; with act_in
+ *                         GELU the layer's input is GELU(X8)
+ * H8 [M][n_out] for the forward pass, [M][n_in] for the input gradient; X8 [M][n_in].
+ * The workspace holds dyad_mx8_workspace_bytes() bytes for the pass (act_in
+ * counts for the weight gradient only).
+ */
+typedef enum { DYAD_MX8_FORWARD = 0, DYAD_MX8_DX = 1, DYAD_MX8_DW = 2 } dyad_mx8_pass;
+size_t dyad_mx8_workspace_bytes(dyad_mx8_pass pass, dyad_variant variant, int64_t n_in, int64_t n_out, int64_t n_dyad,
+                                int64_t M, dyad_dtype dtype, dyad_act act_in);
+int dyad_forward_mx8(dyad_variant variant, int64_t n_in, int64_t n_out, int64_t n_dyad, int64_t M, dyad_dtype dtype,
+                     const void *X, const void *W1, const void *W2, const void *bias, void *Y, void *H8, void *Hs,
+                     void *workspace, size_t workspace_bytes, hipStream_t stream);
+int dyad_backward_dx_mx8(dyad_variant variant, int64_t n_in, int64_t n_out, int64_t n_dyad, int64_t M,
+                         dyad_dtype dtype, const void *dZ, const void *W1, const void *W2, const void *H8,
+                         const void *Hs, void *dX, void *workspace, size_t workspace_bytes, hipStream_t stream);
+int dyad_backward_dw_mx8(dyad_variant variant, int64_t n_in, int64_t n_out, int64_t n_dyad, int64_t M,
+                         dyad_dtype dtype, dyad_act act_in, const void *dZ, const void *X8, const void *Xs, void *dW1,
+                         void *dW2, void *dbias, void *workspace, size_t workspace_bytes, hipStream_t stream);
 
 /* Static, human-readable text for a dyad_status value. */
 const char *dyad_strerror(int status);

@@ -11,6 +11,7 @@ Two levels:
   * ``forward``, ``backward_dx``, ``backward_dw``: tensor-level helpers that
     allocate outputs with torch on the inputs' device, call the C-ABI on
     torch's current stream, and raise ``DyadError`` on a non-zero status.
+    Those of the microscaled formats are in ``mx``.
 
 There is no CPU fallback: if ``libdyad.so`` is missing or fails to load, every
 call raises.
@@ -27,11 +28,16 @@ __all__ = [
     "dyad_forward", "dyad_forward_noalloc", "dyad_forward_ex", "dyad_backward_dx", "dyad_backward_dw",
     "dyad_backward_dw_ex", "dyad_dw_workspace_bytes", "dyad_dw_workspace_bytes_ex",
     "dyad_strerror", "forward", "backward_dx", "backward_dw", "lib_path",
+    "MX_INT8", "MX_FP4", "MX8_FORWARD", "MX8_DX", "MX8_DW", "dyad_mx_quantize", "dyad_mx_dequantize",
+    "dyad_mx4_weight_bytes", "dyad_mx4_quantize_weights", "dyad_mx4_workspace_bytes", "dyad_mx4_forward",
+    "dyad_mx8_workspace_bytes", "dyad_forward_mx8", "dyad_backward_dx_mx8", "dyad_backward_dw_mx8",
 ]
 
 IT, OT, DT = 0, 1, 2
 F32, BF16 = 0, 1
 ACT_NONE, ACT_GELU = 0, 1
+MX_INT8, MX_FP4 = 0, 1
+MX8_FORWARD, MX8_DX, MX8_DW = 0, 1, 2
 VARIANTS = {"IT": IT, "OT": OT, "DT": DT}
 ACTS = {"none": ACT_NONE, "gelu": ACT_GELU}
 STATUS = {0: "DYAD_OK", -1: "DYAD_ERR_INVALID_ARG", -2: "DYAD_ERR_SHAPE", -3: "DYAD_ERR_ALIGN",
@@ -85,6 +91,20 @@ def _load():
                                         _vp, ctypes.c_size_t, _vp]
     lib.dyad_dw_workspace_bytes_ex.restype = ctypes.c_size_t
     lib.dyad_dw_workspace_bytes_ex.argtypes = [_int, _i64, _i64, _i64, _i64, _int, _int]
+    size = ctypes.c_size_t
+    for name, restype, args in (
+            ("dyad_mx_quantize", _int, [_int, _i64, _i64, _int, _vp, _vp, _vp, _vp]),
+            ("dyad_mx_dequantize", _int, [_int, _i64, _i64, _int, _vp, _vp, _vp, _vp]),
+            ("dyad_mx4_weight_bytes", size, [_int, _i64, _i64, _i64]),
+            ("dyad_mx4_quantize_weights", _int, [_int, _i64, _i64, _i64, _int, _vp, _vp, _vp, size, _vp]),
+            ("dyad_mx4_workspace_bytes", size, [_int, _i64, _i64, _i64, _i64]),
+            ("dyad_mx4_forward", _int, [_int, _i64, _i64, _i64, _i64, _int, _vp, _vp, size, _vp, _int, _vp, _vp, size, _vp]),
+            ("dyad_mx8_workspace_bytes", size, [_int, _int, _i64, _i64, _i64, _i64, _int, _int]),
+            ("dyad_forward_mx8", _int, [_int, _i64, _i64, _i64, _i64, _int, *[_vp] * 8, size, _vp]),
+            ("dyad_backward_dx_mx8", _int, [_int, _i64, _i64, _i64, _i64, _int, *[_vp] * 7, size, _vp]),
+            ("dyad_backward_dw_mx8", _int, [_int, _i64, _i64, _i64, _i64, _int, _int, *[_vp] * 7, size, _vp])):
+        fn = getattr(lib, name)
+        fn.restype, fn.argtypes = restype, args
     lib.dyad_strerror.restype = ctypes.c_char_p
     lib.dyad_strerror.argtypes = [_int]
     _lib = lib
@@ -134,6 +154,55 @@ def dyad_backward_dw_ex(variant, n_in, n_out, n_dyad, M, dtype, act_in, dZ, X, d
 
 def dyad_dw_workspace_bytes_ex(variant, n_in, n_out, n_dyad, M, dtype, act_in) -> int:
     return _load().dyad_dw_workspace_bytes_ex(variant, n_in, n_out, n_dyad, M, dtype, act_in)
+
+
+def dyad_mx_quantize(format, rows, cols, dtype, X, codes, scales, stream) -> int:
+    return _load().dyad_mx_quantize(format, rows, cols, dtype, X, codes, scales, stream)
+
+
+def dyad_mx_dequantize(format, rows, cols, dtype, codes, scales, Y, stream) -> int:
+    return _load().dyad_mx_dequantize(format, rows, cols, dtype, codes, scales, Y, stream)
+
+
+def dyad_mx4_weight_bytes(variant, n_in, n_out, n_dyad) -> int:
+    return _load().dyad_mx4_weight_bytes(variant, n_in, n_out, n_dyad)
+
+
+def dyad_mx4_quantize_weights(variant, n_in, n_out, n_dyad, dtype, W1, W2, packed, packed_bytes, stream) -> int:
+    return _load().dyad_mx4_quantize_weights(variant, n_in, n_out, n_dyad, dtype, W1, W2, packed, packed_bytes,
+                                             stream)
+
+
+def dyad_mx4_workspace_bytes(variant, n_in, n_out, n_dyad, M) -> int:
+    return _load().dyad_mx4_workspace_bytes(variant, n_in, n_out, n_dyad, M)
+
+
+def dyad_mx4_forward(variant, n_in, n_out, n_dyad, M, dtype, X, packed, packed_bytes, bias, act, Y, workspace,
+                     workspace_bytes, stream) -> int:
+    return _load().dyad_mx4_forward(variant, n_in, n_out, n_dyad, M, dtype, X, packed, packed_bytes, bias, act, Y,
+                                    workspace, workspace_bytes, stream)
+
+
+def dyad_mx8_workspace_bytes(pass_, variant, n_in, n_out, n_dyad, M, dtype, act_in) -> int:
+    return _load().dyad_mx8_workspace_bytes(pass_, variant, n_in, n_out, n_dyad, M, dtype, act_in)
+
+
+def dyad_forward_mx8(variant, n_in, n_out, n_dyad, M, dtype, X, W1, W2, bias, Y, H8, Hs, workspace,
+                     workspace_bytes, stream) -> int:
+    return _load().dyad_forward_mx8(variant, n_in, n_out, n_dyad, M, dtype, X, W1, W2, bias, Y, H8, Hs, workspace,
+                                    workspace_bytes, stream)
+
+
+def dyad_backward_dx_mx8(variant, n_in, n_out, n_dyad, M, dtype, dZ, W1, W2, H8, Hs, dX, workspace,
+                         workspace_bytes, stream) -> int:
+    return _load().dyad_backward_dx_mx8(variant, n_in, n_out, n_dyad, M, dtype, dZ, W1, W2, H8, Hs, dX, workspace,
+                                        workspace_bytes, stream)
+
+
+def dyad_backward_dw_mx8(variant, n_in, n_out, n_dyad, M, dtype, act_in, dZ, X8, Xs, dW1, dW2, dbias, workspace,
+                         workspace_bytes, stream) -> int:
+    return _load().dyad_backward_dw_mx8(variant, n_in, n_out, n_dyad, M, dtype, act_in, dZ, X8, Xs, dW1, dW2, dbias,
+                                        workspace, workspace_bytes, stream)
 
 
 def dyad_strerror(status: int) -> str:

@@ -3,49 +3,14 @@
 // the first HIP call.
 #include "dyad.h"
 
-#include <string.h>
-
+#include "abi_checks.h"
 #include "dyad_internal.h"
 
 namespace {
 
+using namespace dyad::abi;
 using dyad::DwPass;
 using dyad::GemmPass;
-
-constexpr int64_t kMaxDim = (int64_t)1 << 31;   // any single width or token count
-constexpr int64_t kMaxElems = (int64_t)1 << 40; // any single tensor, in elements
-
-// Per-block size; a width that D does not divide is zero-padded up to D blocks.
-int64_t block(int64_t n, int64_t D) { return (n + D - 1) / D; }
-
-// The int a caller passed for an enum parameter.  A C caller may pass any
-// int there; reading the parameter through its enum type would be undefined
-// in C++ for values outside the enumerators' range, so its bytes are read as
-// an int and every check works on that.
-template <class E>
-int enum_value(const E &e) {
-    static_assert(sizeof(E) == sizeof(int), "C enums are int-sized");
-    int v;
-    memcpy(&v, &e, sizeof v);
-    return v;
-}
-
-bool aligned16(const void *p) { return p == nullptr || ((uintptr_t)p & 15u) == 0; }
-
-int check_sizes(int variant, int64_t n_in, int64_t n_out, int64_t D, int64_t M, int dtype) {
-    if (variant != DYAD_IT && variant != DYAD_OT && variant != DYAD_DT) return DYAD_ERR_INVALID_ARG;
-    if (dtype != DYAD_F32 && dtype != DYAD_BF16) return DYAD_ERR_DTYPE;
-    if (n_in <= 0 || n_out <= 0 || D <= 0 || M < 0) return DYAD_ERR_INVALID_ARG;
-    if (n_in >= kMaxDim || n_out >= kMaxDim || M >= kMaxDim) return DYAD_ERR_INVALID_ARG;
-    if (M * n_in >= kMaxElems || M * n_out >= kMaxElems) return DYAD_ERR_INVALID_ARG;
-    if (D >= kMaxDim || D * block(n_in, D) * block(n_out, D) >= kMaxElems) return DYAD_ERR_INVALID_ARG;
-    return DYAD_OK;
-}
-
-bool in_transposed(int v) { return v == DYAD_IT || v == DYAD_DT; }
-bool out_transposed(int v) { return v == DYAD_OT || v == DYAD_DT; }
-
-int launch_status(hipError_t e) { return e == hipSuccess ? DYAD_OK : DYAD_ERR_LAUNCH; }
 
 int run_gemm(const GemmPass &p, hipStream_t s) {
     const dyad::WorkspaceHold hold;
@@ -220,10 +185,10 @@ const char *dyad_strerror(int status) {
     switch (status) {
     case DYAD_OK: return "ok";
     case DYAD_ERR_INVALID_ARG: return "invalid argument (enum, size or NULL pointer)";
-    case DYAD_ERR_SHAPE: return "no kernel applies an input activation to this shape";
+    case DYAD_ERR_SHAPE: return "no kernel takes this shape";
     case DYAD_ERR_ALIGN: return "pointer not 16-byte aligned";
     case DYAD_ERR_DTYPE: return "unsupported dtype";
-    case DYAD_ERR_WORKSPACE: return "dW workspace missing or too small";
+    case DYAD_ERR_WORKSPACE: return "workspace or packed weights missing or too small";
     case DYAD_ERR_LAUNCH: return "kernel launch failed";
     default: return "unknown status";
     }

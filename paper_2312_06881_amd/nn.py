@@ -11,6 +11,10 @@
   applies GELU' inside fc2's input-gradient epilogue, so the activation
   gradient is never a separate pass.
 
+* ``stash="mx8"`` on either keeps what the backward pass reads (the layer's input,
+  the pre-activation) as 8-bit microscaled blocks; the gradients see the kept values.
+* ``MX4DyadLinear``, ``MX4DyadFF``: inference on fp4 weights and inputs.
+
 Autograd runs every pass through the C-ABI (forward, input gradient, weight and
 bias gradient); there is no torch fallback and CPU tensors are rejected.
 Leading input dimensions are flattened into the token dimension.  Weights
@@ -25,9 +29,9 @@ import math
 import torch
 from torch.autograd import forward_ad
 
-from . import DyadError, backward_dw, backward_dx, forward
+from . import DyadError, backward_dw, backward_dx, forward, mx
 
-__all__ = ["DyadLinear", "DyadFF", "dyad_linear", "dyad_ff"]
+__all__ = ["DyadLinear", "DyadFF", "MX4DyadLinear", "MX4DyadFF", "dyad_linear", "dyad_ff"]
 
 
 def _tokens(x: torch.Tensor) -> torch.Tensor:
@@ -121,6 +125,79 @@ class _DyadFFFn(torch.autograd.Function):
         return dx, dw1a, dw2a, dba, dw1b, dw2b, dbb, None, None, None, None
 
 
+def _parts(q):
+    """The tensors of an 8-bit checkpoint, as autograd saves (and frees) them."""
+    return (None, None) if q is None else (q.codes, q.scales)
+
+
+def _kept(parts, like, cols):
+    return mx.MXTensor(*parts, (like.shape[0], cols), like.dtype, "int8")
+
+
+class _DyadLinearStashFn(torch.autograd.Function):
+    """One layer whose input is kept in 8 bits, where a weight gradient will read it."""
+
+    @staticmethod
+    def forward(ctx, x, w1, w2, bias, variant, n_out):
+        ctx.variant, ctx.n_in, ctx.has_bias = variant, x.shape[1], bias is not None
+        kept = mx.quantize(x) if any(ctx.needs_input_grad[1:4]) else None
+        ctx.save_for_backward(w1, w2, *_parts(kept))
+        return forward(x, w1, w2, bias, variant, n_out=n_out)
+
+    @staticmethod
+    def backward(ctx, dy):
+        w1, w2, *kept = ctx.saved_tensors
+        dy = dy.contiguous()
+        dx = backward_dx(dy, w1, w2, ctx.variant, n_in=ctx.n_in) if ctx.needs_input_grad[0] else None
+        dw1 = dw2 = db = None
+        if any(ctx.needs_input_grad[1:4]):
+            dw1, dw2, db = mx.backward_dw(dy, _kept(kept, dy, ctx.n_in), w1.shape[0], ctx.variant, want_db=ctx.has_bias)
+        return dx, dw1, dw2, db, None, None
+
+
+class _DyadFFStashFn(torch.autograd.Function):
+    """fc1 -> GELU -> fc2 that keeps x and fc1's pre-activation in 8 bits.  The backward pass
+    takes GELU' and fc2's input from the kept pre-activation, fc1's weight gradient from the
+    kept x; what nothing will read is not kept."""
+
+    @staticmethod
+    def forward(ctx, x, w1a, w2a, ba, w1b, w2b, bb, variants, ffn, d_out):
+        va, vb = variants
+        need = ctx.needs_input_grad
+        ctx.variants, ctx.n_in, ctx.bias = variants, x.shape[1], (ba is not None, bb is not None)
+        kept_x = mx.quantize(x) if any(need[1:4]) else None
+        ctx.ffn = ffn
+        if any(need[:7]):
+            a, kept_h = mx.forward_gelu(x, w1a, w2a, ba, va, n_out=ffn)
+        else:
+            a, kept_h = forward(x, w1a, w2a, ba, va, act="gelu", n_out=ffn), None
+        ctx.save_for_backward(w1a, w2a, w1b, w2b, *_parts(kept_x), *_parts(kept_h))
+        return forward(a, w1b, w2b, bb, vb, n_out=d_out)
+
+    @staticmethod
+    def backward(ctx, dy):
+        w1a, w2a, w1b, w2b, *kept = ctx.saved_tensors
+        va, vb = ctx.variants
+        need = ctx.needs_input_grad
+        dy = dy.contiguous()
+        kept_h = _kept(kept[2:], dy, ctx.ffn) if any(need[:7]) else None
+        dx = dw1a = dw2a = dba = dw1b = dw2b = dbb = None
+        if any(need[4:7]):
+            dw1b, dw2b, dbb = mx.backward_dw(dy, kept_h, w1b.shape[0], vb, want_db=ctx.bias[1], act_in="gelu")
+        if any(need[:4]):
+            dz = mx.backward_dx_gelu(dy, w1b, w2b, kept_h, vb)
+            if need[0]:
+                dx = backward_dx(dz, w1a, w2a, va, n_in=ctx.n_in)
+            if any(need[1:4]):
+                dw1a, dw2a, dba = mx.backward_dw(dz, _kept(kept[:2], dz, ctx.n_in), w1a.shape[0], va, want_db=ctx.bias[0])
+        return dx, dw1a, dw2a, dba, dw1b, dw2b, dbb, None, None, None
+
+
+def _check_stash(stash):
+    if stash not in (None, "mx8"):
+        raise ValueError("stash is None or mx8")
+
+
 def _variant_pair(variant):
     pair = (variant, variant) if isinstance(variant, str) else tuple(variant)
     if len(pair) != 2 or any(v not in ("IT", "OT", "DT") for v in pair):
@@ -128,24 +205,32 @@ def _variant_pair(variant):
     return pair
 
 
-def dyad_linear(x, w1, w2, bias=None, variant="IT", out_features=None):
+def dyad_linear(x, w1, w2, bias=None, variant="IT", out_features=None, stash=None):
     """Functional form of ``DyadLinear``: x [..., n_in] -> [..., n_out], where n_out is
-    out_features, else bias's length, else n_dyad * bo."""
+    out_features, else bias's length, else n_dyad * bo.  stash="mx8": x is kept for the
+    backward pass in 8 bits."""
+    _check_stash(stash)
     D, bo, _ = w1.shape
     if out_features is None:
         out_features = bias.shape[0] if bias is not None else D * bo
     if _plain(x, w1, w2, bias):
         y = forward(_tokens(x), w1, w2, bias, variant, n_out=out_features)
+    elif stash:
+        y = _DyadLinearStashFn.apply(_tokens(x), w1, w2, bias, variant, out_features)
     else:
         y = _DyadLinearFn.apply(_tokens(x), w1, w2, bias, variant, out_features)
     return y.reshape(*x.shape[:-1], out_features)
 
 
-def dyad_ff(x, fc1, fc2, variant="IT", ffn=None, fused=False):
+def dyad_ff(x, fc1, fc2, variant="IT", ffn=None, fused=False, stash=None):
     """Functional form of ``DyadFF``; fc1 / fc2 are (W1, W2, bias) triples; variant is one
     variant or an (fc1, fc2) pair; ffn is the hidden width (default n_dyad * fc1's bo).
     The output width is x's, as the block is d -> ffn -> d.  fused: GELU applied inside
-    fc2's kernels, the activation never written (see _DyadFFFn)."""
+    fc2's kernels, the activation never written (see _DyadFFFn).  stash="mx8": the
+    backward pass reads x and the pre-activation from 8-bit checkpoints (not with fused)."""
+    _check_stash(stash)
+    if stash and fused:
+        raise ValueError("stash and fused exclude each other")
     d = x.shape[-1]
     if ffn is None:
         ffn = fc1[0].shape[0] * fc1[0].shape[1]
@@ -154,6 +239,8 @@ def dyad_ff(x, fc1, fc2, variant="IT", ffn=None, fused=False):
         # nothing to stash for a backward pass: the pre-activation is not written
         a = forward(_tokens(x), *fc1, pair[0], act="gelu", n_out=ffn)
         y = forward(a, *fc2, pair[1], n_out=d)
+    elif stash:
+        y = _DyadFFStashFn.apply(_tokens(x), *fc1, *fc2, pair, ffn, d)
     else:
         y = _DyadFFFn.apply(_tokens(x), *fc1, *fc2, pair, ffn, d, bool(fused))
     return y.reshape(*x.shape[:-1], d)
@@ -167,12 +254,14 @@ class DyadLinear(torch.nn.Module):
     their blocks from 512 tokens, and on the general kernels below.  Initialisation
     (a convenience, not part of the method): uniform in +-1/sqrt(2 * in_features /
     n_dyad), the fan-in of one output feature (two components of in_features /
-    n_dyad inputs each).
+    n_dyad inputs each).  ``stash="mx8"`` keeps the input in 8 bits for the backward pass.
     """
 
     def __init__(self, in_features, out_features, n_dyad, variant="IT", bias=True, device=None,
-                 dtype=torch.bfloat16):
+                 dtype=torch.bfloat16, stash=None):
         super().__init__()
+        _check_stash(stash)
+        self.stash = stash
         if min(in_features, out_features, n_dyad) <= 0:
             raise ValueError("widths and n_dyad must be positive")
         if variant not in ("IT", "OT", "DT"):
@@ -193,7 +282,7 @@ class DyadLinear(torch.nn.Module):
                     p.uniform_(-bound, bound)
 
     def forward(self, x):
-        return dyad_linear(x, self.w1, self.w2, self.bias, self.variant, self.out_features)
+        return dyad_linear(x, self.w1, self.w2, self.bias, self.variant, self.out_features, self.stash)
 
     def extra_repr(self):
         return (f"in_features={self.in_features}, out_features={self.out_features}, "
@@ -205,12 +294,17 @@ class DyadFF(torch.nn.Module):
 
     ``variant`` is one of IT / OT / DT for both layers, or an (fc1, fc2) pair for a
     heterogeneous mix; ``n_dyad`` likewise may be one value or a pair.  ``fused``: fc1
-    writes only its pre-activation and fc2's kernels apply GELU as they stage it."""
+    writes only its pre-activation and fc2's kernels apply GELU as they stage it.
+    ``stash="mx8"``: the input and the pre-activation are kept in 8 bits for the backward
+    pass (not with ``fused``)."""
 
     def __init__(self, d, ffn, n_dyad, variant="IT", bias=True, device=None, dtype=torch.bfloat16,
-                 fused=False):
+                 fused=False, stash=None):
         super().__init__()
-        self.fused = fused
+        _check_stash(stash)
+        if stash and fused:
+            raise ValueError("stash and fused exclude each other")
+        self.fused, self.stash = fused, stash
         va, vb = _variant_pair(variant)
         da, db = (n_dyad, n_dyad) if isinstance(n_dyad, int) else tuple(n_dyad)
         self.fc1 = DyadLinear(d, ffn, da, va, bias, device, dtype)
@@ -220,4 +314,39 @@ class DyadFF(torch.nn.Module):
 
     def forward(self, x):
         return dyad_ff(x, (self.fc1.w1, self.fc1.w2, self.fc1.bias),
-                       (self.fc2.w1, self.fc2.w2, self.fc2.bias), self.variant, self.ffn, self.fused)
+                       (self.fc2.w1, self.fc2.w2, self.fc2.bias), self.variant, self.ffn, self.fused, self.stash)
+
+
+class MX4DyadLinear(torch.nn.Module):
+    """A ``DyadLinear`` for inference on fp4 weights, its input quantised to fp4 within the
+    call; the weights are quantised once, here.  act: "none" or "gelu"."""
+
+    def __init__(self, layer: DyadLinear, act="none"):
+        super().__init__()
+        if act not in ("none", "gelu"):
+            raise ValueError("act is none or gelu")
+        self.in_features, self.out_features, self.n_dyad = layer.in_features, layer.out_features, layer.n_dyad
+        self.variant, self.act = layer.variant, act
+        w = mx.quantize_weights(layer.w1.detach(), layer.w2.detach(), layer.variant, layer.in_features,
+                                layer.out_features)
+        self.register_buffer("packed", w.packed)
+        self.register_buffer("bias", None if layer.bias is None else layer.bias.detach().clone())
+
+    def forward(self, x):
+        w = mx.MX4Weights(self.packed, self.variant, self.in_features, self.out_features, self.n_dyad)
+        return mx.forward(_tokens(x), w, self.bias, self.act).reshape(*x.shape[:-1], self.out_features)
+
+    def extra_repr(self):
+        return (f"in_features={self.in_features}, out_features={self.out_features}, n_dyad={self.n_dyad}, "
+                f"variant={self.variant}, act={self.act}, bias={self.bias is not None}")
+
+
+class MX4DyadFF(torch.nn.Module):
+    """A ``DyadFF`` for inference on fp4 weights and inputs of both layers."""
+
+    def __init__(self, block: DyadFF):
+        super().__init__()
+        self.fc1, self.fc2 = MX4DyadLinear(block.fc1, "gelu"), MX4DyadLinear(block.fc2)
+
+    def forward(self, x):
+        return self.fc2(self.fc1(x))
