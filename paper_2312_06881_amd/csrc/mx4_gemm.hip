@@ -12,148 +12,227 @@
 // swizzle and no edge: rows and steps past the real ones hold zeros.  The
 // input's copy under an input transpose holds each residue's columns k*D + g
 // as a block of its own, so the permutation costs the quantising pass alone.
+// Both components run in one loop over 2 * steps, the loads of the next steps
+// in flight over a step's multiplies.
 //
-// Output transpose.  Component 2's block g makes columns j*D + g, component 1's
-// block i columns i*bo + r.  A workgroup owns 16 * CF * D consecutive columns:
-// every residue's CF fragments of 16 j for component 2, whose sums meet their
-// columns in LDS, and the fragments of component 1 over the same columns, which
-// add to them as they finish.
-#include "mx_common.h"
+// Output transpose.  A wave owns a residue: its outputs j*D + g take block g of
+// component 2, and component 1's rows kept by residue (mx4_by_residue), into the
+// same accumulators.  The D waves of a workgroup make 16 * SN * D consecutive
+// columns, which meet in LDS on the way out.  Shapes whose residues do not fit a
+// block so run a form that adds component 1 to component 2's sums in LDS.
+#include "mx4_gemm.h"
 
 namespace dyad {
 
 namespace {
 
-typedef __attribute__((ext_vector_type(8))) int i32x8_t;
-
-struct Mx4Args {
-    int64_t M, n_in, n_out;
-    int D, bi, bo;
-    const uint8_t *wc, *ws, *xc, *xs;    // codes and scales of weights and input
-    int w_frags, x_frags, steps, words;
-    const void *bias;
-    void *Y;
-    int gelu, in_t;
-    int tiles_n, tiles;
+// Where a wave's fragments start for each component.
+struct Mx4Wave {
+    int wp[2], wf[2];      // weights: part and first fragment
+    int xp[2];             // input: part
+    int xf;                // first token fragment
 };
 
-// acc[c][t] += W fragment row c (codes at wc + wo[c], scales at ws + wso[c]) times
-// X fragment t over all steps.  The weights are the first operand: a lane
-// ends up with four consecutive outputs 4 * (lane / 16) + v of token lane % 16.
-template <int CF, int TM>
-struct Mx4Frags {
-    int64_t w[CF], x[TM];   // fragment numbers (part * frags + fragment), wave-uniform
-};
-
-template <int CF, int TM>
-__device__ __forceinline__ void mx4_span(const Mx4Args &a, const Mx4Frags<CF, TM> &f, int lane, f32x4_t (&acc)[CF][TM]) {
-    const int steps = a.steps, words = a.words;
-    auto step = [&](auto byte, const uint32_t (&sw)[CF], const uint32_t (&sx)[TM], int s) {
-        constexpr int B = decltype(byte)::value;
-        uint4 w[CF], x[TM];
+// acc += both components, PF steps of loads in flight.  Fragments past the last
+// load the last again (their results are not stored).
+template <int SN, int SM, int PF>
+__device__ __forceinline__ void mx4_loop(const Mx4Args &a, const Mx4Wave &v, int lane, f32x4_t (&acc)[SN][SM]) {
+    constexpr int GN = (SN + 3) / 4, GM = (SM + 3) / 4;
+    uint4 w[PF][SN], x[PF][SM];
+    uint32_t sw[PF][GN], sx[PF][GM];
+    const int steps = a.steps, total = 2 * steps;
+    const uint32_t l16 = 16u * (uint32_t)lane, l4 = 4u * (uint32_t)lane;
+    auto load = [&](auto slot, int t) {
+        constexpr int P = decltype(slot)::value;
+        const int c = t >= steps ? 1 : 0, s = t - c * steps;
+        const uint8_t *wb = a.wc + (int64_t)v.wp[c] * a.w_frags * steps * 1024 + (int64_t)s * 1024;
+        const uint8_t *xb = a.xc + (int64_t)v.xp[c] * a.x_frags * steps * 1024 + (int64_t)s * 1024;
 #pragma unroll
-        for (int c = 0; c < CF; ++c) w[c] = reinterpret_cast<const uint4 *>(a.wc + (f.w[c] * steps + s) * 1024)[lane];
+        for (int j = 0; j < SN; ++j) {
+            const int f = v.wf[c] + j < a.w_frags ? v.wf[c] + j : a.w_frags - 1;
+            w[P][j] = *reinterpret_cast<const uint4 *>(wb + (int64_t)f * steps * 1024 + l16);
+        }
 #pragma unroll
-        for (int t = 0; t < TM; ++t) x[t] = reinterpret_cast<const uint4 *>(a.xc + (f.x[t] * steps + s) * 1024)[lane];
+        for (int i = 0; i < SM; ++i) {
+            const int f = v.xf + i < a.x_frags ? v.xf + i : a.x_frags - 1;
+            x[P][i] = *reinterpret_cast<const uint4 *>(xb + (int64_t)f * steps * 1024 + l16);
+        }
+        const uint8_t *wsb = a.ws + ((int64_t)v.wp[c] * a.w_groups * steps + s) * 256;
+        const uint8_t *xsb = a.xs + ((int64_t)v.xp[c] * a.x_groups * steps + s) * 256;
 #pragma unroll
-        for (int c = 0; c < CF; ++c)
+        for (int q = 0; q < GN; ++q) {
+            const int f = (v.wf[c] >> 2) + q < a.w_groups ? (v.wf[c] >> 2) + q : a.w_groups - 1;
+            sw[P][q] = *reinterpret_cast<const uint32_t *>(wsb + (int64_t)f * steps * 256 + l4);
+            if constexpr (SN < 4) sw[P][q] >>= 8 * (v.wf[c] & 3);
+        }
 #pragma unroll
-            for (int t = 0; t < TM; ++t) {
-                const i32x8_t wv = {(int)w[c].x, (int)w[c].y, (int)w[c].z, (int)w[c].w, 0, 0, 0, 0};
-                const i32x8_t xv = {(int)x[t].x, (int)x[t].y, (int)x[t].z, (int)x[t].w, 0, 0, 0, 0};
-                acc[c][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv, xv, acc[c][t], 4, 4, B, (int)sw[c], B,
-                                                                             (int)sx[t]);
-            }
+        for (int q = 0; q < GM; ++q) {
+            const int f = (v.xf >> 2) + q < a.x_groups ? (v.xf >> 2) + q : a.x_groups - 1;
+            sx[P][q] = *reinterpret_cast<const uint32_t *>(xsb + (int64_t)f * steps * 256 + l4);
+            if constexpr (SM < 4) sx[P][q] >>= 8 * (v.xf & 3);
+        }
     };
-    for (int q = 0; q < words; ++q) {
-        uint32_t sw[CF], sx[TM];
-#pragma unroll
-        for (int c = 0; c < CF; ++c) sw[c] = reinterpret_cast<const uint32_t *>(a.ws + (f.w[c] * words + q) * 256)[lane];
-#pragma unroll
-        for (int t = 0; t < TM; ++t) sx[t] = reinterpret_cast<const uint32_t *>(a.xs + (f.x[t] * words + q) * 256)[lane];
-        const int s = 4 * q;
-        step(std::integral_constant<int, 0>{}, sw, sx, s);
-        if (s + 4 <= steps) {
-            step(std::integral_constant<int, 1>{}, sw, sx, s + 1);
-            step(std::integral_constant<int, 2>{}, sw, sx, s + 2);
-            step(std::integral_constant<int, 3>{}, sw, sx, s + 3);
+    auto multiply = [&](auto slot) {
+        constexpr int P = decltype(slot)::value;
+        mx4_multiply<0, 0, SN, SM>(w[P], x[P], sw[P], sx[P], acc);
+    };
+    using S0 = std::integral_constant<int, 0>;
+    using S1 = std::integral_constant<int, 1>;
+    load(S0{}, 0);
+    load(S1{}, 1);
+    if constexpr (PF == 2) {
+        for (int t = 2; t < total; t += 2) {
+            multiply(S0{});
+            load(S0{}, t);
+            multiply(S1{});
+            load(S1{}, t + 1);
+        }
+        multiply(S0{});
+        multiply(S1{});
+    } else {
+        // four steps at a time, the last two of an odd pair on their own
+        using S2 = std::integral_constant<int, 2>;
+        using S3 = std::integral_constant<int, 3>;
+        int t = 2;
+        for (; t + 4 <= total; t += 4) {
+            load(S2{}, t);
+            load(S3{}, t + 1);
+            multiply(S0{});
+            multiply(S1{});
+            load(S0{}, t + 2);
+            load(S1{}, t + 3);
+            multiply(S2{});
+            multiply(S3{});
+        }
+        if (t < total) {
+            load(S2{}, t);
+            load(S3{}, t + 1);
+            multiply(S0{});
+            multiply(S1{});
+            multiply(S2{});
+            multiply(S3{});
         } else {
-            if (s + 1 < steps) step(std::integral_constant<int, 1>{}, sw, sx, s + 1);
-            if (s + 2 < steps) step(std::integral_constant<int, 2>{}, sw, sx, s + 2);
+            multiply(S0{});
+            multiply(S1{});
         }
     }
 }
 
-template <int CF, int TM>
-__device__ __forceinline__ void mx4_zero(f32x4_t (&acc)[CF][TM]) {
-#pragma unroll
-    for (int c = 0; c < CF; ++c)
-#pragma unroll
-        for (int t = 0; t < TM; ++t) acc[c][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-}
-
-// Up to four consecutive outputs x of token m from column f: `n` of them real.
-template <typename T>
-__device__ __forceinline__ void mx4_store(const Mx4Args &a, int64_t m, int64_t f, int n, f32x4_t x) {
-    if (n <= 0 || m >= a.M) return;
-    const T *bias = static_cast<const T *>(a.bias);
-    if (bias) {
-#pragma unroll
-        for (int v = 0; v < 4; ++v) x[v] += v < n ? load_f32<T>(bias, f + v) : 0.f;
-    }
-    if (a.gelu) {
-#pragma unroll
-        for (int v = 0; v < 4; ++v) x[v] = sizeof(T) == 2 ? gelu(x[v]) : gelu_f32(x[v]);
-    }
-    T *dst = static_cast<T *>(a.Y) + m * a.n_out + f;
-    if (n >= 4 && ((uintptr_t)dst & (4 * sizeof(T) - 1)) == 0) {
-        if constexpr (sizeof(T) == 2)
-            *reinterpret_cast<uint2 *>(dst) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
-        else
-            *reinterpret_cast<f32x4_t *>(dst) = x;
-    } else {
-#pragma unroll
-        for (int v = 0; v < 4; ++v)
-            if (v < n) store_f32<T>(dst, v, x[v]);
-    }
-}
-
-// No output transpose: block i's columns take block i of both components; a
-// wave owns CF x TM fragments of one block, a workgroup 2 x 2 waves.
-template <int CF, int TM, typename T>
-__global__ void __launch_bounds__(256) mx4_gemm_kernel(Mx4Args a) {
+// No output transpose: a wave owns SN x SM fragments of one block.
+template <int SN, int SM, int PF, typename T>
+__global__ void __launch_bounds__(256, 2) mx4_gemm_kernel(Mx4Args a) {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int tile = xcd_tile(blockIdx.x, a.tiles);
-    const int per_block = a.tiles_n / a.D;
+    const int per_block = a.tiles_n / a.D, wm = 4 / a.wave_n;
     const int tn = tile % a.tiles_n, g = tn / per_block;
-    const int c0 = (tn - g * per_block) * 2 * CF + (wave & 1) * CF;
-    const int t0 = (tile / a.tiles_n) * 2 * TM + (wave >> 1) * TM;
+    const int c0 = ((tn - g * per_block) * a.wave_n + wave % a.wave_n) * SN;
+    const int t0 = (tile / a.tiles_n * wm + wave / a.wave_n) * SM;
     if (c0 >= a.w_frags || t0 >= a.x_frags) return;
-    f32x4_t acc[CF][TM];
+    const Mx4Wave v{{g, a.D + g}, {c0, c0}, {g, a.in_t ? a.D + g : g}, t0};
+    f32x4_t acc[SN][SM];
     mx4_zero(acc);
-#pragma unroll 1
-    for (int comp = 0; comp < 2; ++comp) {
-        Mx4Frags<CF, TM> f;
-        const int64_t wp = (int64_t)(comp * a.D + g) * a.w_frags, xp = (int64_t)(comp && a.in_t ? a.D + g : g) * a.x_frags;
+    mx4_loop<SN, SM, PF>(a, v, lane, acc);
+    mx4_epilogue<SN, SM, T>(a, g, c0, t0, lane, acc);
+}
+
+// Output transpose by residue: wave g of D makes the SN fragments jl0.. of
+// residue g in a block.  out: rows of 16 * SN * D columns for 16 tokens.
+template <int SN, int SM, int PF, typename T>
+__global__ void __launch_bounds__(SN * SM >= 16 ? 512 : 1024) mx4_gemm_res_kernel(Mx4Args a) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    T *out = reinterpret_cast<T *>(smem);
+    const int lane = threadIdx.x & 63;
+    const int g = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tile = xcd_tile(blockIdx.x, a.tiles);
+    const int D = a.D, per = a.bo / (16 * D);             // fragments of a residue in a block
+    const int tn = tile % a.tiles_n, jf0 = tn * SN, i1 = jf0 / per;
+    const int t0 = tile / a.tiles_n * SM;
+    const Mx4Wave v{{i1, D + g}, {g * per + jf0 - i1 * per, jf0}, {i1, a.in_t ? D + g : g}, t0};
+    f32x4_t acc[SN][SM];
+    mx4_zero(acc);
+    mx4_loop<SN, SM, PF>(a, v, lane, acc);
+
+    constexpr int E = sizeof(T);
+    const int N = 16 * SN * D, pitch = N + 16 / E;
+    const int64_t f0 = (int64_t)tn * N;
+    const int row = lane & 15, quad = 4 * (lane >> 4);
+    const T *bias = static_cast<const T *>(a.bias);
+    float b[SN][4];
 #pragma unroll
-        for (int c = 0; c < CF; ++c) f.w[c] = wp + (c0 + c < a.w_frags ? c0 + c : a.w_frags - 1);
+    for (int j = 0; j < SN; ++j)
 #pragma unroll
-        for (int t = 0; t < TM; ++t) f.x[t] = xp + (t0 + t < a.x_frags ? t0 + t : a.x_frags - 1);
-        mx4_span<CF, TM>(a, f, lane, acc);
-    }
+        for (int q = 0; q < 4; ++q) {
+            const int64_t f = f0 + (16 * j + quad + q) * D + g;
+            b[j][q] = bias && f < a.n_out ? load_f32<T>(bias, f) : 0.f;
+        }
 #pragma unroll
-    for (int c = 0; c < CF; ++c) {
-        const int r = (c0 + c) * 16 + 4 * (lane >> 4);
-        const int64_t col = (int64_t)g * a.bo + r;
-        const int64_t left = a.bo - r < a.n_out - col ? a.bo - r : a.n_out - col;
+    for (int i = 0; i < SM; ++i) {
+        if (i) __syncthreads();
 #pragma unroll
-        for (int t = 0; t < TM; ++t)
-            if (c0 + c < a.w_frags) mx4_store<T>(a, (int64_t)(t0 + t) * 16 + (lane & 15), col, left < 4 ? (int)left : 4, acc[c][t]);
+        for (int j = 0; j < SN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                store_f32<T>(out, row * pitch + (16 * j + quad + q) * D + g, mx4_act<T>(a, acc[j][i][q] + b[j][q]));
+        __syncthreads();
+        const int64_t m0 = (int64_t)(t0 + i) * 16;
+        const int real = (int)(a.M - m0 < 16 ? a.M - m0 : 16), cols = (int)(a.n_out - f0 < N ? a.n_out - f0 : N);
+        T *dst = static_cast<T *>(a.Y) + m0 * a.n_out + f0;
+        if (a.n_out * E % 16 == 0) {
+            // pieces of 16 bytes, a power of two or a few to a row: N * E / 16 = 2 * SN * D * E / 2
+            const int per_row = cols * E / 16;
+            for (int p = threadIdx.x; p < real * per_row; p += blockDim.x) {
+                const int r = p / per_row, q = p - r * per_row;
+                *reinterpret_cast<uint4 *>(reinterpret_cast<unsigned char *>(dst + r * a.n_out) + 16 * q) =
+                    *reinterpret_cast<const uint4 *>(smem + (r * pitch) * E + 16 * q);
+            }
+        } else {
+            for (int p = threadIdx.x; p < real * cols; p += blockDim.x) {
+                const int r = p / cols, q = p - r * cols;
+                dst[r * a.n_out + q] = out[r * pitch + q];
+            }
+        }
     }
 }
 
-// Output transpose (see the top): 16 * TM tokens x 16 * CF * D columns.
+// ---- output transpose, any block size ---------------------------------------------
+
+template <int CF, int TM>
+struct Mx4Frags {
+    int wp, w[CF], xp, x[TM];   // parts, and fragments in them
+};
+
+template <int CF, int TM>
+__device__ __forceinline__ void mx4_span(const Mx4Args &a, const Mx4Frags<CF, TM> &f, int lane, f32x4_t (&acc)[CF][TM]) {
+    const int steps = a.steps;
+    for (int s = 0; s < steps; ++s) {
+        uint4 w[CF], x[TM];
+        uint32_t sw[CF], sx[TM];
+        auto code = [&](const uint8_t *c, int part, int frags, int n) {
+            return reinterpret_cast<const uint4 *>(c + (((int64_t)part * frags + n) * steps + s) * 1024)[lane];
+        };
+        auto scale = [&](const uint8_t *c, int part, int groups, int n) {
+            return reinterpret_cast<const uint32_t *>(c + (((int64_t)part * groups + (n >> 2)) * steps + s) * 256)[lane] >> (8 * (n & 3));
+        };
+#pragma unroll
+        for (int c = 0; c < CF; ++c) {
+            w[c] = code(a.wc, f.wp, a.w_frags, f.w[c]);
+            sw[c] = scale(a.ws, f.wp, a.w_groups, f.w[c]);
+        }
+#pragma unroll
+        for (int t = 0; t < TM; ++t) {
+            x[t] = code(a.xc, f.xp, a.x_frags, f.x[t]);
+            sx[t] = scale(a.xs, f.xp, a.x_groups, f.x[t]);
+        }
+#pragma unroll
+        for (int c = 0; c < CF; ++c)
+#pragma unroll
+            for (int t = 0; t < TM; ++t) acc[c][t] = mx4_mfma<0, 0>(w[c], x[t], acc[c][t], sw[c], sx[t]);
+    }
+}
+
+// 16 * TM tokens x 16 * CF * D columns: component 2's sums go to their columns
+// in LDS, component 1's fragments over the same columns add to them.
 template <int CF, int TM, typename T>
 __global__ void __launch_bounds__(TM == 4 ? 512 : 1024) mx4_gemm_ot_kernel(Mx4Args a) {
     extern __shared__ __attribute__((aligned(16))) float sums[];
@@ -166,14 +245,15 @@ __global__ void __launch_bounds__(TM == 4 ? 512 : 1024) mx4_gemm_ot_kernel(Mx4Ar
     const int row = lane & 15, quad = 4 * (lane >> 4);
     Mx4Frags<CF, TM> f;
     f32x4_t acc[CF][TM];
+#pragma unroll
+    for (int t = 0; t < TM; ++t) f.x[t] = t0 + t < a.x_frags ? t0 + t : a.x_frags - 1;
 
     for (int g = wave; g < D; g += waves) {
         mx4_zero(acc);
-        const int64_t wp = (int64_t)(D + g) * a.w_frags, xp = (int64_t)(a.in_t ? D + g : g) * a.x_frags;
+        f.wp = D + g;
+        f.xp = a.in_t ? D + g : g;
 #pragma unroll
-        for (int c = 0; c < CF; ++c) f.w[c] = wp + (jf0 + c < a.w_frags ? jf0 + c : a.w_frags - 1);
-#pragma unroll
-        for (int t = 0; t < TM; ++t) f.x[t] = xp + (t0 + t < a.x_frags ? t0 + t : a.x_frags - 1);
+        for (int c = 0; c < CF; ++c) f.w[c] = jf0 + c < a.w_frags ? jf0 + c : a.w_frags - 1;
         mx4_span<CF, TM>(a, f, lane, acc);
 #pragma unroll
         for (int c = 0; c < CF; ++c)
@@ -194,11 +274,9 @@ __global__ void __launch_bounds__(TM == 4 ? 512 : 1024) mx4_gemm_ot_kernel(Mx4Ar
         for (int r0 = lo; r0 < hi; r0 += CF, ++unit) {
             if (unit % waves != wave) continue;
             mx4_zero(acc);
-            const int64_t wp = (int64_t)i * a.w_frags, xp = (int64_t)i * a.x_frags;
+            f.wp = f.xp = i;
 #pragma unroll
-            for (int c = 0; c < CF; ++c) f.w[c] = wp + (r0 + c < hi ? r0 + c : hi - 1);
-#pragma unroll
-            for (int t = 0; t < TM; ++t) f.x[t] = xp + (t0 + t < a.x_frags ? t0 + t : a.x_frags - 1);
+            for (int c = 0; c < CF; ++c) f.w[c] = r0 + c < hi ? r0 + c : hi - 1;
             mx4_span<CF, TM>(a, f, lane, acc);
 #pragma unroll
             for (int c = 0; c < CF; ++c) {
@@ -227,121 +305,26 @@ __global__ void __launch_bounds__(TM == 4 ? 512 : 1024) mx4_gemm_ot_kernel(Mx4Ar
     }
 }
 
-// ---- fragment order ------------------------------------------------------------
-
-// 32 values of a row into codes and a scale byte of fragment order: lane's
-// place in fragment `frag` (numbered part * frags + fragment), step s.
-__device__ __forceinline__ void mx4_put(uint8_t *codes, uint8_t *scales, int64_t frag, int steps, int words, int s, int lane,
-                                        const float (&x)[4][8]) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) top = max(top, mag_bits(x[q][e]));
-    const uint32_t sb = mx_scale<kMxFp4>(top);
-    uint4 c = make_uint4(0u, 0u, 0u, 0u);
-    if (sb != 255u) {
-        const float pow = mx_pow(sb);
-        c = make_uint4(mx_fp4x8(x[0], pow), mx_fp4x8(x[1], pow), mx_fp4x8(x[2], pow), mx_fp4x8(x[3], pow));
-    }
-    reinterpret_cast<uint4 *>(codes + (frag * steps + s) * 1024)[lane] = c;
-    scales[(frag * words + s / 4) * 256 + lane * 4 + s % 4] = (uint8_t)sb;
-}
-
-struct Mx4PackArgs {
-    int64_t M, n_in, n_out;
-    int D, bi, bo, in_t, out_t;
-    const void *W1, *W2, *X;
-    uint8_t *codes, *scales;
-    int parts, frags, steps, words;
-    int64_t items;      // fragments times steps
-};
-
-// A wave a fragment and step; WEIGHTS: part = component * D + block of W1 / W2,
-// else block (or, from D on, residue) of the input.
-template <bool WEIGHTS, typename T>
-__global__ void __launch_bounds__(256) mx4_pack_kernel(Mx4PackArgs a) {
-    const int lane = threadIdx.x & 63;
-    const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (item >= a.items) return;
-    // parts fastest: the waves that read the same rows' residues run together
-    const int part = (int)(item % a.parts), s = (int)(item / a.parts % a.steps);
-    const int64_t fr = item / a.parts / a.steps;
-    const bool second = part >= a.D;
-    const int g = second ? part - a.D : part;
-    const bool strided = second && a.in_t;                // input columns k*D + g
-    const int64_t row = fr * 16 + (lane & 15);
-    const int k0 = s * 128 + (lane >> 4) * 32;
-    const int64_t n = a.n_in;
-    float x[4][8];
-    const T *src;
-    int64_t step;
-    bool real;
-    if constexpr (WEIGHTS) {
-        src = static_cast<const T *>(second ? a.W2 : a.W1) + ((int64_t)g * a.bo + row) * a.bi;
-        const int64_t out = second && a.out_t ? row * a.D + g : (int64_t)g * a.bo + row;
-        real = row < a.bo && out < a.n_out;
-        step = 1;
-    } else {
-        src = static_cast<const T *>(a.X) + row * n + (strided ? g : (int64_t)g * a.bi);
-        real = row < a.M;
-        step = strided ? a.D : 1;
-    }
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int k = k0 + 8 * q + e;
-            const int64_t col = strided ? (int64_t)k * a.D + g : (int64_t)g * a.bi + k;
-            x[q][e] = real && k < a.bi && col < n ? load_f32<T>(src, k * step) : 0.f;
-        }
-    mx4_put(a.codes, a.scales, part * (int64_t)a.frags + fr, a.steps, a.words, s, lane, x);
-}
-
-template <bool WEIGHTS>
-hipError_t run_pack(Mx4PackArgs &a, const Mx4Layout &l, int dtype, hipStream_t s) {
-    if (l.frags >= ((int64_t)1 << 31) || l.parts >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
-    a.parts = (int)l.parts; a.frags = (int)l.frags; a.steps = (int)l.steps; a.words = (int)l.words();
-    a.scales = a.codes + l.code_bytes();
-    a.items = l.parts * l.frags * l.steps;
-    const int64_t grid = (a.items + 3) / 4;
-    if (grid >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
-    if (dtype == kBF16) mx4_pack_kernel<WEIGHTS, uint16_t><<<(unsigned)grid, 256, 0, s>>>(a);
-    else mx4_pack_kernel<WEIGHTS, float><<<(unsigned)grid, 256, 0, s>>>(a);
-    return hipGetLastError();
-}
+template <int N>
+using Int = std::integral_constant<int, N>;
 
 }  // namespace
 
-hipError_t launch_mx4_pack(int64_t n_in, int64_t n_out, int64_t D, bool in_t, bool out_t, int dtype, const void *W1,
-                           const void *W2, void *packed, hipStream_t s) {
-    Mx4PackArgs a{};
-    a.n_in = n_in; a.n_out = n_out; a.D = (int)D;
-    a.bi = (int)((n_in + D - 1) / D); a.bo = (int)((n_out + D - 1) / D);
-    a.in_t = in_t; a.out_t = out_t;
-    a.W1 = W1; a.W2 = W2;
-    a.codes = static_cast<uint8_t *>(packed);
-    return run_pack<true>(a, mx4_weights_layout(D, a.bi, a.bo), dtype, s);
-}
-
 hipError_t launch_mx4_forward(const Mx4Pass &p, hipStream_t s) {
-    const Mx4Layout wl = mx4_weights_layout(p.D, p.bi, p.bo), xl = mx4_input_layout(p.D, p.bi, p.M, p.in_t);
-    Mx4PackArgs q{};
-    q.M = p.M; q.n_in = p.n_in; q.n_out = p.n_out; q.D = (int)p.D; q.bi = (int)p.bi; q.bo = (int)p.bo;
-    q.in_t = p.in_t; q.out_t = p.out_t;
-    q.X = p.X;
-    q.codes = static_cast<uint8_t *>(p.ws);
-    hipError_t e = run_pack<false>(q, xl, p.dtype, s);
+    hipError_t e = launch_mx4_input(p, s);
     if (e != hipSuccess) return e;
-
+    const bool in_t = p.in_t && p.D > 1, out_t = p.out_t && p.D > 1;
+    const Mx4Layout wl = mx4_weights_layout(p.D, p.bi, p.bo), xl = mx4_input_layout(p.D, p.bi, p.M, in_t);
     Mx4Args a{};
     a.M = p.M; a.n_in = p.n_in; a.n_out = p.n_out; a.D = (int)p.D; a.bi = (int)p.bi; a.bo = (int)p.bo;
     a.wc = static_cast<const uint8_t *>(p.packed);
     a.ws = a.wc + wl.code_bytes();
     a.xc = static_cast<const uint8_t *>(p.ws);
     a.xs = a.xc + xl.code_bytes();
-    a.w_frags = (int)wl.frags; a.x_frags = (int)xl.frags; a.steps = (int)wl.steps; a.words = (int)wl.words();
-    a.bias = p.bias; a.Y = p.Y; a.gelu = p.gelu; a.in_t = p.in_t;
+    a.w_frags = (int)wl.frags; a.w_groups = (int)wl.groups();
+    a.x_frags = (int)xl.frags; a.x_groups = (int)xl.groups();
+    a.steps = (int)wl.steps;
+    a.bias = p.bias; a.Y = p.Y; a.gelu = p.gelu; a.in_t = in_t;
     auto tiles = [&](int64_t n, int64_t m) -> bool {
         if (n * m >= ((int64_t)1 << 31)) return false;
         a.tiles_n = (int)n;
@@ -352,18 +335,42 @@ hipError_t launch_mx4_forward(const Mx4Pass &p, hipStream_t s) {
         if (p.dtype == kBF16) go(uint16_t{});
         else go(float{});
     };
-    const int64_t xf = xl.frags, wf = wl.frags;
-    if (!p.out_t || p.D == 1) {
-        const bool small = xf <= 2;
-        if (!tiles(p.D * ((wf + (small ? 1 : 7)) / (small ? 2 : 8)), small ? (xf + 1) / 2 : (xf + 7) / 8)) return hipErrorInvalidValue;
-        by_type([&](auto t) {
-            using T = decltype(t);
-            if (small) mx4_gemm_kernel<1, 1, T><<<(unsigned)a.tiles, 256, 0, s>>>(a);
-            else mx4_gemm_kernel<4, 4, T><<<(unsigned)a.tiles, 256, 0, s>>>(a);
-        });
-        return hipGetLastError();
+    const int64_t xf = xl.frags, wf = wl.frags, D = p.D;
+    if (!out_t) {
+        auto plain = [&](auto sn, auto sm, auto pf, int wave_n) -> hipError_t {
+            constexpr int SN = decltype(sn)::value, SM = decltype(sm)::value, PF = decltype(pf)::value;
+            const int64_t bn = (int64_t)SN * wave_n, bm = (int64_t)SM * (4 / wave_n);
+            a.wave_n = wave_n;
+            if (!tiles(D * ((wf + bn - 1) / bn), (xf + bm - 1) / bm)) return hipErrorInvalidValue;
+            by_type([&](auto t) { mx4_gemm_kernel<SN, SM, PF, decltype(t)><<<(unsigned)a.tiles, 256, 0, s>>>(a); });
+            return hipGetLastError();
+        };
+        // the largest wave tile that still gives every SIMD two waves
+        auto waves = [&](int sn, int sm) { return D * ((wf + sn - 1) / sn) * ((xf + sm - 1) / sm); };
+        if (xf >= 4 && waves(4, 4) >= 2048) return plain(Int<4>{}, Int<4>{}, Int<2>{}, 2);
+        if (xf >= 2 && waves(2, 2) >= 2048) return plain(Int<2>{}, Int<2>{}, Int<2>{}, 2);
+        return plain(Int<1>{}, Int<1>{}, Int<4>{}, xf >= 2 ? 2 : 4);
     }
-    const int64_t D = p.D, waves = D < 16 ? D : 16;
+    if (mx4_by_residue(D, p.bo, out_t)) {
+        const int64_t per = p.bo / (16 * D), all = (p.n_out + 16 * D - 1) / (16 * D);
+        auto res = [&](auto sn, auto sm, auto pf) -> hipError_t {
+            constexpr int SN = decltype(sn)::value, SM = decltype(sm)::value, PF = decltype(pf)::value;
+            if (!tiles((all + SN - 1) / SN, (xf + SM - 1) / SM)) return hipErrorInvalidValue;
+            by_type([&](auto t) {
+                using T = decltype(t);
+                const size_t lds = 16 * ((size_t)(16 * SN * D) * sizeof(T) + 16);
+                mx4_gemm_res_kernel<SN, SM, PF, T><<<(unsigned)a.tiles, (unsigned)(64 * D), lds, s>>>(a);
+            });
+            return hipGetLastError();
+        };
+        auto waves = [&](int sn, int sm) { return D * ((all + sn - 1) / sn) * ((xf + sm - 1) / sm); };
+        if (per % 4 == 0 && xf >= 4 && waves(4, 4) >= 2048 && D <= 8) return res(Int<4>{}, Int<4>{}, Int<2>{});
+        if (per % 2 == 0 && xf >= 4 && waves(2, 4) >= 2048) return res(Int<2>{}, Int<4>{}, Int<2>{});
+        if (xf >= 4 && waves(1, 4) >= 2048) return res(Int<1>{}, Int<4>{}, Int<2>{});
+        if (xf >= 2) return res(Int<1>{}, Int<2>{}, Int<2>{});
+        return res(Int<1>{}, Int<1>{}, Int<4>{});
+    }
+    const int64_t waves = D < 16 ? D : 16;
     auto ot = [&](auto cf, auto tm) -> hipError_t {
         constexpr int CF = decltype(cf)::value, TM = decltype(tm)::value;
         const int64_t N = 16 * CF * D;
@@ -372,13 +379,10 @@ hipError_t launch_mx4_forward(const Mx4Pass &p, hipStream_t s) {
         by_type([&](auto t) { mx4_gemm_ot_kernel<CF, TM, decltype(t)><<<(unsigned)a.tiles, (unsigned)(64 * waves), lds, s>>>(a); });
         return hipGetLastError();
     };
-    using One = std::integral_constant<int, 1>;
-    using Two = std::integral_constant<int, 2>;
-    using Four = std::integral_constant<int, 4>;
-    if (xf <= 1) return ot(One{}, One{});
-    if (D <= 8) return ot(Four{}, Four{});
-    if (D <= 16) return ot(Four{}, Two{});
-    return ot(Four{}, One{});
+    if (xf <= 1) return ot(Int<1>{}, Int<1>{});
+    if (D <= 8) return ot(Int<4>{}, Int<4>{});
+    if (D <= 16) return ot(Int<4>{}, Int<2>{});
+    return ot(Int<4>{}, Int<1>{});
 }
 
 }  // namespace dyad

@@ -46,9 +46,9 @@ def test_quantize_rejects(call, args, code):
 
 
 def test_mx4_sizes():
-    # blocks of 192: two steps of 128 reduction indices, 1 KB of codes and a word of scales a lane
-    # (256 bytes) for each fragment of 16 rows
-    assert dy.dyad_mx4_weight_bytes(dy.IT, 768, 768, 4) == 2 * 4 * 12 * (2 * 1024 + 256)
+    # blocks of 192: two steps of 128 reduction indices, each 1 KB of codes for a fragment of 16 rows
+    # and 256 bytes of scales for four of them
+    assert dy.dyad_mx4_weight_bytes(dy.IT, 768, 768, 4) == 2 * 4 * 2 * (12 * 1024 + 3 * 256)
     assert dy.dyad_mx4_workspace_bytes(dy.OT, 768, 768, 4, 17) == 4 * 2 * (2 * 1024 + 256)
     assert dy.dyad_mx4_workspace_bytes(dy.DT, 768, 768, 4, 17) == 2 * 4 * 2 * (2 * 1024 + 256)
     assert dy.dyad_mx4_workspace_bytes(dy.DT, 768, 768, 4, 0) == 0
