@@ -337,6 +337,7 @@ hipError_t launch_mx4_forward(const Mx4Pass &p, hipStream_t s) {
     };
     const int64_t xf = xl.frags, wf = wl.frags, D = p.D;
     if (!out_t) {
+        if (const hipError_t pp = launch_mx4_tiles(a, p.dtype == kBF16, s); pp != hipErrorNotSupported) return pp;
         auto plain = [&](auto sn, auto sm, auto pf, int wave_n) -> hipError_t {
             constexpr int SN = decltype(sn)::value, SM = decltype(sm)::value, PF = decltype(pf)::value;
             const int64_t bn = (int64_t)SN * wave_n, bm = (int64_t)SM * (4 / wave_n);
