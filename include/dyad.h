@@ -254,7 +254,9 @@ int dyad_mx4_forward(dyad_variant variant, int64_t n_in, int64_t n_out, int64_t 
  *   dyad_forward_mx8      dyad_forward with GELU, whose pre-activation H is kept as
  *                         H8 / Hs, the quantised value of what H would hold
  *   dyad_backward_dx_mx8  dyad_backward_dx with act_in GELU at the kept H:
- *                         dX = (W^T dZ) * GELU'(H8)
+ *                         dX = (W^T dZ) * GELU'(H8).  A, when not NULL, receives
+ *                         GELU(H8) [M][n_in], this layer's input, for the weight
+ *                         gradient (dyad_backward_dw)
  *   dyad_backward_dw_mx8  dyad_backward_dw with X read from X8 / Xs; with act_in
  *                         GELU the layer's input is GELU(X8)
  * H8 [M][n_out] for the forward pass, [M][n_in] for the input gradient; X8 [M][n_in].
@@ -269,7 +271,7 @@ int dyad_forward_mx8(dyad_variant variant, int64_t n_in, int64_t n_out, int64_t 
                      void *workspace, size_t workspace_bytes, hipStream_t stream);
 int dyad_backward_dx_mx8(dyad_variant variant, int64_t n_in, int64_t n_out, int64_t n_dyad, int64_t M,
                          dyad_dtype dtype, const void *dZ, const void *W1, const void *W2, const void *H8,
-                         const void *Hs, void *dX, void *workspace, size_t workspace_bytes, hipStream_t stream);
+                         const void *Hs, void *dX, void *A, void *workspace, size_t workspace_bytes, hipStream_t stream);
 int dyad_backward_dw_mx8(dyad_variant variant, int64_t n_in, int64_t n_out, int64_t n_dyad, int64_t M,
                          dyad_dtype dtype, dyad_act act_in, const void *dZ, const void *X8, const void *Xs, void *dW1,
                          void *dW2, void *dbias, void *workspace, size_t workspace_bytes, hipStream_t stream);

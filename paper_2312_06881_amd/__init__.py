@@ -101,7 +101,7 @@ def _load():
             ("dyad_mx4_forward", _int, [_int, _i64, _i64, _i64, _i64, _int, _vp, _vp, size, _vp, _int, _vp, _vp, size, _vp]),
             ("dyad_mx8_workspace_bytes", size, [_int, _int, _i64, _i64, _i64, _i64, _int, _int]),
             ("dyad_forward_mx8", _int, [_int, _i64, _i64, _i64, _i64, _int, *[_vp] * 8, size, _vp]),
-            ("dyad_backward_dx_mx8", _int, [_int, _i64, _i64, _i64, _i64, _int, *[_vp] * 7, size, _vp]),
+            ("dyad_backward_dx_mx8", _int, [_int, _i64, _i64, _i64, _i64, _int, *[_vp] * 8, size, _vp]),
             ("dyad_backward_dw_mx8", _int, [_int, _i64, _i64, _i64, _i64, _int, _int, *[_vp] * 7, size, _vp])):
         fn = getattr(lib, name)
         fn.restype, fn.argtypes = restype, args
@@ -193,9 +193,9 @@ def dyad_forward_mx8(variant, n_in, n_out, n_dyad, M, dtype, X, W1, W2, bias, Y,
                                     workspace_bytes, stream)
 
 
-def dyad_backward_dx_mx8(variant, n_in, n_out, n_dyad, M, dtype, dZ, W1, W2, H8, Hs, dX, workspace,
+def dyad_backward_dx_mx8(variant, n_in, n_out, n_dyad, M, dtype, dZ, W1, W2, H8, Hs, dX, A, workspace,
                          workspace_bytes, stream) -> int:
-    return _load().dyad_backward_dx_mx8(variant, n_in, n_out, n_dyad, M, dtype, dZ, W1, W2, H8, Hs, dX, workspace,
+    return _load().dyad_backward_dx_mx8(variant, n_in, n_out, n_dyad, M, dtype, dZ, W1, W2, H8, Hs, dX, A, workspace,
                                         workspace_bytes, stream)
 
 

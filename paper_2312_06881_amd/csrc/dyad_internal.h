@@ -41,6 +41,10 @@ struct GemmPass {
     int epilogue;    // Epilogue
     const void *in, *W1, *W2, *bias, *h_in;
     void *out, *h_out;
+    // bf16, Nout a multiple of 32: the pre-activation in microscaled int8 blocks
+    // (mx_common.h), written in place of h_out or read in place of h_in; null: none
+    uint8_t *h8, *hs;
+    void *a_out;     // kEpiGeluGrad with h8: receives GELU(h); null: not wanted
 };
 
 // Weight/bias gradient of one layer (forward-variant flags in_t/out_t):

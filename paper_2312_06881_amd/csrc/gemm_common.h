@@ -6,6 +6,7 @@
 
 #include "dyad_internal.h"
 #include "mfma_common.h"
+#include "mx_common.h"
 
 namespace dyad {
 
@@ -13,6 +14,8 @@ struct GemmArgs {
     int64_t M, Kin, Nout, bk, bn, D;
     const uint16_t *in, *W1, *W2, *bias, *h_in;
     uint16_t *out, *h_out;
+    uint8_t *h8, *hs;   // the pre-activation in 8 bits (GemmPass)
+    uint16_t *a_out;    // GELU of it (GemmPass)
     int epilogue;
     int tiles_n;        // output tiles per token panel
     int tiles_total;
@@ -33,6 +36,35 @@ struct GemmArgs {
 
 // One launch of the block-ordered large tiles (gemm_pp.h), form a PPForm (pp_plan.h).
 hipError_t launch_pp(int form, bool w_t, const GemmArgs &a, hipStream_t s);
+
+// Eight values of the 8-bit pre-activation at byte vo of the bf16 rows: their
+// codes (x, y) and scale byte (z).
+__device__ __forceinline__ uint4 load_h8(__amdgpu_buffer_rsrc_t codes, __amdgpu_buffer_rsrc_t scales, uint32_t vo) {
+    const auto c = __builtin_amdgcn_raw_buffer_load_b64(codes, (int)(vo >> 1), 0, kStreamPolicy);
+    return make_uint4(c[0], c[1], __builtin_amdgcn_raw_buffer_load_b8(scales, (int)(vo >> 6), 0, 0), 0u);
+}
+
+// The values as bf16 holds them (what the stashed pre-activation would be).
+__device__ __forceinline__ void bf16_values(const float (&x)[8], float (&r)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        const uint32_t w = pack_bf16(x[e], x[e + 1]);
+        r[e] = unpack_bf16(w, 0);
+        r[e + 1] = unpack_bf16(w, 1);
+    }
+}
+
+// Eight of a 32-block's values, each quad of lanes holding a block.
+__device__ __forceinline__ void store_h8(__amdgpu_buffer_rsrc_t codes, __amdgpu_buffer_rsrc_t scales, uint32_t vo,
+                                         const float (&x)[8]) {
+    float r[8];
+    bf16_values(x, r);
+    const uint32_t s = mx_scale<kMxInt8>(quad_max(mag_max(r)));
+    typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
+    const u32x2_t c = {mx_int8x4(r[0], r[1], r[2], r[3], s), mx_int8x4(r[4], r[5], r[6], r[7], s)};
+    __builtin_amdgcn_raw_buffer_store_b64(c, codes, (int)(vo >> 1), 0, kStreamPolicy);
+    if ((vo & 48u) == 0u) __builtin_amdgcn_raw_buffer_store_b8((unsigned char)s, scales, (int)(vo >> 6), 0, 0);
+}
 
 // Epilogue of a BM x BN tile whose accumulators sit in the MFMA layout (wave w
 // owns rows (w / WGN) * WM + 16 i + 4 (lane / 16) + v and internal columns
@@ -72,8 +104,17 @@ __device__ __forceinline__ void gemm_epilogue_as(const GemmArgs &a, unsigned cha
     const uint32_t rows_t = (uint32_t)(rows_left < BM ? rows_left : BM);
     const uint32_t o_bytes = rows_t * (uint32_t)a.Nout * 2u;
     const __amdgpu_buffer_rsrc_t rO = buffer_rsrc(a.out + m0 * a.Nout, o_bytes);
-    const uint16_t *hbase = grad ? a.h_in : a.h_out;
+    // (an 8-bit pre-activation is elsewhere: rH is then where GELU of it goes)
+    const uint16_t *hbase = grad ? (a.a_out ? a.a_out : a.h_in) : a.h_out;
     const __amdgpu_buffer_rsrc_t rH = buffer_rsrc((hbase ? hbase : a.out) + m0 * a.Nout, o_bytes);
+    // the pre-activation in 8 bits: a byte a value and one for 32, so a value at
+    // byte v of the bf16 rows is at v / 2 of the codes and v / 64 of the scales
+    const bool h8 = !PARTIAL && a.h8 != nullptr;
+    const __amdgpu_buffer_rsrc_t rH8 = buffer_rsrc(h8 ? a.h8 + m0 * a.Nout : nullptr, h8 ? o_bytes / 2 : 0u);
+    const __amdgpu_buffer_rsrc_t rHs = buffer_rsrc(h8 ? a.hs + m0 * (a.Nout / 32) : nullptr, h8 ? o_bytes / 64 : 0u);
+    auto load_h = [&](uint32_t vo) __attribute__((always_inline)) -> uint4 {
+        return h8 ? load_h8(rH8, rHs, vo) : bload16_stream(rH, vo, 0);
+    };
     const uint32_t row16 = 16u * (uint32_t)a.Nout * 2u;  // bytes between block rows
 
     uint32_t voE[kQ];
@@ -97,7 +138,7 @@ __device__ __forceinline__ void gemm_epilogue_as(const GemmArgs &a, unsigned cha
         ADD ? buffer_rsrc(a.part + ((int64_t)a.slice0 * a.M + m0) * a.Nout, 2u * o_bytes) : rO;
     if (grad) {
 #pragma unroll
-        for (int q = 0; q < kQ; ++q) hq[0][q] = bload16_stream(rH, voE[q], 0);
+        for (int q = 0; q < kQ; ++q) hq[0][q] = load_h(voE[q]);
     }
 
 #pragma unroll
@@ -139,7 +180,7 @@ __device__ __forceinline__ void gemm_epilogue_as(const GemmArgs &a, unsigned cha
         __syncthreads();
         if (grad && i + 1 < C::kSubM) {
 #pragma unroll
-            for (int q = 0; q < kQ; ++q) hq[(i + 1) & 1][q] = bload16_stream(rH, voE[q] + (uint32_t)(i + 1) * row16, 0);
+            for (int q = 0; q < kQ; ++q) hq[(i + 1) & 1][q] = load_h(voE[q] + (uint32_t)(i + 1) * row16);
         }
 #pragma unroll
         for (int q = 0; q < kQ; ++q) {
@@ -183,9 +224,18 @@ __device__ __forceinline__ void gemm_epilogue_as(const GemmArgs &a, unsigned cha
                 for (int e = 0; e < 8; ++e) x[e] += pa[q][e];
             }
             if (grad) {
-                const uint4 h = hq[i & 1][q];
+                uint4 h = hq[i & 1][q];
+                if (h8) h = mx_int8_bf16(h.x, h.y, h.z);
+                if (h8 && a.a_out) {
+                    float g[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] *= gelu_grad(unpack_bf16(word_of(h, e >> 1), e & 1));
+                    for (int e = 0; e < 8; ++e) x[e] *= gelu_grad_and(unpack_bf16(word_of(h, e >> 1), e & 1), g[e]);
+                    bstore16(rH, vo, make_uint4(pack_bf16(g[0], g[1]), pack_bf16(g[2], g[3]), pack_bf16(g[4], g[5]),
+                                                pack_bf16(g[6], g[7])));
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] *= gelu_grad(unpack_bf16(word_of(h, e >> 1), e & 1));
+                }
             } else {
                 if (bias) {
                     const uint4 b = bq[kBiasQ == 1 ? 0 : q];
@@ -196,6 +246,7 @@ __device__ __forceinline__ void gemm_epilogue_as(const GemmArgs &a, unsigned cha
                     if (keep_h)
                         bstore16(rH, vo, make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]),
                                                     pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])));
+                    if (h8) store_h8(rH8, rHs, vo, x);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) x[e] = gelu(x[e]);
                 }

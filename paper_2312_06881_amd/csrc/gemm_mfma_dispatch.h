@@ -55,6 +55,9 @@ hipError_t launch_tile(const GemmPass &p, hipStream_t s, int splits = 0) {
     a.h_in = static_cast<const uint16_t *>(p.h_in);
     a.out = static_cast<uint16_t *>(p.out);
     a.h_out = static_cast<uint16_t *>(p.h_out);
+    a.h8 = p.h8;
+    a.hs = p.hs;
+    a.a_out = static_cast<uint16_t *>(p.a_out);
     a.epilogue = p.epilogue;
     const int64_t tiles_m = (p.M + BM - 1) / BM;
     const int64_t tiles_n = p.Nout / BN;
@@ -85,6 +88,9 @@ hipError_t launch_tile2(const GemmPass &p, hipStream_t s) {
     a.h_in = static_cast<const uint16_t *>(p.h_in);
     a.out = static_cast<uint16_t *>(p.out);
     a.h_out = static_cast<uint16_t *>(p.h_out);
+    a.h8 = p.h8;
+    a.hs = p.hs;
+    a.a_out = static_cast<uint16_t *>(p.a_out);
     a.epilogue = p.epilogue;
     const int64_t tiles_m = (p.M + BM - 1) / BM;
     const int64_t tiles_n = p.Nout / BN;
@@ -120,6 +126,9 @@ hipError_t launch_component(const GemmPass &p, float *part, int slice, bool unpe
         a.h_in = static_cast<const uint16_t *>(p.h_in);
         a.out = static_cast<uint16_t *>(p.out);
         a.h_out = static_cast<uint16_t *>(p.h_out);
+        a.h8 = p.h8;
+        a.hs = p.hs;
+        a.a_out = static_cast<uint16_t *>(p.a_out);
         a.epilogue = p.epilogue;
     }
     const int64_t tiles_m = (p.M + BM - 1) / BM;
@@ -273,6 +282,11 @@ hipError_t launch_permuted_as(const GemmPass &p, bool in_t, bool out_t, hipStrea
         c.out = static_cast<uint16_t *>(p.out) + m0 * p.Nout;
         if (p.h_in) c.h_in = static_cast<const uint16_t *>(p.h_in) + m0 * p.Nout;
         if (p.h_out) c.h_out = static_cast<uint16_t *>(p.h_out) + m0 * p.Nout;
+        if (p.h8) {
+            c.h8 = p.h8 + m0 * p.Nout;
+            c.hs = p.hs + m0 * (p.Nout / 32);
+            if (p.a_out) c.a_out = static_cast<uint16_t *>(p.a_out) + m0 * p.Nout;
+        }
         GemmPass c2 = c;
         c2.W1 = p.W2;
         if (in_t) {

@@ -119,8 +119,13 @@ __device__ __forceinline__ void pp_epilogue(const GemmArgs &a, unsigned char *sm
     }
     const bool rows16 = !PAD || Nr % 8 == 0;               // pieces are 16-byte aligned
     const __amdgpu_buffer_rsrc_t rO = buffer_rsrc(a.out + m0 * Nr, rows_t * Nr * 2u);
-    const uint16_t *hbase = grad ? a.h_in : a.h_out;
+    const uint16_t *hbase = grad ? (a.a_out ? a.a_out : a.h_in) : a.h_out;
     const __amdgpu_buffer_rsrc_t rH = buffer_rsrc((hbase ? hbase : a.out) + m0 * Nr, rows_t * Nr * 2u);
+
+    // the pre-activation in 8 bits, real rows of whole 32-blocks only
+    const bool h8 = !PAD && !RES && a.h8 != nullptr;
+    const __amdgpu_buffer_rsrc_t rH8 = buffer_rsrc(h8 ? a.h8 + m0 * Nr : nullptr, h8 ? rows_t * Nr : 0u);
+    const __amdgpu_buffer_rsrc_t rHs = buffer_rsrc(h8 ? a.hs + m0 * (Nr / 32) : nullptr, h8 ? rows_t * (Nr / 32) : 0u);
 
     float bias[SN][4];
 #pragma unroll
@@ -147,7 +152,10 @@ __device__ __forceinline__ void pp_epilogue(const GemmArgs &a, unsigned char *sm
         const uint32_t row = (uint32_t)(wm0 + 16 * i + lr);
         const int t = wn0 + 32 * jp + piece;
         uint4 h = make_uint4(0u, 0u, 0u, 0u);
-        if (decltype(whole)::value || (rows16 && t >= lo && t + 8 <= nt)) {
+        if (h8) {
+            h = load_h8(rH8, rHs, (row * Nr + (uint32_t)(cb + t)) * 2u);
+            h = mx_int8_bf16(h.x, h.y, h.z);
+        } else if (decltype(whole)::value || (rows16 && t >= lo && t + 8 <= nt)) {
             h = bload16_stream(rH, (row * Nr + (uint32_t)(cb + t)) * 2u, 0);
         } else if (row < rows_t) {
             const uint16_t *src = a.h_in + (m0 + row) * (int64_t)Nr + cb + t;
@@ -177,6 +185,20 @@ __device__ __forceinline__ void pp_epilogue(const GemmArgs &a, unsigned char *sm
             for (int k = 0; k < 8; ++k)
                 if (t + k >= lo && t + k < nt) dst[k] = (uint16_t)(w[k >> 1] >> (16 * (k & 1)));
         }
+    };
+
+    // a 32-block is a column block pair of a token: the four lane rows' eight values each
+    auto store_h = [&](int i, int jp, const float (&x)[8]) {
+        float r[8];
+        bf16_values(x, r);
+        const uint32_t s = mx_scale<kMxInt8>(rows_max(mag_max(r)));
+        uint32_t c0 = mx_int8x4(r[0], r[1], r[2], r[3], s), c1 = mx_int8x4(r[4], r[5], r[6], r[7], s);
+        swap_rows(c0, c1);
+        typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
+        const u32x2_t c = {c0, c1};
+        const uint32_t vo = (uint32_t)(wm0 + 16 * i + lr) * Nr + (uint32_t)(cb + wn0 + 32 * jp);
+        __builtin_amdgcn_raw_buffer_store_b64(c, rH8, (int)(vo + (uint32_t)piece), 0, 0);
+        if (lg == 0) __builtin_amdgcn_raw_buffer_store_b8((unsigned char)s, rHs, (int)(vo / 32u), 0, 0);
     };
 
     // slice through LDS: token rows of a.D runs of `span` columns, one per residue
@@ -259,7 +281,12 @@ __device__ __forceinline__ void pp_epilogue(const GemmArgs &a, unsigned char *sm
                     else x[e] += slice_at(i, j, v);
                 }
             }
-            if (grad) {
+            if (grad && h8 && a.a_out) {
+                float ga[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] *= gelu_grad_and(unpack_bf16(word_of(h[jp], e >> 1), e & 1), ga[e]);
+                store(whole, rH, a.a_out, i, jp, ga);
+            } else if (grad) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] *= gelu_grad(unpack_bf16(word_of(h[jp], e >> 1), e & 1));
             } else {
@@ -267,6 +294,7 @@ __device__ __forceinline__ void pp_epilogue(const GemmArgs &a, unsigned char *sm
                 for (int e = 0; e < 8; ++e) x[e] += bias[2 * jp + (e >> 2)][e & 3];
                 if (act) {
                     if (keep_h) store(whole, rH, a.h_out, i, jp, x);
+                    if (h8) store_h(i, jp, x);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) x[e] = gelu(x[e]);
                 }

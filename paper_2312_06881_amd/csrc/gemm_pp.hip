@@ -134,6 +134,9 @@ hipError_t launch_permuted_pp(const GemmPass &p, hipStream_t s) {
         a.out = out;
         a.h_out = p.h_out ? static_cast<uint16_t *>(p.h_out) + m0 * p.Nout : nullptr;
         a.h_in = p.h_in ? static_cast<const uint16_t *>(p.h_in) + m0 * p.Nout : nullptr;
+        a.h8 = p.h8 ? p.h8 + m0 * p.Nout : nullptr;
+        a.hs = p.h8 ? p.hs + m0 * (p.Nout / 32) : nullptr;
+        a.a_out = p.a_out ? static_cast<uint16_t *>(p.a_out) + m0 * p.Nout : nullptr;
         if (p.in_t) {
             e = launch_deinterleave(a.in, xp, a.M, p.bk, D, s);
             a.in2 = xp;
@@ -147,7 +150,7 @@ hipError_t launch_permuted_pp(const GemmPass &p, hipStream_t s) {
         } else {
             GemmArgs c2 = a;
             c2.in = a.in2; c2.W1 = a.W2;
-            c2.bias = nullptr; c2.h_in = nullptr; c2.out = nullptr; c2.h_out = nullptr; c2.epilogue = kEpiBias;
+            c2.bias = nullptr; c2.h_in = nullptr; c2.out = nullptr; c2.h_out = nullptr; c2.h8 = nullptr; c2.a_out = nullptr; c2.epilogue = kEpiBias;
             c2.part = slice; c2.unperm = 0;
             if (e == hipSuccess) e = launch_pp(kPPSlice, p.w_t, c2, s);
             a.part = slice; a.unperm = 1;

@@ -183,6 +183,15 @@ __device__ __forceinline__ float gelu_grad(float x) {
     return fmaf(x * e, 0.3989422804014327f, cdf);
 }
 
+// GELU'(x), and GELU(x) = x Phi(x) from the same tail.
+__device__ __forceinline__ float gelu_grad_and(float x, float &g) {
+    float e;
+    const float tail = normal_tail(x, e);
+    const float cdf = x >= 0.f ? 1.f - tail : tail;
+    g = x * cdf;
+    return fmaf(x * e, 0.3989422804014327f, cdf);
+}
+
 __device__ __forceinline__ uint32_t gelu2(uint32_t w) { return pack_bf16(gelu(unpack_bf16(w, 0)), gelu(unpack_bf16(w, 1))); }
 
 // GELU of 8 packed bf16 values, each computed in fp32 and rounded once to

@@ -6,6 +6,7 @@
 #include "mx_internal.h"
 
 using namespace dyad::abi;
+using dyad::GemmPass;
 
 static size_t round256(size_t b) { return (b + 255) & ~(size_t)255; }
 
@@ -18,11 +19,39 @@ static int check_matrix(int fmt, int64_t rows, int64_t cols, int dtype) {
 
 static size_t elem(int dtype) { return dtype == DYAD_BF16 ? 2 : 4; }
 
-// Bytes in front of the inner call's own workspace: the checkpoint read back
-// (or, in the forward pass, the pre-activation to quantise).
-static size_t kept_bytes(int pass, int64_t n_in, int64_t n_out, int64_t M, int dtype) {
-    return round256((size_t)M * (size_t)(pass == DYAD_MX8_FORWARD ? n_out : n_in) * elem(dtype));
+// The matrix-core tiles write and read an 8-bit pre-activation in their
+// epilogues.  Other shapes (zero-padded blocks, fp32, n_dyad without tiles) run
+// the plain pass beside a copy of it in the layer's type, a chunk of tokens of at
+// most kChunkBytes at a time, in the workspace.  The weight gradient always reads
+// a copy: staged from 8 bits tile by tile it was slower (OPT-125m fc1 73 us
+// against 66 + 8 for the copy, OPT-350m 157 against 95 + 11; with GELU, which
+// every tile then repeats, OPT-125m fc2 186 against 67 + 41).
+constexpr size_t kChunkBytes = (size_t)64 << 20;
+
+static int64_t chunk_tokens(int64_t n, int64_t M, int dtype) {
+    int64_t c = (int64_t)(kChunkBytes / ((size_t)n * elem(dtype))) / 256 * 256;
+    if (c < 1024) c = 1024;
+    return M < c ? M : c;
 }
+
+// Bytes of the copy in front of the inner call's own workspace.
+static size_t kept_bytes(int pass, int64_t n_in, int64_t n_out, int64_t M, int dtype) {
+    if (pass == DYAD_MX8_DW) return round256((size_t)M * (size_t)n_in * elem(dtype));
+    const int64_t n = pass == DYAD_MX8_FORWARD ? n_out : n_in;
+    return round256((size_t)chunk_tokens(n, M, dtype) * (size_t)n * elem(dtype));
+}
+
+// A pass on the kernels that take its pre-activation in 8 bits.
+static hipError_t run_h8(const GemmPass &p, hipStream_t s) {
+    if (p.dtype != DYAD_BF16 || p.Nout % 32 != 0 || p.Nout != p.D * p.bn) return hipErrorNotSupported;
+    const dyad::WorkspaceHold hold;
+    hipError_t e = dyad::skinny_ok(p) ? dyad::launch_skinny_gemm(p, s) : hipErrorNotSupported;
+    if (e == hipErrorNotSupported) e = dyad::launch_mfma_gemm(p, s);
+    return e;
+}
+
+static const void *rows(const void *p, int64_t m, int64_t n, size_t e) { return static_cast<const char *>(p) + (size_t)m * (size_t)n * e; }
+static void *rows(void *p, int64_t m, int64_t n, size_t e) { return static_cast<char *>(p) + (size_t)m * (size_t)n * e; }
 
 extern "C" {
 
@@ -118,27 +147,63 @@ int dyad_forward_mx8(dyad_variant variant_arg, int64_t n_in, int64_t n_out, int6
     if (M == 0) return DYAD_OK;
     const size_t need = dyad_mx8_workspace_bytes(DYAD_MX8_FORWARD, variant_arg, n_in, n_out, n_dyad, M, dtype_arg, DYAD_ACT_NONE);
     if (need > 0 && (!workspace || workspace_bytes < need)) return DYAD_ERR_WORKSPACE;
-    rc = dyad_forward(variant_arg, n_in, n_out, n_dyad, M, dtype_arg, X, W1, W2, bias, DYAD_ACT_GELU, Y, workspace, stream);
-    if (rc) return rc;
-    return launch_status(dyad::launch_mx_quantize(DYAD_MX_INT8, M, n_out, dtype, workspace, H8, Hs, stream));
+    GemmPass p{};
+    p.M = M; p.Kin = n_in; p.Nout = n_out; p.D = n_dyad; p.bk = block(n_in, n_dyad); p.bn = block(n_out, n_dyad);
+    p.in_t = in_transposed(variant); p.out_t = out_transposed(variant); p.dtype = dtype; p.epilogue = dyad::kEpiBiasGelu;
+    p.in = X; p.W1 = W1; p.W2 = W2; p.bias = bias; p.out = Y;
+    p.h8 = static_cast<uint8_t *>(H8); p.hs = static_cast<uint8_t *>(Hs);
+    const hipError_t e = run_h8(p, stream);
+    if (e != hipErrorNotSupported) return launch_status(e);
+    const int64_t chunk = chunk_tokens(n_out, M, dtype);
+    for (int64_t m = 0; m < M; m += chunk) {
+        const int64_t c = M - m < chunk ? M - m : chunk;
+        rc = dyad_forward(variant_arg, n_in, n_out, n_dyad, c, dtype_arg, rows(X, m, n_in, elem(dtype)), W1, W2, bias,
+                          DYAD_ACT_GELU, rows(Y, m, n_out, elem(dtype)), workspace, stream);
+        if (rc) return rc;
+        rc = launch_status(dyad::launch_mx_quantize(DYAD_MX_INT8, c, n_out, dtype, workspace, rows(H8, m, n_out, 1),
+                                                    rows(Hs, m, (n_out + 31) / 32, 1), stream));
+        if (rc) return rc;
+    }
+    return DYAD_OK;
 }
 
 int dyad_backward_dx_mx8(dyad_variant variant_arg, int64_t n_in, int64_t n_out, int64_t n_dyad, int64_t M,
                          dyad_dtype dtype_arg, const void *dZ, const void *W1, const void *W2, const void *H8,
-                         const void *Hs, void *dX, void *workspace, size_t workspace_bytes, hipStream_t stream) {
+                         const void *Hs, void *dX, void *A, void *workspace, size_t workspace_bytes, hipStream_t stream) {
     const int variant = enum_value(variant_arg), dtype = enum_value(dtype_arg);
-    const int rc = check_sizes(variant, n_in, n_out, n_dyad, M, dtype);
+    int rc = check_sizes(variant, n_in, n_out, n_dyad, M, dtype);
     if (rc) return rc;
     if (!W1 || !W2 || (M > 0 && (!dZ || !dX || !H8 || !Hs))) return DYAD_ERR_INVALID_ARG;
     if (!aligned16(dZ) || !aligned16(W1) || !aligned16(W2) || !aligned16(H8) || !aligned16(Hs) || !aligned16(dX) ||
-        !aligned16(workspace))
+        !aligned16(A) || !aligned16(workspace))
         return DYAD_ERR_ALIGN;
     if (M == 0) return DYAD_OK;
     const size_t need = dyad_mx8_workspace_bytes(DYAD_MX8_DX, variant_arg, n_in, n_out, n_dyad, M, dtype_arg, DYAD_ACT_NONE);
     if (need > 0 && (!workspace || workspace_bytes < need)) return DYAD_ERR_WORKSPACE;
-    const hipError_t e = dyad::launch_mx_dequantize(DYAD_MX_INT8, M, n_in, dtype, H8, Hs, false, workspace, stream);
-    if (e != hipSuccess) return launch_status(e);
-    return dyad_backward_dx(variant_arg, n_in, n_out, n_dyad, M, dtype_arg, dZ, W1, W2, DYAD_ACT_GELU, workspace, dX, stream);
+    GemmPass p{};
+    p.M = M; p.Kin = n_out; p.Nout = n_in; p.D = n_dyad; p.bk = block(n_out, n_dyad); p.bn = block(n_in, n_dyad);
+    p.in_t = out_transposed(variant); p.out_t = in_transposed(variant); p.w_t = true; p.dtype = dtype;
+    p.epilogue = dyad::kEpiGeluGrad;
+    p.in = dZ; p.W1 = W1; p.W2 = W2; p.out = dX;
+    p.h8 = static_cast<uint8_t *>(const_cast<void *>(H8)); p.hs = static_cast<uint8_t *>(const_cast<void *>(Hs));
+    p.a_out = A;
+    const hipError_t e = run_h8(p, stream);
+    if (e != hipErrorNotSupported) return launch_status(e);
+    const int64_t chunk = chunk_tokens(n_in, M, dtype);
+    for (int64_t m = 0; m < M; m += chunk) {
+        const int64_t c = M - m < chunk ? M - m : chunk;
+        rc = launch_status(dyad::launch_mx_dequantize(DYAD_MX_INT8, c, n_in, dtype, rows(H8, m, n_in, 1),
+                                                      rows(Hs, m, (n_in + 31) / 32, 1), false, workspace, stream));
+        if (!rc && A)
+            rc = launch_status(dyad::launch_mx_dequantize(DYAD_MX_INT8, c, n_in, dtype, rows(H8, m, n_in, 1),
+                                                          rows(Hs, m, (n_in + 31) / 32, 1), true,
+                                                          rows(A, m, n_in, elem(dtype)), stream));
+        if (rc) return rc;
+        rc = dyad_backward_dx(variant_arg, n_in, n_out, n_dyad, c, dtype_arg, rows(dZ, m, n_out, elem(dtype)), W1, W2,
+                              DYAD_ACT_GELU, workspace, rows(dX, m, n_in, elem(dtype)), stream);
+        if (rc) return rc;
+    }
+    return DYAD_OK;
 }
 
 int dyad_backward_dw_mx8(dyad_variant variant_arg, int64_t n_in, int64_t n_out, int64_t n_dyad, int64_t M,

@@ -25,16 +25,59 @@ __device__ __forceinline__ uint32_t mx_scale(uint32_t top) {
 // 2^(s - 127), s < 255 (2^-127 is subnormal).
 __device__ __forceinline__ float mx_pow(uint32_t s) { return __uint_as_float(s ? s << 23 : 0x00400000u); }
 
-// int8 code of x: rounded to nearest even at 2^(s - 133), |code| <= 127.
-__device__ __forceinline__ int mx_int8(float x, uint32_t s) {
-    const float k = __builtin_amdgcn_fmed3f(rintf(ldexpf(x, 133 - (int)s)), -127.f, 127.f);
-    return s == 255u ? 0 : (int)k;
+// int8 codes of four values: rounded to nearest even at 2^(s - 133) and at most
+// 127.  Adding 1.5 * 2^23 leaves the code in the sum's low byte.
+__device__ __forceinline__ uint32_t mx_int8x4(float a, float b, float c, float d, uint32_t s) {
+    auto code = [&](float x) {
+        return __float_as_uint(__builtin_amdgcn_fmed3f(ldexpf(x, 133 - (int)s), -127.f, 127.f) + 12582912.f);
+    };
+    const uint32_t ab = __builtin_amdgcn_perm(code(b), code(a), 0x0c0c0400u);
+    const uint32_t cd = __builtin_amdgcn_perm(code(d), code(c), 0x04000c0cu);
+    return s == 255u ? 0u : ab | cd;
 }
 
 // What the codes of a block are multiplied with: NaN for a non-finite block.
 // Products of it with a code are exact in fp32, and in bf16: 7 bits.
 __device__ __forceinline__ float mx_int8_step(uint32_t s) {
     return s == 255u ? __uint_as_float(0x7fc00000u) : ldexpf(1.f, (int)s - 133);
+}
+
+// Values of four codes.  The bytes become unsigned (code + 128), which convert
+// in one instruction; one fused multiply-add takes the 128 off again, exactly.
+__device__ __forceinline__ void mx_int8_values(uint32_t codes, float step, float (&x)[4]) {
+    const uint32_t u = codes ^ 0x80808080u;
+    const float off = -128.f * step;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = fmaf((float)((u >> (8 * e)) & 255u), step, off);
+}
+
+// Eight codes as packed bf16, which holds each exactly.
+__device__ __forceinline__ uint4 mx_int8_bf16(uint32_t lo, uint32_t hi, uint32_t s) {
+    const float step = mx_int8_step(s);
+    float a[4], b[4];
+    mx_int8_values(lo, step, a);
+    mx_int8_values(hi, step, b);
+    return make_uint4(pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3]), pack_bf16(b[0], b[1]), pack_bf16(b[2], b[3]));
+}
+
+// Largest of a value over the four lanes of a quad, and over the four 16-lane rows.
+__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xb1, 0xf, 0xf, true));   // lanes 1, 0, 3, 2
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4e, 0xf, 0xf, true));   // lanes 2, 3, 0, 1
+}
+__device__ __forceinline__ uint32_t rows_max(uint32_t v) {
+    const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = max((uint32_t)a[0], (uint32_t)a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return max((uint32_t)b[0], (uint32_t)b[1]);
+}
+
+// Magnitude bits of the largest of eight.
+__device__ __forceinline__ uint32_t mag_max(const float (&x)[8]) {
+    uint32_t top = mag_bits(x[0]);
+#pragma unroll
+    for (int e = 1; e < 8; ++e) top = max(top, mag_bits(x[e]));
+    return top;
 }
 
 // fp4 codes of two values, the first in the low nibble (nearest even,

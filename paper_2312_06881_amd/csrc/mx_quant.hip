@@ -73,18 +73,12 @@ __global__ void __launch_bounds__(kThreads) mx_quantize_kernel(int64_t rows, int
     }
 #pragma unroll
     for (int q = 0; q < kUnits; ++q) {
-        uint32_t top = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) top = max(top, mag_bits(x[q][e]));
-        top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-        top = max(top, (uint32_t)__shfl_xor((int)top, 2));
-        const uint32_t s = mx_scale<FMT>(top);
+        const uint32_t s = mx_scale<FMT>(quad_max(mag_max(x[q])));
         if (n[q] > 0 && (u[q] & 3u) == 0u) scales[row[q] * nb + u[q] / 4u] = (uint8_t)s;
         if constexpr (FMT == kMxInt8) {
             uint8_t *dst = codes + row[q] * code_row + (int64_t)u[q] * 8;
-            uint32_t w[2] = {0u, 0u};
-#pragma unroll
-            for (int e = 0; e < 8; ++e) w[e >> 2] |= (uint32_t)(mx_int8(x[q][e], s) & 255) << (8 * (e & 3));
+            const uint32_t w[2] = {mx_int8x4(x[q][0], x[q][1], x[q][2], x[q][3], s),
+                                   mx_int8x4(x[q][4], x[q][5], x[q][6], x[q][7], s)};
             if constexpr (VEC) {
                 if (n[q] > 0) *reinterpret_cast<uint2 *>(dst) = make_uint2(w[0], w[1]);
             } else {
@@ -148,11 +142,20 @@ __global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(int64_t rows, i
 #pragma unroll
     for (int q = 0; q < kUnits; ++q) {
         float x[8];
-        const float step = FMT == kMxInt8 ? mx_int8_step(s[q]) : mx_fp4_half_step(s[q]);
+        if constexpr (FMT == kMxInt8) {
+            float lo[4], hi[4];
+            mx_int8_values(w[q][0], mx_int8_step(s[q]), lo);
+            mx_int8_values(w[q][1], mx_int8_step(s[q]), hi);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                x[e] = lo[e];
+                x[4 + e] = hi[e];
+            }
+        }
+        const float half = mx_fp4_half_step(s[q]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            if constexpr (FMT == kMxInt8) x[e] = (float)(int8_t)(w[q][e >> 2] >> (8 * (e & 3))) * step;
-            else x[e] = mx_fp4_twice(w[q][0] >> (4 * e)) * step;
+            if constexpr (FMT == kMxFp4) x[e] = mx_fp4_twice(w[q][0] >> (4 * e)) * half;
             if constexpr (GELU) x[e] = sizeof(T) == 2 ? gelu(x[e]) : gelu_f32(x[e]);
         }
         T *dst = Y + row[q] * cols + (int64_t)u[q] * 8;

@@ -70,7 +70,7 @@ inline bool pp_rounds_filled(int64_t M, int64_t N, int percent) {
 inline bool pp_pays(const GemmPass &p) {
     if (p.M <= 1024 || p.bk % 32 != 0 || p.bn % 64 != 0) return false;
     if (!pp_fits(256, p.Kin, p.Nout, p.D * p.bn * p.bk)) return false;
-    const bool h = p.h_out != nullptr || p.epilogue == kEpiGeluGrad;
+    const bool h = p.h_out != nullptr || p.h8 != nullptr || p.epilogue == kEpiGeluGrad;
     const bool res = pp_res_columns(p);
     const int64_t tiles = (p.M + 255) / 256 * (p.Nout / 256);
     if (p.D >= 8) {

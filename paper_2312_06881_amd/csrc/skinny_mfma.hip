@@ -29,6 +29,7 @@
 // instead, 32 tokens a wave, each looping over chunks of the reduction.
 #include "dyad_internal.h"
 #include "mfma_common.h"
+#include "mx_common.h"
 
 namespace dyad {
 namespace {
@@ -286,7 +287,14 @@ __global__ void __launch_bounds__(256) skinny_reduce_kernel(GemmPass p, const fl
     }
     uint32_t o[4], h[4];
     if (p.epilogue == kEpiGeluGrad) {
-        const uint4 hv = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p.h_in) + e0);
+        uint4 hv;
+        if (p.h8) {
+            const uint2 c = *reinterpret_cast<const uint2 *>(p.h8 + e0);
+            hv = mx_int8_bf16(c.x, c.y, p.hs[e0 / 32]);
+            if (p.a_out) *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p.a_out) + e0) = gelu8(hv);
+        } else {
+            hv = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p.h_in) + e0);
+        }
         const uint32_t hw[4] = {hv.x, hv.y, hv.z, hv.w};
 #pragma unroll
         for (int w = 0; w < 4; ++w)
@@ -309,6 +317,16 @@ __global__ void __launch_bounds__(256) skinny_reduce_kernel(GemmPass p, const fl
                 o[w] = pack_bf16(gelu(x[2 * w]), gelu(x[2 * w + 1]));
             }
             if (p.h_out) *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p.h_out) + e0) = make_uint4(h[0], h[1], h[2], h[3]);
+            if (p.h8) {
+                // rows of whole 32-blocks: a quad of lanes holds one
+                float r[8];
+#pragma unroll
+                for (int v = 0; v < 8; ++v) r[v] = unpack_bf16(h[v >> 1], v & 1);
+                const uint32_t s = mx_scale<kMxInt8>(quad_max(mag_max(r)));
+                *reinterpret_cast<uint2 *>(p.h8 + e0) = make_uint2(mx_int8x4(r[0], r[1], r[2], r[3], s),
+                                                                  mx_int8x4(r[4], r[5], r[6], r[7], s));
+                if ((e0 & 31) == 0) p.hs[e0 / 32] = (uint8_t)s;
+            }
         } else {
 #pragma unroll
             for (int w = 0; w < 4; ++w) o[w] = pack_bf16(x[2 * w], x[2 * w + 1]);

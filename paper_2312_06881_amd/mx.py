@@ -157,8 +157,9 @@ def forward_gelu(x, w1, w2, bias=None, variant="IT", n_out=None):
     return y, h
 
 
-def backward_dx_gelu(dz, w1, w2, h, variant="IT"):
-    """(W^T dz) * GELU'(h) per token, h the kept pre-activation [M, n_in]."""
+def backward_dx_gelu(dz, w1, w2, h, variant="IT", want_act=False):
+    """(W^T dz) * GELU'(h) per token, h the kept pre-activation [M, n_in]; with want_act
+    (that, GELU(h)), the latter being the layer's input."""
     D, bo, bi = w1.shape
     M, n_out = dz.shape
     n_in = _width(h.shape[1], D, bi, "n_in")
@@ -166,10 +167,11 @@ def backward_dx_gelu(dz, w1, w2, h, variant="IT"):
     _kept(h, M, n_in, dz)
     v, dt, zp = _variant(variant), _dtype(dz, w1, w2), _ptr(dz)
     dx = torch.empty((M, n_in), dtype=dz.dtype, device=dz.device)
+    a = torch.empty_like(dx) if want_act else None
     ws, need = _workspace(MX8_DX, v, n_in, n_out, D, M, dt, ACT_NONE, dz.device)
     _check(_dy.dyad_backward_dx_mx8(v, n_in, n_out, D, M, dt, zp, _ptr(w1), _ptr(w2), _ptr(h.codes), _ptr(h.scales),
-                                    _ptr(dx), _ptr(ws), need, _stream(dz)))
-    return dx
+                                    _ptr(dx), _ptr(a), _ptr(ws), need, _stream(dz)))
+    return (dx, a) if want_act else dx
 
 
 def backward_dw(dz, x, n_dyad, variant="IT", want_db=True, act_in="none"):

@@ -182,10 +182,15 @@ class _DyadFFStashFn(torch.autograd.Function):
         dy = dy.contiguous()
         kept_h = _kept(kept[2:], dy, ctx.ffn) if any(need[:7]) else None
         dx = dw1a = dw2a = dba = dw1b = dw2b = dbb = None
-        if any(need[4:7]):
+        if any(need[:4]):
+            # fc2's input comes out beside the gradient through it
+            dz = mx.backward_dx_gelu(dy, w1b, w2b, kept_h, vb, want_act=any(need[4:7]))
+            if any(need[4:7]):
+                dz, a = dz
+                dw1b, dw2b, dbb = backward_dw(dy, a, w1b.shape[0], vb, want_db=ctx.bias[1])
+        elif any(need[4:7]):
             dw1b, dw2b, dbb = mx.backward_dw(dy, kept_h, w1b.shape[0], vb, want_db=ctx.bias[1], act_in="gelu")
         if any(need[:4]):
-            dz = mx.backward_dx_gelu(dy, w1b, w2b, kept_h, vb)
             if need[0]:
                 dx = backward_dx(dz, w1a, w2a, va, n_in=ctx.n_in)
             if any(need[1:4]):

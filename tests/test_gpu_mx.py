@@ -272,13 +272,17 @@ def test_backward_dx(shape, variant, dtype):
     banner("dx", shape, variant, dtype)
     L = layer_inputs(n_in, n_out, D, M, dtype, seed_offset=22)
     kept = mx.quantize(L.H_in.to(DEV))
-    dx = mx.backward_dx_gelu(L.dZ.to(DEV), L.W1.to(DEV), L.W2.to(DEV), kept, variant)
+    args = (L.dZ.to(DEV), L.W1.to(DEV), L.W2.to(DEV), kept, variant)
+    dx = mx.backward_dx_gelu(*args)
+    again, act = mx.backward_dx_gelu(*args, want_act=True)
     torch.cuda.synchronize()
+    assert torch.equal(dx, again)
     rows = np.unique(np.linspace(0, M - 1, min(M, 200)).astype(int))
     hk = ref.values(L.f64("H_in")[rows], "int8")
     want = oracle.backward_dx(variant, n_in, n_out, D, L.f64("dZ")[rows], L.f64("W1"), L.f64("W2"),
                               act_in=oracle.ACT_GELU, H_in=hk)
     assert_close(dx[torch.from_numpy(rows).to(DEV)], want, dtype, "dX")
+    assert_close(act[torch.from_numpy(rows).to(DEV)], gelu64(hk), dtype, "GELU(H)")
 
 
 @pytest.mark.parametrize("act_in", ["none", "gelu"])

@@ -95,7 +95,7 @@ def test_mx8_passes_reject():
     shape = dict(variant=0, n_in=64, n_out=256, n_dyad=4, M=8, dtype=1)
     tail = dict(workspace=FAKE, workspace_bytes=1 << 30, stream=None)
     fwd = dict(shape, X=FAKE, W1=FAKE, W2=FAKE, bias=None, Y=FAKE, H8=FAKE, Hs=FAKE, **tail)
-    dx = dict(shape, dZ=FAKE, W1=FAKE, W2=FAKE, H8=FAKE, Hs=FAKE, dX=FAKE, **tail)
+    dx = dict(shape, dZ=FAKE, W1=FAKE, W2=FAKE, H8=FAKE, Hs=FAKE, dX=FAKE, A=None, **tail)
     dw = dict(shape, act_in=0, dZ=FAKE, X8=FAKE, Xs=FAKE, dW1=FAKE, dW2=FAKE, dbias=None, **tail)
     for call, good, pointers, pass_ in ((dy.dyad_forward_mx8, fwd, ("X", "W1", "W2", "Y", "H8", "Hs"), dy.MX8_FORWARD),
                                         (dy.dyad_backward_dx_mx8, dx, ("dZ", "W1", "W2", "H8", "Hs", "dX"), dy.MX8_DX),
@@ -112,6 +112,7 @@ def test_mx8_passes_reject():
         assert call(**dict(good, dtype=dy.F32, workspace_bytes=need - 1)) == -5
         assert call(**dict(good, dtype=dy.F32, workspace=None)) == -5
     assert dy.dyad_backward_dw_mx8(**dict(dw, act_in=3)) == -1
+    assert dy.dyad_backward_dx_mx8(**dict(dx, A=FAKE + 2)) == -3
     for call, good in ((dy.dyad_forward_mx8, fwd), (dy.dyad_backward_dx_mx8, dx)):
         assert call(**dict(good, M=0, workspace=None, workspace_bytes=0)) == 0
     assert dy.dyad_mx8_workspace_bytes(3, 0, 64, 256, 4, 8, 1, 0) == 0
