@@ -240,7 +240,7 @@ int dyad_mx4_quantize_weights(dyad_variant variant, int64_t n_in, int64_t n_out,
  * X[m][i*bi + k], component 2 the same or, under an input transpose, the
  * residues X[m][k*n_dyad + i], 32 consecutive k to a scale.  X is quantised within
  * the call, each token on its own, into the workspace of
- * dyad_mx4_workspace_bytes() bytes.  With Dyad-OT / -DT, n_dyad above 32 returns
+ * dyad_mx4_workspace_bytes() bytes (0 for a few tokens of a narrow layer).  With Dyad-OT / -DT, n_dyad above 32 returns
  * DYAD_ERR_SHAPE.
  */
 size_t dyad_mx4_workspace_bytes(dyad_variant variant, int64_t n_in, int64_t n_out, int64_t n_dyad, int64_t M);

@@ -10,12 +10,14 @@ typedef __attribute__((ext_vector_type(8))) int i32x8_t;
 struct Mx4Args {
     int64_t M, n_in, n_out;
     int D, bi, bo;
+    const void *X;
     const uint8_t *wc, *ws, *xc, *xs;    // codes and scales of weights and input
     int w_frags, w_groups, x_frags, x_groups, steps;
     const void *bias;
     void *Y;
     int gelu, in_t;
     int tiles_n, tiles;
+    int tiles_m, m_fast; // token panels; whether they are the fastest (small tiles)
     int wave_n;          // waves side by side along the columns
     int group_m;         // large tiles: token panels per run of tiles
 };

@@ -12,8 +12,6 @@ namespace dyad {
 
 namespace {
 
-typedef __attribute__((ext_vector_type(2))) unsigned short u16x2_t;
-
 struct Mx4PackArgs {
     int64_t M, n_in, n_out;
     int D, bi, bo, in_t, out_t, by_residue;
@@ -29,45 +27,6 @@ __device__ __forceinline__ void mx4_put(const Mx4PackArgs &a, int part, int64_t 
     const int s = kb >> 2, lane = (kb & 3) * 16 + row;
     reinterpret_cast<uint4 *>(a.codes + ((part * (int64_t)a.frags + frag) * a.steps + s) * 1024)[lane] = c;
     a.scales[((part * (int64_t)a.groups + (frag >> 2)) * a.steps + s) * 256 + lane * 4 + (frag & 3)] = (uint8_t)sb;
-}
-
-__device__ __forceinline__ uint4 mx4_encode(const float (&x)[32], uint32_t &sb) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int e = 0; e < 32; ++e) top = max(top, mag_bits(x[e]));
-    sb = mx_scale<kMxFp4>(top);
-    if (sb == 255u) return make_uint4(0u, 0u, 0u, 0u);
-    const float pow = mx_pow(sb);
-    uint32_t w[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        w[q] = mx_fp4x2<0>(0u, x[8 * q], x[8 * q + 1], pow);
-        w[q] = mx_fp4x2<1>(w[q], x[8 * q + 2], x[8 * q + 3], pow);
-        w[q] = mx_fp4x2<2>(w[q], x[8 * q + 4], x[8 * q + 5], pow);
-        w[q] = mx_fp4x2<3>(w[q], x[8 * q + 6], x[8 * q + 7], pow);
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
-// 32 bf16 values as 16 words: magnitudes compared in pairs as whole numbers,
-// codes from pairs.
-__device__ __forceinline__ uint4 mx4_encode(const uint32_t (&x)[16], uint32_t &sb) {
-    u16x2_t top = {0, 0};
-#pragma unroll
-    for (int e = 0; e < 16; ++e) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2_t, x[e] & 0x7fff7fffu));
-    sb = mx_scale<kMxFp4>((uint32_t)max(top.x, top.y) << 16);
-    if (sb == 255u) return make_uint4(0u, 0u, 0u, 0u);
-    const float pow = mx_pow(sb);
-    uint32_t w[4];
-    auto pair = [&](int e) { return __builtin_bit_cast(bf16x2_t, x[e]); };
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        w[q] = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(0u, pair(4 * q), pow, 0);
-        w[q] = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w[q], pair(4 * q + 1), pow, 1);
-        w[q] = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w[q], pair(4 * q + 2), pow, 2);
-        w[q] = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w[q], pair(4 * q + 3), pow, 3);
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // Any shape, and the weights: a wave a fragment and step, values loaded one by
@@ -232,13 +191,17 @@ template <typename T>
 hipError_t run_input(Mx4PackArgs &a, hipStream_t s) {
     constexpr int E = sizeof(T);
     const int D = a.D;
-    const int rw = !a.in_t ? 0 : E == 2 && D % 4 == 0 ? 4 : D % 2 == 0 ? 2 : 1;
-    // whole steps of every residue where 64 KB hold them, else fewer blocks; without
-    // residues any columns do, fewer where that leaves CUs idle
+    // whole steps of every residue where 64 KB hold them and the GPU has enough
+    // workgroups, else fewer blocks; without residues any columns do
     int span = a.in_t ? 0 : (int64_t)a.frags * ((a.n_in + 511) / 512) >= 512 ? 512 : 128;
     if (a.in_t)
         for (int kb = 4; kb >= 1 && !span; kb /= 2)
-            if ((int64_t)16 * 32 * kb * D * E <= 65536) span = 32 * kb * D;
+            if ((int64_t)16 * 32 * kb * D * E <= 65536 &&
+                (kb == 1 || a.frags * ((a.n_in + 32 * kb * D - 1) / (32 * kb * D)) >= 256))
+                span = 32 * kb * D;
+    // residues a lane takes: one where there are fewer than lanes otherwise
+    const int64_t lanes = span / 32 * 16;
+    const int rw = !a.in_t ? 0 : E == 2 && D % 4 == 0 && lanes >= 1024 ? 4 : D % 2 == 0 && lanes >= 512 ? 2 : 1;
     const int64_t tiles = span ? (a.n_in + span - 1) / span : 0;
     if (a.bi % 32 != 0 || a.n_in != (int64_t)D * a.bi || !span || tiles * a.frags >= ((int64_t)1 << 31)) {
         mx4_pack_kernel<false, T><<<(unsigned)((a.items + 3) / 4), 256, 0, s>>>(a);

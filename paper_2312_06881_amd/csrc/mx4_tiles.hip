@@ -213,6 +213,8 @@ hipError_t launch_mx4_tiles(const Mx4Args &a, bool bf16, hipStream_t s) {
     auto tiles = [&](int sm, int sn) {
         return (int64_t)a.D * ((a.w_frags + 4 * sn - 1) / (4 * sn)) * ((a.x_frags + sm - 1) / sm);
     };
+    // tiles of 128 tokens, not for a few of them
+    if (a.x_frags < 8) return hipErrorNotSupported;
     if (tiles(8, 4) >= 512) return launch<8, 4>(a, bf16, s);
     if (tiles(8, 2) >= 256) return launch<8, 2>(a, bf16, s);
     return hipErrorNotSupported;

@@ -98,6 +98,7 @@ int dyad_mx4_quantize_weights(dyad_variant variant_arg, int64_t n_in, int64_t n_
 size_t dyad_mx4_workspace_bytes(dyad_variant variant_arg, int64_t n_in, int64_t n_out, int64_t n_dyad, int64_t M) {
     const int variant = enum_value(variant_arg);
     if (check_sizes(variant, n_in, n_out, n_dyad, M, DYAD_BF16)) return 0;
+    if (dyad::mx4_in_place(n_in, n_dyad, block(n_in, n_dyad), block(n_out, n_dyad), M, out_transposed(variant))) return 0;
     return (size_t)dyad::mx4_input_layout(n_dyad, block(n_in, n_dyad), M, in_transposed(variant)).bytes();
 }
 
@@ -114,8 +115,8 @@ int dyad_mx4_forward(dyad_variant variant_arg, int64_t n_in, int64_t n_out, int6
     if (!packed || packed_bytes < dyad_mx4_weight_bytes(variant_arg, n_in, n_out, n_dyad)) return DYAD_ERR_WORKSPACE;
     if (out_transposed(variant) && n_dyad > dyad::kMx4MaxOutResidues) return DYAD_ERR_SHAPE;
     if (M == 0) return DYAD_OK;
-    if (!workspace || workspace_bytes < dyad_mx4_workspace_bytes(variant_arg, n_in, n_out, n_dyad, M))
-        return DYAD_ERR_WORKSPACE;
+    const size_t need = dyad_mx4_workspace_bytes(variant_arg, n_in, n_out, n_dyad, M);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return DYAD_ERR_WORKSPACE;
     dyad::Mx4Pass p{};
     p.M = M; p.n_in = n_in; p.n_out = n_out; p.D = n_dyad; p.bi = block(n_in, n_dyad); p.bo = block(n_out, n_dyad);
     p.in_t = in_transposed(variant); p.out_t = out_transposed(variant); p.gelu = act == DYAD_ACT_GELU;

@@ -10,6 +10,8 @@
 
 namespace dyad {
 
+typedef __attribute__((ext_vector_type(2))) unsigned short u16x2_t;
+
 // Magnitude bits of a float: they order like the magnitudes, NaN above all.
 __device__ __forceinline__ uint32_t mag_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
@@ -92,6 +94,45 @@ __device__ __forceinline__ uint32_t mx_fp4x8(const float (&x)[8], float pow) {
     w = mx_fp4x2<1>(w, x[2], x[3], pow);
     w = mx_fp4x2<2>(w, x[4], x[5], pow);
     return mx_fp4x2<3>(w, x[6], x[7], pow);
+}
+// 32 values into 32 codes, and their scale byte.
+__device__ __forceinline__ uint4 mx4_encode(const float (&x)[32], uint32_t &sb) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 32; ++e) top = max(top, mag_bits(x[e]));
+    sb = mx_scale<kMxFp4>(top);
+    if (sb == 255u) return make_uint4(0u, 0u, 0u, 0u);
+    const float pow = mx_pow(sb);
+    uint32_t w[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        w[q] = mx_fp4x2<0>(0u, x[8 * q], x[8 * q + 1], pow);
+        w[q] = mx_fp4x2<1>(w[q], x[8 * q + 2], x[8 * q + 3], pow);
+        w[q] = mx_fp4x2<2>(w[q], x[8 * q + 4], x[8 * q + 5], pow);
+        w[q] = mx_fp4x2<3>(w[q], x[8 * q + 6], x[8 * q + 7], pow);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// 32 bf16 values as 16 words: magnitudes compared in pairs as whole numbers,
+// codes from pairs.
+__device__ __forceinline__ uint4 mx4_encode(const uint32_t (&x)[16], uint32_t &sb) {
+    u16x2_t top = {0, 0};
+#pragma unroll
+    for (int e = 0; e < 16; ++e) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2_t, x[e] & 0x7fff7fffu));
+    sb = mx_scale<kMxFp4>((uint32_t)max(top.x, top.y) << 16);
+    if (sb == 255u) return make_uint4(0u, 0u, 0u, 0u);
+    const float pow = mx_pow(sb);
+    uint32_t w[4];
+    auto pair = [&](int e) { return __builtin_bit_cast(bf16x2_t, x[e]); };
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        w[q] = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(0u, pair(4 * q), pow, 0);
+        w[q] = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w[q], pair(4 * q + 1), pow, 1);
+        w[q] = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w[q], pair(4 * q + 2), pow, 2);
+        w[q] = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w[q], pair(4 * q + 3), pow, 3);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 // Value of a code times two (a whole number): 0, 1, 2, 3, 4, 6, 8, 12.
 __device__ __forceinline__ float mx_fp4_twice(uint32_t c) {

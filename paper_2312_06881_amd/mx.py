@@ -120,9 +120,10 @@ def forward(x, weights, bias=None, act="none", workspace=None):
     v, dt, xp = _variant(w.variant), _dtype(x, bias), _ptr(x)
     y = torch.empty((M, w.n_out), dtype=x.dtype, device=x.device)
     if workspace is None:
-        workspace = _bytes(_dy.dyad_mx4_workspace_bytes(v, n_in, w.n_out, w.n_dyad, M), x.device)
+        need = _dy.dyad_mx4_workspace_bytes(v, n_in, w.n_out, w.n_dyad, M)
+        workspace = _bytes(need, x.device) if need else None
     _check(_dy.dyad_mx4_forward(v, n_in, w.n_out, w.n_dyad, M, dt, xp, _ptr(w.packed), w.packed.numel(), _ptr(bias),
-                                _act(act), _ptr(y), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                _act(act), _ptr(y), _ptr(workspace), 0 if workspace is None else workspace.nbytes,
                                 _stream(x)))
     return y
 

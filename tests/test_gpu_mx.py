@@ -114,7 +114,10 @@ def test_offsets_past_32_bits():
 
 PRODUCT = [  # (n_in, n_out, n_dyad, tokens)
     (768, 768, 4, 1),
+    (1024, 192, 4, 7),        # few tokens: a block that ends inside a step
+    (160, 64, 4, 3),          # and inside a block of 32
     (256, 512, 4, 16),
+    (1024, 512, 2, 16),
     (512, 256, 2, 17),
     (64, 64, 1, 33),          # blocks shorter than one matrix step
     (250, 154, 4, 65),        # widths n_dyad does not divide
@@ -160,12 +163,12 @@ def test_mx4_forward_many_tokens(variant):
 
 
 def test_mx4_no_bias_no_tokens_and_own_workspace():
-    L = layer_inputs(256, 512, 4, 9, "bf16")
+    L = layer_inputs(256, 512, 4, 39, "bf16")
     w = mx.quantize_weights(L.W1.to(DEV), L.W2.to(DEV), "DT")
     x = L.X.to(DEV)
     assert mx.forward(x[:0], w).shape == (0, 512)
     y = mx.forward(x, w)
-    ws = torch.full((dy.dyad_mx4_workspace_bytes(dy.DT, 256, 512, 4, 9),), 255, dtype=torch.uint8, device=DEV)
+    ws = torch.full((dy.dyad_mx4_workspace_bytes(dy.DT, 256, 512, 4, 39),), 255, dtype=torch.uint8, device=DEV)
     assert torch.equal(mx.forward(x, w, workspace=ws), y)
     with pytest.raises(dy.DyadError) as e:
         mx.forward(x, w, workspace=ws[:-1])

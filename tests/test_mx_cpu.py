@@ -52,6 +52,9 @@ def test_mx4_sizes():
     assert dy.dyad_mx4_workspace_bytes(dy.OT, 768, 768, 4, 17) == 4 * 2 * (2 * 1024 + 256)
     assert dy.dyad_mx4_workspace_bytes(dy.DT, 768, 768, 4, 17) == 2 * 4 * 2 * (2 * 1024 + 256)
     assert dy.dyad_mx4_workspace_bytes(dy.DT, 768, 768, 4, 0) == 0
+    # a few tokens of a narrow layer are quantised where they are multiplied
+    assert dy.dyad_mx4_workspace_bytes(dy.DT, 768, 768, 4, 1) == 0
+    assert dy.dyad_mx4_workspace_bytes(dy.DT, 770, 768, 4, 1) > 0
     for bad in ((3, 768, 768, 4), (0, 0, 768, 4), (0, 768, 768, 0)):
         assert dy.dyad_mx4_weight_bytes(*bad) == 0 and dy.dyad_mx4_workspace_bytes(*bad, 5) == 0
 
@@ -75,7 +78,7 @@ def test_mx4_sizes():
     (dict(M=0, X=None, Y=None, workspace=None, workspace_bytes=0), 0),
 ])
 def test_mx4_forward_rejects(args, code):
-    a = dict(variant=0, n_in=64, n_out=256, n_dyad=4, M=8, dtype=1, X=FAKE, packed=FAKE, packed_bytes=1 << 30, bias=None,
+    a = dict(variant=0, n_in=64, n_out=256, n_dyad=4, M=40, dtype=1, X=FAKE, packed=FAKE, packed_bytes=1 << 30, bias=None,
              act=0, Y=FAKE, workspace=FAKE, workspace_bytes=1 << 30, stream=None)
     a.update(args)
     assert dy.dyad_mx4_forward(**a) == code
