@@ -559,9 +559,11 @@ hipError_t launch_mx4_forward(const Mx4Pass &p, hipStream_t s) {
         by_type([&](auto t) { mx4_gemm_ot_kernel<CF, TM, decltype(t)><<<(unsigned)a.tiles, (unsigned)(64 * waves), lds, s>>>(a); });
         return hipGetLastError();
     };
-    if (xf <= 1) return ot(Int<1>{}, Int<1>{});
-    if (D <= 8) return ot(Int<4>{}, Int<4>{});
-    if (D <= 16) return ot(Int<4>{}, Int<2>{});
+    // as many tokens to a workgroup as LDS holds sums of and still fill the GPU
+    const int64_t cols = (p.n_out + 64 * D - 1) / (64 * D);
+    if (xf <= 1 || cols * xf < 256) return ot(Int<1>{}, Int<1>{});
+    if (D <= 8 && cols * ((xf + 3) / 4) >= 512) return ot(Int<4>{}, Int<4>{});
+    if (D <= 16 && cols * ((xf + 1) / 2) >= 512) return ot(Int<4>{}, Int<2>{});
     return ot(Int<4>{}, Int<1>{});
 }
 

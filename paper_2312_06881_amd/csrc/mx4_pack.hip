@@ -29,7 +29,7 @@ __device__ __forceinline__ void mx4_put(const Mx4PackArgs &a, int part, int64_t 
     a.scales[((part * (int64_t)a.groups + (frag >> 2)) * a.steps + s) * 256 + lane * 4 + (frag & 3)] = (uint8_t)sb;
 }
 
-// Any shape, and the weights: a wave a fragment and step, values loaded one by
+// Wide rows of any blocks, and the weights: a wave a fragment and step, values loaded one by
 // one.  WEIGHTS: part = component * D + block of W1 / W2, else block (or, from D
 // on, residue) of the input.
 template <bool WEIGHTS, typename T>
@@ -179,6 +179,47 @@ __global__ void __launch_bounds__(256) mx4_input_kernel(Mx4PackArgs a) {
     }
 }
 
+// Input of any blocks whose rows fit LDS sixteen at a time: a workgroup stages
+// 16 tokens whole and takes `per` of the parts from them.
+template <typename T>
+__global__ void __launch_bounds__(256) mx4_rows_kernel(Mx4PackArgs a, int per) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    constexpr int E = sizeof(T);
+    const int tid = threadIdx.x, n = (int)a.n_in, pieces = n * E / 16, pitch = (n * E + 15) / 16 * 16 + 16;
+    const int64_t frag = blockIdx.x / a.tiles, m0 = frag * 16;
+    const int p0 = blockIdx.x % a.tiles * per, p1 = p0 + per < a.parts ? p0 + per : a.parts;
+    const int real = (int)(a.M - m0 < 16 ? a.M - m0 : 16);
+    const T *src = static_cast<const T *>(a.X) + m0 * n;
+    for (int i = tid; i < real * pieces; i += 256) {
+        const int row = i / pieces, q = i - row * pieces;
+        *reinterpret_cast<uint4 *>(smem + row * pitch + 16 * q) = load_any<uint4>(src + (int64_t)row * n + q * (16 / E));
+    }
+    const int first = pieces * (16 / E), rest = n - first;
+    for (int i = tid; i < real * rest; i += 256) {
+        const int row = i / rest, c = first + i - row * rest;
+        *reinterpret_cast<T *>(smem + row * pitch + c * E) = src[(int64_t)row * n + c];
+    }
+    __syncthreads();
+    const int row = tid & 15, kbs = 4 * a.steps;
+    for (int i = tid >> 4; i < (p1 - p0) * kbs; i += 16) {
+        const int part = p0 + i / kbs, kb = i % kbs;
+        const bool second = part >= a.D;
+        const int g = second ? part - a.D : part;
+        const bool strided = second && a.in_t;
+        const int col0 = strided ? kb * 32 * a.D + g : g * a.bi + kb * 32, step = strided ? a.D : 1;
+        float x[32];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+            const int col = col0 + e * step;
+            x[e] = row < real && kb * 32 + e < a.bi && col < n
+                       ? load_f32<T>(reinterpret_cast<const T *>(smem + row * pitch), col) : 0.f;
+        }
+        uint32_t sb;
+        const uint4 c = mx4_encode(x, sb);
+        mx4_put(a, part, frag, row, kb, sb, c);
+    }
+}
+
 hipError_t layout_args(Mx4PackArgs &a, const Mx4Layout &l) {
     if (l.frags >= ((int64_t)1 << 31) || l.parts >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
     a.parts = (int)l.parts; a.frags = (int)l.frags; a.steps = (int)l.steps; a.groups = (int)l.groups();
@@ -204,6 +245,17 @@ hipError_t run_input(Mx4PackArgs &a, hipStream_t s) {
     const int rw = !a.in_t ? 0 : E == 2 && D % 4 == 0 && lanes >= 1024 ? 4 : D % 2 == 0 && lanes >= 512 ? 2 : 1;
     const int64_t tiles = span ? (a.n_in + span - 1) / span : 0;
     if (a.bi % 32 != 0 || a.n_in != (int64_t)D * a.bi || !span || tiles * a.frags >= ((int64_t)1 << 31)) {
+        const size_t rows = 16 * ((size_t)(a.n_in * E + 15) / 16 * 16 + 16);
+        if (rows <= 65536 + 256) {
+            // as many workgroups to 16 tokens as fill the GPU
+            const int64_t want = (512 + a.frags - 1) / a.frags, most = want < a.parts ? want : a.parts;
+            const int per = (int)((a.parts + most - 1) / most);
+            a.tiles = (a.parts + per - 1) / per;
+            if ((int64_t)a.tiles * a.frags < ((int64_t)1 << 31)) {
+                mx4_rows_kernel<T><<<(unsigned)(a.tiles * a.frags), 256, rows, s>>>(a, per);
+                return hipGetLastError();
+            }
+        }
         mx4_pack_kernel<false, T><<<(unsigned)((a.items + 3) / 4), 256, 0, s>>>(a);
         return hipGetLastError();
     }

@@ -12,6 +12,19 @@ namespace dyad {
 
 typedef __attribute__((ext_vector_type(2))) unsigned short u16x2_t;
 
+// Bytes at any address: rows of an odd width start anywhere (the hardware takes
+// vector accesses at every alignment).
+template <typename V>
+__device__ __forceinline__ V load_any(const void *p) {
+    V v;
+    __builtin_memcpy(&v, p, sizeof v);
+    return v;
+}
+template <typename V>
+__device__ __forceinline__ void store_any(void *p, const V &v) {
+    __builtin_memcpy(p, &v, sizeof v);
+}
+
 // Magnitude bits of a float: they order like the magnitudes, NaN above all.
 __device__ __forceinline__ uint32_t mag_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 

@@ -12,21 +12,19 @@ namespace {
 
 constexpr int kThreads = 256, kUnits = 4;     // units of 8 values a thread
 
-// Eight values of a row from `col`: whole and aligned with VEC, else the `n` that exist.
-template <typename T, bool VEC>
+// Eight values of a row, of which `n` exist.
+template <typename T>
 __device__ __forceinline__ void load8(const T *p, int n, float (&x)[8]) {
-    if constexpr (VEC && sizeof(T) == 2) {
-        const uint4 v = n > 0 ? *reinterpret_cast<const uint4 *>(p) : make_uint4(0u, 0u, 0u, 0u);
+    if (n == 8) {
+        if constexpr (sizeof(T) == 2) {
+            const uint4 v = load_any<uint4>(p);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = unpack_bf16(word_of(v, e >> 1), e & 1);
-    } else if constexpr (VEC) {
-        float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
-        if (n > 0) {
-            a = *reinterpret_cast<const float4 *>(p);
-            b = *reinterpret_cast<const float4 *>(p + 4);
+            for (int e = 0; e < 8; ++e) x[e] = unpack_bf16(word_of(v, e >> 1), e & 1);
+        } else {
+            const float4 a = load_any<float4>(p), b = load_any<float4>(p + 4);
+            x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+            x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
         }
-        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-        x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = e < n ? load_f32<T>(p, e) : 0.f;
@@ -54,7 +52,7 @@ struct Units {
     }
 };
 
-template <int FMT, typename T, bool VEC>
+template <int FMT, typename T>
 __global__ void __launch_bounds__(kThreads) mx_quantize_kernel(int64_t rows, int64_t cols, const T *__restrict__ X,
                                                                uint8_t *__restrict__ codes,
                                                                uint8_t *__restrict__ scales) {
@@ -69,7 +67,7 @@ __global__ void __launch_bounds__(kThreads) mx_quantize_kernel(int64_t rows, int
         const bool in = units.at(q, row[q], u[q]);
         const int64_t left = cols - (int64_t)u[q] * 8;
         n[q] = !in || left < 0 ? 0 : left < 8 ? (int)left : 8;
-        load8<T, VEC>(X + row[q] * cols + (int64_t)u[q] * 8, n[q], x[q]);
+        load8<T>(X + row[q] * cols + (int64_t)u[q] * 8, n[q], x[q]);
     }
 #pragma unroll
     for (int q = 0; q < kUnits; ++q) {
@@ -79,8 +77,8 @@ __global__ void __launch_bounds__(kThreads) mx_quantize_kernel(int64_t rows, int
             uint8_t *dst = codes + row[q] * code_row + (int64_t)u[q] * 8;
             const uint32_t w[2] = {mx_int8x4(x[q][0], x[q][1], x[q][2], x[q][3], s),
                                    mx_int8x4(x[q][4], x[q][5], x[q][6], x[q][7], s)};
-            if constexpr (VEC) {
-                if (n[q] > 0) *reinterpret_cast<uint2 *>(dst) = make_uint2(w[0], w[1]);
+            if (n[q] == 8) {
+                store_any(dst, make_uint2(w[0], w[1]));
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
@@ -89,8 +87,8 @@ __global__ void __launch_bounds__(kThreads) mx_quantize_kernel(int64_t rows, int
         } else {
             uint8_t *dst = codes + row[q] * code_row + (int64_t)u[q] * 4;
             const uint32_t w = s == 255u ? 0u : mx_fp4x8(x[q], mx_pow(s));
-            if constexpr (VEC) {
-                if (n[q] > 0) *reinterpret_cast<uint32_t *>(dst) = w;
+            if (n[q] == 8) {
+                store_any(dst, w);
             } else {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
@@ -100,7 +98,7 @@ __global__ void __launch_bounds__(kThreads) mx_quantize_kernel(int64_t rows, int
     }
 }
 
-template <int FMT, typename T, bool VEC, bool GELU>
+template <int FMT, typename T, bool GELU>
 __global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(int64_t rows, int64_t cols,
                                                                  const uint8_t *__restrict__ codes,
                                                                  const uint8_t *__restrict__ scales,
@@ -119,15 +117,13 @@ __global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(int64_t rows, i
         w[q][0] = w[q][1] = 0u;
         s[q] = n[q] > 0 ? scales[row[q] * nb + u[q] / 4u] : 0u;
         const uint8_t *src = codes + row[q] * code_row + (int64_t)u[q] * (FMT == kMxInt8 ? 8 : 4);
-        if constexpr (VEC) {
-            if (n[q] > 0) {
-                if constexpr (FMT == kMxInt8) {
-                    const uint2 v = *reinterpret_cast<const uint2 *>(src);
-                    w[q][0] = v.x;
-                    w[q][1] = v.y;
-                } else {
-                    w[q][0] = *reinterpret_cast<const uint32_t *>(src);
-                }
+        if (n[q] == 8) {
+            if constexpr (FMT == kMxInt8) {
+                const uint2 v = load_any<uint2>(src);
+                w[q][0] = v.x;
+                w[q][1] = v.y;
+            } else {
+                w[q][0] = load_any<uint32_t>(src);
             }
         } else if constexpr (FMT == kMxInt8) {
 #pragma unroll
@@ -159,18 +155,15 @@ __global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(int64_t rows, i
             if constexpr (GELU) x[e] = sizeof(T) == 2 ? gelu(x[e]) : gelu_f32(x[e]);
         }
         T *dst = Y + row[q] * cols + (int64_t)u[q] * 8;
-        if constexpr (!VEC) {
+        if (n[q] < 8) {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 if (e < n[q]) store_f32<T>(dst, e, x[e]);
-        } else if (n[q] > 0) {
-            if constexpr (sizeof(T) == 2) {
-                *reinterpret_cast<uint4 *>(dst) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]),
-                                                             pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
-            } else {
-                *reinterpret_cast<float4 *>(dst) = make_float4(x[0], x[1], x[2], x[3]);
-                *reinterpret_cast<float4 *>(dst + 4) = make_float4(x[4], x[5], x[6], x[7]);
-            }
+        } else if constexpr (sizeof(T) == 2) {
+            store_any(dst, make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])));
+        } else {
+            store_any(dst, make_float4(x[0], x[1], x[2], x[3]));
+            store_any(dst + 4, make_float4(x[4], x[5], x[6], x[7]));
         }
     }
 }
@@ -188,18 +181,14 @@ hipError_t launch_mx_quantize(int fmt, int64_t rows, int64_t cols, int dtype, co
                               hipStream_t s) {
     const unsigned grid = grid_for(rows, cols);
     if (!grid) return hipErrorInvalidValue;
-    auto go = [&](auto f, auto t, auto vec) {
+    auto go = [&](auto f, auto t) {
         using T = decltype(t);
-        mx_quantize_kernel<decltype(f)::value, T, decltype(vec)::value><<<grid, kThreads, 0, s>>>(
+        mx_quantize_kernel<decltype(f)::value, T><<<grid, kThreads, 0, s>>>(
             rows, cols, static_cast<const T *>(X), static_cast<uint8_t *>(codes), static_cast<uint8_t *>(scales));
     };
-    auto by_vec = [&](auto f, auto t) {
-        if (cols % 8 == 0) go(f, t, std::true_type{});
-        else go(f, t, std::false_type{});
-    };
     auto by_type = [&](auto f) {
-        if (dtype == kBF16) by_vec(f, uint16_t{});
-        else by_vec(f, float{});
+        if (dtype == kBF16) go(f, uint16_t{});
+        else go(f, float{});
     };
     if (fmt == kMxInt8) by_type(std::integral_constant<int, kMxInt8>{});
     else by_type(std::integral_constant<int, kMxFp4>{});
@@ -210,18 +199,14 @@ hipError_t launch_mx_dequantize(int fmt, int64_t rows, int64_t cols, int dtype, 
                                 bool gelu, void *Y, hipStream_t s) {
     const unsigned grid = grid_for(rows, cols);
     if (!grid) return hipErrorInvalidValue;
-    auto go = [&](auto f, auto t, auto vec, auto act) {
+    auto go = [&](auto f, auto t, auto act) {
         using T = decltype(t);
-        mx_dequantize_kernel<decltype(f)::value, T, decltype(vec)::value, decltype(act)::value><<<grid, kThreads, 0, s>>>(
+        mx_dequantize_kernel<decltype(f)::value, T, decltype(act)::value><<<grid, kThreads, 0, s>>>(
             rows, cols, static_cast<const uint8_t *>(codes), static_cast<const uint8_t *>(scales), static_cast<T *>(Y));
     };
-    auto by_vec = [&](auto f, auto t, auto act) {
-        if (cols % 8 == 0) go(f, t, std::true_type{}, act);
-        else go(f, t, std::false_type{}, act);
-    };
     auto by_type = [&](auto f, auto act) {
-        if (dtype == kBF16) by_vec(f, uint16_t{}, act);
-        else by_vec(f, float{}, act);
+        if (dtype == kBF16) go(f, uint16_t{}, act);
+        else go(f, float{}, act);
     };
     if (fmt == kMxFp4) by_type(std::integral_constant<int, kMxFp4>{}, std::false_type{});
     else if (gelu) by_type(std::integral_constant<int, kMxInt8>{}, std::true_type{});
