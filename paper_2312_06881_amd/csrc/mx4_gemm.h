@@ -26,6 +26,10 @@ struct Mx4Args {
 // nothing, where they would leave CUs idle.
 hipError_t launch_mx4_tiles(const Mx4Args &a, bool bf16, hipStream_t s);
 
+// Large tiles under an output transpose (mx4_res_tiles.hip), bf16 and weights by
+// residue; hipErrorNotSupported, launching nothing, for the others.
+hipError_t launch_mx4_res_tiles(const Mx4Args &a, hipStream_t s);
+
 // acc += W fragment (16 outputs) times X fragment (16 tokens) over 128 indices.
 // The weights are the first operand: a lane's four sums are outputs
 // 4 * (lane / 16) + v of token lane % 16.  BW, BX: bytes of the scale words.

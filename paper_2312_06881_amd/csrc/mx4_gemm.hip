@@ -512,6 +512,8 @@ hipError_t launch_mx4_forward(const Mx4Pass &p, hipStream_t s) {
         return plain(Int<1>{}, Int<1>{}, wide);
     }
     if (mx4_by_residue(D, p.bo, out_t)) {
+        if (p.dtype == kBF16)
+            if (const hipError_t t = launch_mx4_res_tiles(a, s); t != hipErrorNotSupported) return t;
         const int64_t per = p.bo / (16 * D), all = (p.n_out + 16 * D - 1) / (16 * D);
         auto res = [&](auto sn, auto sm) -> hipError_t {
             constexpr int SN = decltype(sn)::value, SM = decltype(sm)::value;

@@ -149,15 +149,30 @@ def test_mx4_forward(shape, variant, dtype):
     assert_close(y, want, dtype, "Y")
 
 
+MANY = [  # (n_in, n_out, n_dyad, tokens): every form of the large tiles, last panels of a few tokens
+    (768, 1536, 4, 5000),
+    (1024, 2048, 4, 4103),    # blocks of two steps
+    (4096, 4096, 4, 6000),
+    (512, 4096, 8, 8200),     # one step: an odd number in each component
+    (3072, 2048, 8, 1025),    # three
+    (2048, 4096, 16, 3333),
+    (2048, 8192, 16, 2049),
+    (1152, 768, 4, 9001),
+    (1536, 1536, 3, 4097),
+]
+
+
 @pytest.mark.parametrize("variant", VARIANTS)
-def test_mx4_forward_many_tokens(variant):
+@pytest.mark.parametrize("shape", MANY, ids=lambda s: "x".join(map(str, s)))
+def test_mx4_forward_many_tokens(shape, variant):
     """Rows that repeat 37 tokens: every place in the large tiles gives the oracle's rows."""
-    n_in, n_out, D, M = 768, 1536, 4, 5000
+    n_in, n_out, D, M = shape
+    banner("product, many tokens", shape, variant)
     L = layer_inputs(n_in, n_out, D, 37, "bf16", seed_offset=12)
     w = mx.quantize_weights(L.W1.to(DEV), L.W2.to(DEV), variant)
     x = L.X.to(DEV).repeat(M // 37 + 1, 1)[:M].contiguous()
-    y = mx.forward(x, w)
-    want = ref.mx4_forward(variant, n_in, n_out, D, L.f64("X"), L.f64("W1"), L.f64("W2"), None, "none")
+    y = mx.forward(x, w, L.bias.to(DEV))
+    want = ref.mx4_forward(variant, n_in, n_out, D, L.f64("X"), L.f64("W1"), L.f64("W2"), L.f64("bias"), "none")
     assert_close(y[:37], want, "bf16", "Y")
     assert torch.equal(y, y[:37].repeat(M // 37 + 1, 1)[:M])
 
