@@ -90,7 +90,8 @@ __device__ __forceinline__ void mx4_loop(const Mx4Args &a, const Mx4Wave &v, int
 
 // Small tiles: the tile of a workgroup.  Consecutive tiles share an XCD, whose L2
 // then reads either the input or the weights once: the larger of the two (256
-// tokens of 32768 -> 8192, n_dyad 16, 18 MB of weights over 4 MB of input: %M%).
+// tokens of 32768 -> 8192, n_dyad 16, Dyad-OT, 18 MB of weights over 4 of input:
+// 33 -> 31 us).
 __device__ __forceinline__ void mx4_tile(const Mx4Args &a, int &tn, int &tm) {
     const int tile = xcd_tile(blockIdx.x, a.tiles);
     tn = a.m_fast ? tile / a.tiles_m : tile % a.tiles_n;
@@ -424,12 +425,16 @@ using Int = std::integral_constant<int, N>;
 
 }  // namespace
 
-// Up to 16 tokens: each wave quantises what it multiplies, in place of a pass of
-// its own in front (a launch, and 3 us at one token of 768), while the input is
-// narrow: all fragments of a block's outputs repeat it, and residues are gathered
-// value by value.
-bool mx4_in_place(int64_t n_in, int64_t D, int64_t bi, int64_t bo, int64_t M, bool out_t) {
-    return M <= 16 && M * n_in <= kMx4InPlace && bi % 8 == 0 && n_in == D * bi &&
+// Up to 16 tokens over blocks of at most two steps: each wave quantises what it
+// multiplies, in place of a pass in front (a launch, 3 us at one token of 768).
+// All fragments of a block's outputs repeat it, and residues are gathered value
+// by value.  A call of 1 / 4 / 16 tokens, against the two launches: 768 -> 3072,
+// n_dyad 4, Dyad-IT 10.6 / 10.2 / 10.9 us (11.8 / 11.7 / 11.2), -OT 10.9 / 10.0 / 9.8
+// (11.8 / 11.4 / 11.1); 2048 -> 8192, n_dyad 8, -IT 10.1 / 11.2 / 12.7 (11.6 / 11.7 /
+// 11.0), -OT 10.2 / 9.7 / 10.3 (11.6 / 11.4 / 10.9); blocks of 768 (3072 -> 768), -IT
+// 20 / 21 / 29 (11.8 / 11.7 / 11.7), -OT 11.5 / 10.9 / 10.8 (11.4 / 11.5 / 11.4).
+bool mx4_in_place(int64_t n_in, int64_t D, int64_t bi, int64_t bo, int64_t M, bool in_t, bool out_t) {
+    return M <= (in_t && D > 1 ? 4 : 16) && bi <= 256 && bi % 8 == 0 && n_in == D * bi &&
            (!out_t || D == 1 || mx4_by_residue(D, bo, out_t));
 }
 
@@ -460,7 +465,7 @@ hipError_t launch_mx4_forward(const Mx4Pass &p, hipStream_t s) {
         if (p.dtype == kBF16) go(uint16_t{});
         else go(float{});
     };
-    if (mx4_in_place(p.n_in, D, p.bi, p.bo, p.M, out_t)) {
+    if (mx4_in_place(p.n_in, D, p.bi, p.bo, p.M, in_t, out_t)) {
         if (!tiles(out_t ? (p.n_out + 16 * D - 1) / (16 * D) : D * ((wf + 3) / 4), 1)) return hipErrorInvalidValue;
         by_type([&](auto t) {
             using T = decltype(t);

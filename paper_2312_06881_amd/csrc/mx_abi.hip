@@ -98,7 +98,9 @@ int dyad_mx4_quantize_weights(dyad_variant variant_arg, int64_t n_in, int64_t n_
 size_t dyad_mx4_workspace_bytes(dyad_variant variant_arg, int64_t n_in, int64_t n_out, int64_t n_dyad, int64_t M) {
     const int variant = enum_value(variant_arg);
     if (check_sizes(variant, n_in, n_out, n_dyad, M, DYAD_BF16)) return 0;
-    if (dyad::mx4_in_place(n_in, n_dyad, block(n_in, n_dyad), block(n_out, n_dyad), M, out_transposed(variant))) return 0;
+    if (dyad::mx4_in_place(n_in, n_dyad, block(n_in, n_dyad), block(n_out, n_dyad), M, in_transposed(variant),
+                           out_transposed(variant)))
+        return 0;
     return (size_t)dyad::mx4_input_layout(n_dyad, block(n_in, n_dyad), M, in_transposed(variant)).bytes();
 }
 

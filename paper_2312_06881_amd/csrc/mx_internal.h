@@ -57,9 +57,8 @@ struct Mx4Pass {
 };
 
 // Whether a call multiplies its input without a pass that quantises it in front
-// (and needs no workspace), and the widest input of M tokens that does.
-constexpr int64_t kMx4InPlace = 8192;
-bool mx4_in_place(int64_t n_in, int64_t D, int64_t bi, int64_t bo, int64_t M, bool out_t);
+// (and needs no workspace).
+bool mx4_in_place(int64_t n_in, int64_t D, int64_t bi, int64_t bo, int64_t M, bool in_t, bool out_t);
 
 constexpr int64_t kMx4MaxOutResidues = 32;   // n_dyad under an output transpose
 

@@ -55,6 +55,9 @@ def test_mx4_sizes():
     # a few tokens of a narrow layer are quantised where they are multiplied
     assert dy.dyad_mx4_workspace_bytes(dy.DT, 768, 768, 4, 1) == 0
     assert dy.dyad_mx4_workspace_bytes(dy.DT, 770, 768, 4, 1) > 0
+    assert dy.dyad_mx4_workspace_bytes(dy.DT, 768, 768, 4, 5) > 0
+    assert dy.dyad_mx4_workspace_bytes(dy.OT, 768, 768, 4, 16) == 0
+    assert dy.dyad_mx4_workspace_bytes(dy.OT, 3072, 768, 4, 1) > 0
     for bad in ((3, 768, 768, 4), (0, 0, 768, 4), (0, 768, 768, 0)):
         assert dy.dyad_mx4_weight_bytes(*bad) == 0 and dy.dyad_mx4_workspace_bytes(*bad, 5) == 0
 
