@@ -5,7 +5,7 @@
 // rate without packed forms).  A 128 x 128 tile on four waves of 64 x 64 does
 // 64 of those instructions (32 cycles each) per 16 reduction indices against
 // 8 LDS reads, so operand traffic is small and a plain double-buffered loop
-// with two workgroups per CU suffices.  The decomposition is that of the
+// with two workgroups per CU suffices; small grids take smaller tiles.  The decomposition is that of the
 // general kernels: a tile's columns lie in one class (g1, g2) of output
 // columns, which read the same two input slabs; the weight gradient has one
 // product per (component, group), split over the tokens.
@@ -20,8 +20,8 @@
 // (16 bytes at a time, transposed on the way into LDS).
 //
 // Measured on gfx950 against the vector kernels (which keep the other shapes),
-// 768 -> 3072, n_dyad 4, 4096 tokens, Dyad-IT: forward 259 -> 128 us (75
-// TFLOP/s), input gradient 441 -> 137, weight gradient 212 -> 140.
+// 768 -> 3072, n_dyad 4, 4096 tokens, Dyad-IT: forward 259 -> 96 us (101
+// TFLOP/s), input gradient 441 -> 127, weight gradient 212 -> 120.
 #include <type_traits>
 
 #include "dyad_device.h"
@@ -347,6 +347,65 @@ __global__ void __launch_bounds__(kFThreads, 2) f32_dw_kernel(DwPass p, int jt_n
     }
 }
 
+// A tile size, and how many of it cover `each` products of m x n.
+struct FTile {
+    int index;
+    int64_t rows, cols, count;
+    template <class F> void with(F f) const {
+        switch (index) {
+        case 0: return f(std::integral_constant<int, 128>{}, std::integral_constant<int, 128>{});
+        case 1: return f(std::integral_constant<int, 128>{}, std::integral_constant<int, 64>{});
+        case 2: return f(std::integral_constant<int, 64>{}, std::integral_constant<int, 64>{});
+        case 3: return f(std::integral_constant<int, 64>{}, std::integral_constant<int, 32>{});
+        default: return f(std::integral_constant<int, 32>{}, std::integral_constant<int, 32>{});
+        }
+    }
+};
+constexpr int kTiles = 5;
+constexpr int kTileM[kTiles] = {128, 128, 64, 64, 32}, kTileN[kTiles] = {128, 64, 64, 32, 32};
+
+FTile tile_at(int index, int64_t each, int64_t m, int64_t n) {
+    const int64_t rt = (m + kTileM[index] - 1) / kTileM[index], ct = (n + kTileN[index] - 1) / kTileN[index];
+    return FTile{index, rt, ct, each * rt * ct};
+}
+
+// The product's tile by its time per stage on a CU, in us: k tiles there take k
+// times their matrix instructions, more per value the smaller the tile, and no
+// less than one tile's and the latency of a stage (load, LDS, barrier).  Every
+// tile sums in the same order.  Measured on 128 x 128, 128 x 64, 64 x 64, 64 x
+// 32 and 32 x 32 (us):
+//   2048 -> 8192, n_dyad 2, IT, 256 tokens: input gradient  694, 382, 251, 155, 163
+//                                           forward pass    168, 107, 98, 102, 103
+//   768 -> 3072, n_dyad 4, IT, 4096 tokens: forward pass    96, 102, 96, 111, 112
+FTile gemm_tile(int64_t each, int64_t m, int64_t n) {
+    constexpr double per_value[kTiles] = {1., 1., 1.05, 1.2, 1.3};
+    FTile best{};
+    double least = 0;
+    for (int i = 0; i < kTiles; ++i) {
+        const FTile t = tile_at(i, each, m, n);
+        const double one = 0.85 / 8192 * kTileM[i] * kTileN[i], k = (double)((t.count + 255) / 256);
+        const double busy = k * one * per_value[i], cost = busy > 0.45 + one ? busy : 0.45 + one;
+        if (i == 0 || cost < least) { best = t; least = cost; }
+    }
+    return best;
+}
+
+// The weight gradient's tile: a side under a transpose is loaded one value at a
+// time, so the largest, where it pads nothing more than 64 x 64 and every CU
+// gets one; else 64 x 64, or smaller ones if that leaves CUs without a tile.
+// Measured on 128 x 128, 64 x 64, 64 x 32 and 32 x 32 (us):
+//   2048 -> 8192, n_dyad 8, DT, 384 tokens (256 large tiles)   69, 93, 133, 173
+//   1024 -> 4096, n_dyad 4, DT, 640 tokens (128)               79, 47, 61, 84
+//   768 -> 3072, n_dyad 4, IT, 4096 tokens (pads 192 to 256)   164, 119, 125, 144
+//   1024 -> 1024, n_dyad 4, OT, 500 tokens (32)                54, 22, 17, 15
+FTile dw_tile(int64_t each, int64_t m, int64_t n) {
+    const FTile large = tile_at(0, each, m, n);
+    if ((m + 63) / 64 % 2 == 0 && (n + 63) / 64 % 2 == 0 && large.count >= 256) return large;
+    for (int i = 2; i < kTiles - 1; ++i)
+        if (const FTile t = tile_at(i, each, m, n); t.count >= 256) return t;
+    return tile_at(kTiles - 1, each, m, n);
+}
+
 }  // namespace
 
 // Blocks of a multiple of 4 that n_dyad divides the widths into: rows of
@@ -362,17 +421,15 @@ hipError_t launch_f32_gemm(const GemmPass &p, hipStream_t s) {
     if (128 * p.Kin * 4 >= lim || 32 * p.bn * 4 >= lim || 128 * p.D * p.bk * 4 >= lim) return hipErrorNotSupported;
     const int64_t classes = p.out_t ? p.D * p.D : p.D;
     const int64_t per_class = p.out_t ? (p.bn + p.D - 1) / p.D : p.bn;
-    // 64-column tiles where a class (the columns of one block and residue)
-    // pads 128-column ones by more, or where those leave CUs without a tile
-    const int64_t t128 = (per_class + 127) / 128, t64 = (per_class + 63) / 64, rt = (p.M + 127) / 128;
-    const bool wide = t64 * 64 > t128 * 128 - 64 && classes * t128 * rt >= 256;
-    const int64_t col_tiles = wide ? t128 : t64;
-    const int64_t blocks = classes * col_tiles * rt;
-    if (blocks >= ((int64_t)1 << 31)) return hipErrorNotSupported;
+    const FTile tile = gemm_tile(classes, p.M, per_class);
+    if (tile.count >= ((int64_t)1 << 31)) return hipErrorNotSupported;
     auto go = [&](auto in_t, auto out_t, auto w_t) {
         constexpr bool I = decltype(in_t)::value, O = decltype(out_t)::value, W = decltype(w_t)::value;
-        if (wide) f32_gemm_kernel<128, 128, I, O, W><<<(unsigned)blocks, kFThreads, 0, s>>>(p, (int)col_tiles);
-        else f32_gemm_kernel<128, 64, I, O, W><<<(unsigned)blocks, kFThreads, 0, s>>>(p, (int)col_tiles);
+        const unsigned n = (unsigned)tile.count;
+        const int ct = (int)tile.cols;
+        tile.with([&](auto bm, auto bn) {
+            f32_gemm_kernel<decltype(bm)::value, decltype(bn)::value, I, O, W><<<n, kFThreads, 0, s>>>(p, ct);
+        });
         return hipGetLastError();
     };
     auto with = [&](auto w) {
@@ -386,20 +443,15 @@ hipError_t launch_f32_gemm(const GemmPass &p, hipStream_t s) {
 hipError_t launch_f32_dw_tiles(const DwPass &p, int64_t splits, int64_t tps, float *part, hipStream_t s) {
     if (p.dtype != kF32 || !f32_mfma_ok(p.n_in, p.n_out, p.D, p.bi, p.bo)) return hipErrorNotSupported;
     if (32 * (p.n_in > p.n_out ? p.n_in : p.n_out) * 4 >= (int64_t)1 << 31) return hipErrorNotSupported;
-    // 128-wide tiles only where they pad nothing more than 64-wide ones
-    const int64_t jw = (p.bo + 63) / 64 % 2 == 0 ? 128 : 64;
-    const bool wide = (p.bi + 63) / 64 % 2 == 0;
-    const int64_t kw = wide ? 128 : 64;
-    const int64_t jt = (p.bo + jw - 1) / jw, kt = (p.bi + kw - 1) / kw, blocks = splits * 2 * p.D * jt * kt;
-    if (blocks >= ((int64_t)1 << 31)) return hipErrorNotSupported;
-    const unsigned n = (unsigned)blocks;
+    const FTile tile = dw_tile(splits * 2 * p.D, p.bo, p.bi);
+    if (tile.count >= ((int64_t)1 << 31)) return hipErrorNotSupported;
+    const unsigned n = (unsigned)tile.count;
     auto go = [&](auto in_t, auto out_t) {
         constexpr bool I = decltype(in_t)::value, O = decltype(out_t)::value;
-        const int j = (int)jt, k = (int)kt, sp = (int)splits;
-        if (jw == 128 && wide) f32_dw_kernel<128, 128, I, O><<<n, kFThreads, 0, s>>>(p, j, k, sp, tps, part);
-        else if (jw == 128) f32_dw_kernel<128, 64, I, O><<<n, kFThreads, 0, s>>>(p, j, k, sp, tps, part);
-        else if (wide) f32_dw_kernel<64, 128, I, O><<<n, kFThreads, 0, s>>>(p, j, k, sp, tps, part);
-        else f32_dw_kernel<64, 64, I, O><<<n, kFThreads, 0, s>>>(p, j, k, sp, tps, part);
+        tile.with([&](auto bj, auto bk) {
+            f32_dw_kernel<decltype(bj)::value, decltype(bk)::value, I, O><<<n, kFThreads, 0, s>>>(
+                p, (int)tile.rows, (int)tile.cols, (int)splits, tps, part);
+        });
     };
     constexpr std::true_type yes{};
     constexpr std::false_type no{};
