@@ -31,6 +31,8 @@
 namespace dyad {
 namespace {
 
+using f64x4_t = __attribute__((ext_vector_type(4))) double;
+
 constexpr int kFK = 32;          // reduction indices per stage
 constexpr int kFThreads = 256;
 
@@ -128,9 +130,11 @@ struct FLoader {
 // column 4 v + lg stands where 4 lg + v is meant (16-column blocks transposed
 // as 4 x 4), so that lanes lg = 0..3 hold consecutive columns.  KA, KB: the
 // sides' kinds.  DB: with do_db, dacc[i] also gets row 16 i + l % 16's sum.
-template <int BM, int BN, int SM, int SN, int KA, int KB, bool DB>
+// Acc: f32x4_t, or f64x4_t for sums in 64 bits, whose instruction leaves column
+// 4 v + l / 16 where the other leaves 4 (l / 16) + v.
+template <int BM, int BN, int SM, int SN, int KA, int KB, bool DB, class Acc>
 __device__ __forceinline__ void f32_loop(const FSide &sa, const FSide &sb, int64_t k_lo, int64_t k_hi, int rows_a,
-                                         int rows_b, bool perm, bool do_db, float *lds, f32x4_t (&acc)[SN][SM],
+                                         int rows_b, bool perm, bool do_db, float *lds, Acc (&acc)[SN][SM],
                                          f32x4_t (&dacc)[DB ? SM : 1], int wm0, int wn0) {
     const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
     constexpr int kBuf = (BM + BN) * kFK;
@@ -150,7 +154,8 @@ __device__ __forceinline__ void f32_loop(const FSide &sa, const FSide &sb, int64
         la.stash(tid, buf);
         lb.stash(tid, buf + BM * kFK);
     };
-    const int pr = perm ? (lr & 3) * 4 + (lr >> 2) : lr;
+    constexpr bool wide = std::is_same_v<Acc, f64x4_t>;
+    const int pr = perm != wide ? (lr & 3) * 4 + (lr >> 2) : lr;
     fetch(0);
     stash(0);
     __syncthreads();
@@ -172,7 +177,10 @@ __device__ __forceinline__ void f32_loop(const FSide &sa, const FSide &sb, int64
                 for (int j = 0; j < SN; ++j)
 #pragma unroll
                     for (int i = 0; i < SM; ++i)
-                        acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(b[j][s], a[i][s], acc[j][i], 0, 0, 0);
+                        if constexpr (wide)
+                            acc[j][i] = __builtin_amdgcn_mfma_f64_16x16x4f64((double)b[j][s], (double)a[i][s], acc[j][i], 0, 0, 0);
+                        else
+                            acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(b[j][s], a[i][s], acc[j][i], 0, 0, 0);
             if constexpr (DB) {
                 if (do_db) {
 #pragma unroll
@@ -188,7 +196,13 @@ __device__ __forceinline__ void f32_loop(const FSide &sa, const FSide &sb, int64
     }
 }
 
-template <int BM, int BN, bool IN_T, bool OUT_T, bool W_T>
+// WIDE: sums in 64 bits, rounded to 32 once the bias is in.  A pre-activation
+// that is kept in 8 bits takes the code next to the right one where its error
+// carries it over a boundary, and those codes, not the products, then move the
+// gradients off their exact values.  A feed-forward block of 2048 -> 8192 at
+// n_dyad 2, 256 tokens: fc2's weight gradient 1.2e-4 off with sums in 32 bits,
+// 2.9e-7 in 64; this pass 100 -> 174 us (the 64-bit rate is half) of 800.
+template <int BM, int BN, bool IN_T, bool OUT_T, bool W_T, bool WIDE>
 __global__ void __launch_bounds__(kFThreads, 2) f32_gemm_kernel(GemmPass p, int col_tiles) {
     constexpr int SM = BM / 32, SN = BN / 32;      // 2 x 2 waves
     __shared__ __attribute__((aligned(16))) float lds[2 * (BM + BN) * kFK];
@@ -212,11 +226,14 @@ __global__ void __launch_bounds__(kFThreads, 2) f32_gemm_kernel(GemmPass p, int 
     const float *in = static_cast<const float *>(p.in) + m0 * p.Kin;
     const float *W1 = static_cast<const float *>(p.W1), *W2 = static_cast<const float *>(p.W2);
     const int64_t f0 = first + t0 * step, j1 = f0 - lo, j2 = OUT_T ? f0 / D : j1;
-    f32x4_t acc[SN][SM], none[1];
+    using Acc = std::conditional_t<WIDE, f64x4_t, f32x4_t>;
+    using Sum = std::conditional_t<WIDE, double, float>;
+    Acc acc[SN][SM];
+    f32x4_t none[1];
 #pragma unroll
     for (int j = 0; j < SN; ++j)
 #pragma unroll
-        for (int i = 0; i < SM; ++i) acc[j][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < SM; ++i) acc[j][i] = Acc{0, 0, 0, 0};
     const int wm0 = (wave >> 1) * (BM / 2), wn0 = (wave & 1) * (BN / 2);
     const bool perm = step != 1;   // consecutive columns (n_dyad 1 too) leave in 16-byte pieces instead
     // kinds: weights read transposed run along the columns, D apart in
@@ -244,6 +261,7 @@ __global__ void __launch_bounds__(kFThreads, 2) f32_gemm_kernel(GemmPass p, int 
 #pragma unroll
         for (int j = 0; j < SN; ++j) {
             const int tb = wn0 + 16 * j;
+            Sum sum[4];
             float x[4];
             bool ok[4];
             int64_t e[4];
@@ -252,7 +270,8 @@ __global__ void __launch_bounds__(kFThreads, 2) f32_gemm_kernel(GemmPass p, int 
                 const int t = tb + (perm ? 4 * v + lg : 4 * lg + v);
                 ok[v] = t < rows_b;
                 e[v] = at + f0 + t * step;
-                x[v] = acc[j][i][v];
+                sum[v] = acc[j][i][v];
+                x[v] = (float)sum[v];
             }
             if (vec && ok[3]) {
                 if (grad) {
@@ -262,7 +281,8 @@ __global__ void __launch_bounds__(kFThreads, 2) f32_gemm_kernel(GemmPass p, int 
                 } else {
                     if (bias) {
                         const float4 bv = *reinterpret_cast<const float4 *>(bias + (e[0] - at));
-                        x[0] += bv.x; x[1] += bv.y; x[2] += bv.z; x[3] += bv.w;
+                        x[0] = (float)(sum[0] + bv.x); x[1] = (float)(sum[1] + bv.y);
+                        x[2] = (float)(sum[2] + bv.z); x[3] = (float)(sum[3] + bv.w);
                     }
                     if (act) {
                         if (h_out) *reinterpret_cast<float4 *>(h_out + e[0]) = make_float4(x[0], x[1], x[2], x[3]);
@@ -279,7 +299,7 @@ __global__ void __launch_bounds__(kFThreads, 2) f32_gemm_kernel(GemmPass p, int 
                 if (grad) {
                     x[v] *= gelu_grad_f32(h_in[e[v]]);
                 } else {
-                    if (bias) x[v] += bias[e[v] - at];
+                    if (bias) x[v] = (float)(sum[v] + bias[e[v] - at]);
                     if (act) {
                         if (h_out) h_out[e[v]] = x[v];
                         x[v] = gelu_f32(x[v]);
@@ -351,10 +371,13 @@ __global__ void __launch_bounds__(kFThreads, 2) f32_dw_kernel(DwPass p, int jt_n
 struct FTile {
     int index;
     int64_t rows, cols, count;
-    template <class F> void with(F f) const {
+    // f(m, n); MIXED: 128 x 64 is among the sizes.
+    template <bool MIXED, class F> void with(F f) const {
         switch (index) {
         case 0: return f(std::integral_constant<int, 128>{}, std::integral_constant<int, 128>{});
-        case 1: return f(std::integral_constant<int, 128>{}, std::integral_constant<int, 64>{});
+        case 1:
+            if constexpr (MIXED) f(std::integral_constant<int, 128>{}, std::integral_constant<int, 64>{});
+            return;
         case 2: return f(std::integral_constant<int, 64>{}, std::integral_constant<int, 64>{});
         case 3: return f(std::integral_constant<int, 64>{}, std::integral_constant<int, 32>{});
         default: return f(std::integral_constant<int, 32>{}, std::integral_constant<int, 32>{});
@@ -377,15 +400,17 @@ FTile tile_at(int index, int64_t each, int64_t m, int64_t n) {
 //   2048 -> 8192, n_dyad 2, IT, 256 tokens: input gradient  694, 382, 251, 155, 163
 //                                           forward pass    168, 107, 98, 102, 103
 //   768 -> 3072, n_dyad 4, IT, 4096 tokens: forward pass    96, 102, 96, 111, 112
-FTile gemm_tile(int64_t each, int64_t m, int64_t n) {
+// wide: no more than 128 x 64, whose sums in 64 bits stay in registers.
+FTile gemm_tile(int64_t each, int64_t m, int64_t n, bool wide) {
     constexpr double per_value[kTiles] = {1., 1., 1.05, 1.2, 1.3};
     FTile best{};
     double least = 0;
-    for (int i = 0; i < kTiles; ++i) {
+    const int from = wide ? 1 : 0;
+    for (int i = from; i < kTiles; ++i) {
         const FTile t = tile_at(i, each, m, n);
         const double one = 0.85 / 8192 * kTileM[i] * kTileN[i], k = (double)((t.count + 255) / 256);
         const double busy = k * one * per_value[i], cost = busy > 0.45 + one ? busy : 0.45 + one;
-        if (i == 0 || cost < least) { best = t; least = cost; }
+        if (i == from || cost < least) { best = t; least = cost; }
     }
     return best;
 }
@@ -421,14 +446,17 @@ hipError_t launch_f32_gemm(const GemmPass &p, hipStream_t s) {
     if (128 * p.Kin * 4 >= lim || 32 * p.bn * 4 >= lim || 128 * p.D * p.bk * 4 >= lim) return hipErrorNotSupported;
     const int64_t classes = p.out_t ? p.D * p.D : p.D;
     const int64_t per_class = p.out_t ? (p.bn + p.D - 1) / p.D : p.bn;
-    const FTile tile = gemm_tile(classes, p.M, per_class);
+    const FTile tile = gemm_tile(classes, p.M, per_class, p.wide_sums);
     if (tile.count >= ((int64_t)1 << 31)) return hipErrorNotSupported;
     auto go = [&](auto in_t, auto out_t, auto w_t) {
         constexpr bool I = decltype(in_t)::value, O = decltype(out_t)::value, W = decltype(w_t)::value;
         const unsigned n = (unsigned)tile.count;
         const int ct = (int)tile.cols;
-        tile.with([&](auto bm, auto bn) {
-            f32_gemm_kernel<decltype(bm)::value, decltype(bn)::value, I, O, W><<<n, kFThreads, 0, s>>>(p, ct);
+        tile.with<true>([&](auto bm, auto bn) {
+            constexpr int BM = decltype(bm)::value, BN = decltype(bn)::value;
+            constexpr bool wide = !W && BN < 128;
+            if (wide && p.wide_sums) f32_gemm_kernel<BM, BN, I, O, W, wide><<<n, kFThreads, 0, s>>>(p, ct);
+            else f32_gemm_kernel<BM, BN, I, O, W, false><<<n, kFThreads, 0, s>>>(p, ct);
         });
         return hipGetLastError();
     };
@@ -448,7 +476,7 @@ hipError_t launch_f32_dw_tiles(const DwPass &p, int64_t splits, int64_t tps, flo
     const unsigned n = (unsigned)tile.count;
     auto go = [&](auto in_t, auto out_t) {
         constexpr bool I = decltype(in_t)::value, O = decltype(out_t)::value;
-        tile.with([&](auto bj, auto bk) {
+        tile.with<false>([&](auto bj, auto bk) {
             f32_dw_kernel<decltype(bj)::value, decltype(bk)::value, I, O><<<n, kFThreads, 0, s>>>(
                 p, (int)tile.rows, (int)tile.cols, (int)splits, tps, part);
         });

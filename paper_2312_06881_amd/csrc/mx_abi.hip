@@ -160,8 +160,15 @@ int dyad_forward_mx8(dyad_variant variant_arg, int64_t n_in, int64_t n_out, int6
     const int64_t chunk = chunk_tokens(n_out, M, dtype);
     for (int64_t m = 0; m < M; m += chunk) {
         const int64_t c = M - m < chunk ? M - m : chunk;
-        rc = dyad_forward(variant_arg, n_in, n_out, n_dyad, c, dtype_arg, rows(X, m, n_in, elem(dtype)), W1, W2, bias,
-                          DYAD_ACT_GELU, rows(Y, m, n_out, elem(dtype)), workspace, stream);
+        if (dtype == DYAD_F32) {
+            p.M = c; p.in = rows(X, m, n_in, 4); p.out = rows(Y, m, n_out, 4); p.h_out = workspace;
+            p.h8 = p.hs = nullptr;
+            p.wide_sums = true;
+            rc = launch_status(dyad::launch_simt_gemm(p, stream));
+        } else {
+            rc = dyad_forward(variant_arg, n_in, n_out, n_dyad, c, dtype_arg, rows(X, m, n_in, 2), W1, W2, bias,
+                              DYAD_ACT_GELU, rows(Y, m, n_out, 2), workspace, stream);
+        }
         if (rc) return rc;
         rc = launch_status(dyad::launch_mx_quantize(DYAD_MX_INT8, c, n_out, dtype, workspace, rows(H8, m, n_out, 1),
                                                     rows(Hs, m, (n_out + 31) / 32, 1), stream));
