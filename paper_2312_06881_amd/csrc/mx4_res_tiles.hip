@@ -240,6 +240,11 @@ hipError_t launch_mx4_res_tiles(const Mx4Args &a, hipStream_t s) {
         if (sn >= 2 && tiles(8, 2) >= 512) return launch<8, 2, 4>(a, s);
         return hipErrorNotSupported;
     }
+    // two workgroups to a CU, one storing while the other multiplies, where the
+    // reduction is short: 2048 -> 8192, two steps, 66 us against 76 on the tile of
+    // twice the tokens; 4096 -> 16384, four, 210 against 233; 32768 -> 8192, 32, 135
+    // against 124
+    if (sn == 4 && a.steps <= 4 && tiles(4, 4) >= 512) return launch<4, 4, 8>(a, s);
     if (sn == 4 && tiles(8, 4) >= 256) return launch<8, 4, 8>(a, s);
     if (sn >= 2 && tiles(4, 2) >= 512) return launch<4, 2, 8>(a, s);
     if (tiles(4, 1) >= 256) return launch<4, 1, 8>(a, s);

@@ -1,0 +1,34 @@
+"""The fp4 product on large tiles over reductions of one to several matrix steps, n_dyad 8 and 16."""
+import pytest
+import torch
+
+from paper_2312_06881_amd import mx
+from tests import mx_reference as ref
+from tests.parity_util import assert_close
+from workloads import layer_inputs
+
+pytestmark = pytest.mark.gpu
+
+SHAPES = [  # (n_in, n_out, n_dyad, tokens): 1, 2, 3, 4 and 5 steps of 128
+    (1000, 4096, 8, 4100),
+    (2048, 4096, 8, 4100),
+    (4096, 16384, 16, 1100),
+    (3072, 4096, 8, 4131),
+    (4096, 4096, 8, 4100),
+    (5120, 4096, 8, 4200),
+]
+
+
+@pytest.mark.parametrize("variant", ["OT", "DT"])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_reduction_lengths(shape, variant):
+    """Rows that repeat 29 tokens: every place in the tiles gives the oracle's rows."""
+    n_in, n_out, D, M = shape
+    print("CASE mx reductions", shape, variant, flush=True)
+    L = layer_inputs(n_in, n_out, D, 29, "bf16", seed_offset=21)
+    w = mx.quantize_weights(L.W1.cuda(), L.W2.cuda(), variant, n_in, n_out)
+    x = L.X.cuda().repeat(M // 29 + 1, 1)[:M].contiguous()
+    y = mx.forward(x, w, L.bias.cuda(), act="gelu")
+    want = ref.mx4_forward(variant, n_in, n_out, D, L.f64("X"), L.f64("W1"), L.f64("W2"), L.f64("bias"), "gelu")
+    assert_close(y[:29], want, "bf16", "Y")
+    assert torch.equal(y, y[:29].repeat(M // 29 + 1, 1)[:M])
