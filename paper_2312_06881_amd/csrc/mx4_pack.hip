@@ -5,7 +5,8 @@
 // under an input transpose: a workgroup stages 16 tokens x a span of columns in
 // LDS, from which the contiguous blocks and the residues k*D + g are taken.
 // The lanes of a wave write 1 KB of a fragment in a row.  What bounds it is that
-// traffic.
+// traffic: 8192 tokens of 4096 in both orders, 25 us (4.1 TB/s), where one wave a
+// fragment that loads its values itself took 162.
 #include "mx_common.h"
 
 namespace dyad {
