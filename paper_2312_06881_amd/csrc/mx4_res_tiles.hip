@@ -1,8 +1,8 @@
 // The fp4 product on large tiles under an output transpose, bf16, shapes that
 // keep component 1's rows by residue (mx4_by_residue).
 //
-// A workgroup makes 16 * SM tokens x RG residues of 16 * SN outputs each, a wave a
-// residue.  Component 1's block of the input serves every wave and goes through
+// A workgroup makes 16 * SM tokens x RG residues of 16 * SN * SUB outputs each, SUB waves
+// to a residue.  Component 1's block of the input serves every wave and goes through
 // a shared LDS ring, loaded ahead; in component 2 each wave reads a block of its
 // own, through a private pair of slots that needs no barrier (the wave's own
 // wait says when its loads have arrived, and it loads a slot again once it has
@@ -18,24 +18,27 @@ namespace dyad {
 
 namespace {
 
-template <int SM, int SN, int RG>
+template <int SM, int SN, int RG, int SUB>
 struct Mx4ResTile {
+    static constexpr int kWaves = RG * SUB;
     static constexpr int kSlot = SM * 1024;
     // two workgroups to a CU where their rings fit twice
-    static constexpr int kSlots = RG * 2 * kSlot + 2 * kSlot <= 80 * 1024 && RG * 2 * kSlot + 3 * kSlot > 80 * 1024 ? 2 : 3;
+    static constexpr int kSlots =
+        kWaves * 2 * kSlot + 2 * kSlot <= 80 * 1024 && kWaves * 2 * kSlot + 3 * kSlot > 80 * 1024 ? 2 : 3;
     static constexpr int kPrivate = kSlots * kSlot;                        // first private slot
-    static constexpr int kRings = kPrivate + RG * 2 * kSlot;
+    static constexpr int kRings = kPrivate + kWaves * 2 * kSlot;
     static constexpr int kRun = RG * 2;                                    // bytes of a column j's residues
-    static constexpr int kPitch = 16 * SN * kRun + 16;
+    static constexpr int kPitch = 16 * SN * SUB * kRun + 16;
     static constexpr int kLds = kRings > 16 * SM * kPitch ? kRings : 16 * SM * kPitch;
     static constexpr int kGroups = 2 * kLds <= 160 * 1024 ? 2 : 1;         // workgroups to a CU
     static_assert(kLds <= 160 * 1024, "LDS");
 };
 
-template <int SM, int SN, int RG>
-__global__ void __launch_bounds__(64 * RG, (RG / 4 * Mx4ResTile<SM, SN, RG>::kGroups)) mx4_res_tile_kernel(Mx4Args a) {
-    using C = Mx4ResTile<SM, SN, RG>;
-    constexpr int GM = SM / 4, GN = (SN + 3) / 4, kPer = SM >= RG ? SM / RG : 1, kSet = SN + GM + GN;
+template <int SM, int SN, int RG, int SUB>
+__global__ void __launch_bounds__(64 * RG * SUB, (RG * SUB / 4 * Mx4ResTile<SM, SN, RG, SUB>::kGroups))
+mx4_res_tile_kernel(Mx4Args a) {
+    using C = Mx4ResTile<SM, SN, RG, SUB>;
+    constexpr int W = C::kWaves, GM = SM / 4, GN = (SN + 3) / 4, kPer = SM >= W ? SM / W : 1, kSet = SN + GM + GN;
     __shared__ __attribute__((aligned(1024))) unsigned char smem[C::kLds];
     lds_u8 *lds = (lds_u8 *)smem;
     const int lane = threadIdx.x & 63;
@@ -48,8 +51,8 @@ __global__ void __launch_bounds__(64 * RG, (RG / 4 * Mx4ResTile<SM, SN, RG>::kGr
     const int run = a.group_m * cols_n, first = pair / run * a.group_m;
     const int gm = a.tiles_m - first < a.group_m ? a.tiles_m - first : a.group_m;
     const int t0 = (first + pair % run % gm) * SM;
-    const int tn = pair % run / gm, g0 = item % halves * RG, g = g0 + wave;
-    const int per = a.bo / (16 * D), jf0 = tn * SN, i1 = jf0 / per;
+    const int tn = pair % run / gm, g0 = item % halves * RG, gw = wave % RG, g = g0 + gw;
+    const int per = a.bo / (16 * D), jf0 = tn * SN * SUB, i1 = jf0 / per, jf = jf0 + SN * (wave / RG);
     const int steps = a.steps, total = 2 * steps;
 
     // fragments past the tokens read as zeros; a block's SN fragments all exist
@@ -66,18 +69,18 @@ __global__ void __launch_bounds__(64 * RG, (RG / 4 * Mx4ResTile<SM, SN, RG>::kGr
     auto ws_rsrc = [&](int part, int frag) {
         return buffer_rsrc(a.ws + ((int64_t)part * a.w_groups + frag / 4) * steps * 256, (uint32_t)GN * (uint32_t)steps * 256u);
     };
-    const int wf1 = g * per + jf0 - i1 * per, x2 = a.in_t ? D + g : g;
+    const int wf1 = g * per + jf - i1 * per, x2 = a.in_t ? D + g : g;
     const __amdgpu_buffer_rsrc_t rX1 = x_rsrc(i1), rX2 = x_rsrc(x2), sX1 = xs_rsrc(i1), sX2 = xs_rsrc(x2);
-    const __amdgpu_buffer_rsrc_t rW1 = w_rsrc(i1, wf1), rW2 = w_rsrc(D + g, jf0), sW1 = ws_rsrc(i1, wf1), sW2 = ws_rsrc(D + g, jf0);
+    const __amdgpu_buffer_rsrc_t rW1 = w_rsrc(i1, wf1), rW2 = w_rsrc(D + g, jf), sW1 = ws_rsrc(i1, wf1), sW2 = ws_rsrc(D + g, jf);
 
     const uint32_t row = (uint32_t)steps * 1024u, srow = (uint32_t)steps * 256u, l16 = 16u * lane, l4 = 4u * lane;
-    // component 1's step s into ring slot `slot`: wave w takes fragments w, w + RG ..
+    // component 1's step s into ring slot `slot`: wave w takes fragments w, w + W ..
     auto issue1 = [&](int s, int slot) {
         s = s < steps ? s : steps - 1;
 #pragma unroll
         for (int q = 0; q < kPer; ++q)
-            if (SM >= RG || wave < SM)
-                dma16(rX1, lds + slot * C::kSlot + 1024 * (wave + RG * q), (uint32_t)(wave + RG * q) * row + l16, (uint32_t)s * 1024u);
+            if (SM >= W || wave < SM)
+                dma16(rX1, lds + slot * C::kSlot + 1024 * (wave + W * q), (uint32_t)(wave + W * q) * row + l16, (uint32_t)s * 1024u);
     };
     // component 2's step s into the wave's slot s % 2
     auto issue2 = [&](int s) {
@@ -148,7 +151,7 @@ __global__ void __launch_bounds__(64 * RG, (RG / 4 * Mx4ResTile<SM, SN, RG>::kGr
         uint4 x[SM];
         mx4_read<SM>(base + (uint32_t)(C::kPrivate + (2 * wave + (s & 1)) * C::kSlot), x);
         issue2(s + 2);
-        multiply(f, x, jf0);
+        multiply(f, x, jf);
         fetch(t + 2, f);
     };
     int t = 0;
@@ -174,17 +177,18 @@ __global__ void __launch_bounds__(64 * RG, (RG / 4 * Mx4ResTile<SM, SN, RG>::kGr
     const int row16 = lane & 15, quad = 4 * (lane >> 4);
     const uint16_t *bias = static_cast<const uint16_t *>(a.bias);
     const int64_t f00 = (int64_t)jf0 * 16 * D + g0;        // the tile's first column
+    const int c0 = 16 * (jf - jf0) + quad;
 #pragma unroll
     for (int j = 0; j < SN; ++j) {
         float b[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const int64_t f = f00 + (int64_t)(16 * j + quad + q) * D + wave;
+            const int64_t f = f00 + (int64_t)(c0 + 16 * j + q) * D + gw;
             b[q] = bias && f < a.n_out ? bf16_to_f32(bias[f]) : 0.f;
         }
 #pragma unroll
         for (int i = 0; i < SM; ++i) {
-            unsigned char *at = smem + (16 * i + row16) * C::kPitch + (16 * j + quad) * C::kRun + 2 * wave;
+            unsigned char *at = smem + (16 * i + row16) * C::kPitch + (c0 + 16 * j) * C::kRun + 2 * gw;
             float x[4];
 #pragma unroll
             for (int q = 0; q < 4; ++q) x[q] = mx4_act<uint16_t>(a, acc[j][i][q] + b[q]);
@@ -197,13 +201,13 @@ __global__ void __launch_bounds__(64 * RG, (RG / 4 * Mx4ResTile<SM, SN, RG>::kGr
         }
     }
     __syncthreads();
-    // 16-byte pieces: with RG = 8 a column j's eight residues, with 4 two columns of all four
-    constexpr int kRow = 16 * SN * C::kRun / 16, kCols = 8 / RG;
+    // 16-byte pieces: with RG = 8 a column j's eight residues, else 8 / RG columns of all
+    constexpr int kRow = 16 * SN * SUB * C::kRun / 16, kCols = 8 / RG;
     const int64_t m0 = (int64_t)t0 * 16;
     uint16_t *dst = static_cast<uint16_t *>(a.Y) + m0 * a.n_out;
 #pragma unroll 4
-    for (int q = 0; q < 16 * SM * kRow / (64 * RG); ++q) {
-        const int p = threadIdx.x + q * 64 * RG, r = p / kRow, at = p % kRow;
+    for (int q = 0; q < 16 * SM * kRow / (64 * W); ++q) {
+        const int p = threadIdx.x + q * 64 * W, r = p / kRow, at = p % kRow;
         const int64_t f = f00 + (int64_t)(at * kCols) * D;
         if (m0 + r < a.M && f + 8 <= a.n_out)
             *reinterpret_cast<uint4 *>(dst + r * a.n_out + f) = *reinterpret_cast<const uint4 *>(smem + r * C::kPitch + 16 * at);
@@ -212,22 +216,22 @@ __global__ void __launch_bounds__(64 * RG, (RG / 4 * Mx4ResTile<SM, SN, RG>::kGr
 
 }  // namespace
 
-template <int SM, int SN, int RG>
+template <int SM, int SN, int RG, int SUB = 1>
 static hipError_t launch(Mx4Args a, hipStream_t s) {
-    const int64_t tiles_n = a.n_out / (16 * SN * a.D) * (a.D / RG), tiles_m = (a.x_frags + SM - 1) / SM;
+    const int64_t tiles_n = a.n_out / (16 * SN * SUB * a.D) * (a.D / RG), tiles_m = (a.x_frags + SM - 1) / SM;
     if (tiles_n * tiles_m >= ((int64_t)1 << 31)) return hipErrorNotSupported;
     a.tiles_n = (int)tiles_n;
     a.tiles_m = (int)tiles_m;
     a.tiles = (int)(tiles_n * tiles_m);
     a.group_m = 8;
-    mx4_res_tile_kernel<SM, SN, RG><<<(unsigned)a.tiles, 64 * RG, 0, s>>>(a);
+    mx4_res_tile_kernel<SM, SN, RG, SUB><<<(unsigned)a.tiles, 64 * RG * SUB, 0, s>>>(a);
     return hipGetLastError();
 }
 
 hipError_t launch_mx4_res_tiles(const Mx4Args &a, hipStream_t s) {
     const int D = a.D, per = a.bo / (16 * D);
     // whole rows of outputs in 16-byte pieces, 32-bit offsets inside a tile
-    if ((D != 4 && D != 8 && D != 16) || a.n_out != (int64_t)D * a.bo || a.x_frags < 4 || (int64_t)8 * a.steps * 1024 >= ((int64_t)1 << 31))
+    if ((D != 2 && D != 4 && D != 8 && D != 16) || a.n_out != (int64_t)D * a.bo || a.x_frags < 4 || (int64_t)8 * a.steps * 1024 >= ((int64_t)1 << 31))
         return hipErrorNotSupported;
     // short reductions are mostly epilogue, which smaller workgroups overlap better
     // (8192 tokens of 768 -> 3072, n_dyad 4, two steps: 35 us against 31; 2048 -> 8192,
@@ -235,8 +239,17 @@ hipError_t launch_mx4_res_tiles(const Mx4Args &a, hipStream_t s) {
     if (a.steps < 4 && D == 4) return hipErrorNotSupported;
     const int rg = D == 4 ? 4 : 8, sn = per % 4 == 0 ? 4 : per % 2 == 0 ? 2 : 1;
     auto tiles = [&](int sm, int n) { return (int64_t)(a.n_out / (16 * n * D)) * (D / rg) * ((a.x_frags + sm - 1) / sm); };
+    // n_dyad 2: two waves to a residue.  Against the small tiles, 4096 -> 4096, 7561
+    // tokens (960 tiles of 16 steps) 106 us against 153; 16384 -> 4096, 1402 tokens
+    // (176 of 64) 93 against 150; 1024 -> 4096, 2048 tokens (256 of 4) 22 against 20
+    if (D == 2) {
+        if (per % 8 != 0 || a.n_out / 256 * ((a.x_frags + 7) / 8) < (a.steps >= 16 ? 128 : 512)) return hipErrorNotSupported;
+        return launch<8, 4, 2, 2>(a, s);
+    }
     if (rg == 4) {
-        if (sn == 4 && tiles(8, 4) >= 512) return launch<8, 4, 4>(a, s);
+        // long reductions from half a tile a CU: 16384 -> 4096, 1100 tokens (144 tiles)
+        // 59 us against 71; 8192 -> 8192, 512 tokens (128 of 16 steps) 34 and 33
+        if (sn == 4 && tiles(8, 4) >= (a.steps >= 16 ? 128 : 512)) return launch<8, 4, 4>(a, s);
         if (sn >= 2 && tiles(8, 2) >= 512) return launch<8, 2, 4>(a, s);
         return hipErrorNotSupported;
     }

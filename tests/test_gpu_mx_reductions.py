@@ -1,4 +1,4 @@
-"""The fp4 product on large tiles over reductions of one to several matrix steps, n_dyad 8 and 16."""
+"""The fp4 product on large tiles over reductions of one to several matrix steps, n_dyad 2 to 16."""
 import pytest
 import torch
 
@@ -9,13 +9,17 @@ from workloads import layer_inputs
 
 pytestmark = pytest.mark.gpu
 
-SHAPES = [  # (n_in, n_out, n_dyad, tokens): 1, 2, 3, 4 and 5 steps of 128
+SHAPES = [  # (n_in, n_out, n_dyad, tokens): 1 to 5; 2, 8, 16; and 16 steps of 128
     (1000, 4096, 8, 4100),
     (2048, 4096, 8, 4100),
     (4096, 16384, 16, 1100),
     (3072, 4096, 8, 4131),
     (4096, 4096, 8, 4100),
     (5120, 4096, 8, 4200),
+    (512, 4096, 2, 4200),
+    (1900, 8192, 2, 2050),
+    (4096, 4096, 2, 1040),
+    (8192, 4096, 4, 1100),
 ]
 
 
