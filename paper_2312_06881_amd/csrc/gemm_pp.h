@@ -84,7 +84,7 @@ __host__ __device__ constexpr int64_t pp_slice_pitch(int64_t D, int BN) {
 //          pieces at a block's ends.
 //   RES:   the tile's outputs are columns n0.. of residue-major rows; its real
 //          columns (for the bias) are c_real + a.D * t.
-template <class C, int BM, int BN, bool SLICE, bool ADD, bool PAD, bool RES>
+template <class C, int BM, int BN, bool SLICE, bool ADD, bool PAD, bool RES, bool H8>
 __device__ __forceinline__ void pp_epilogue(const GemmArgs &a, unsigned char *smem,
                                             const f32x4_t (&acc)[C::kSubM][C::kSubN], int64_t m0, int n0, int g, int jb,
                                             int64_t rows_left, int lane, int wave, int wm0, int wn0, int c_real) {
@@ -123,7 +123,7 @@ __device__ __forceinline__ void pp_epilogue(const GemmArgs &a, unsigned char *sm
     const __amdgpu_buffer_rsrc_t rH = buffer_rsrc((hbase ? hbase : a.out) + m0 * Nr, rows_t * Nr * 2u);
 
     // the pre-activation in 8 bits, real rows of whole 32-blocks only
-    const bool h8 = !PAD && !RES && a.h8 != nullptr;
+    constexpr bool h8 = H8;
     const __amdgpu_buffer_rsrc_t rH8 = buffer_rsrc(h8 ? a.h8 + m0 * Nr : nullptr, h8 ? rows_t * Nr : 0u);
     const __amdgpu_buffer_rsrc_t rHs = buffer_rsrc(h8 ? a.hs + m0 * (Nr / 32) : nullptr, h8 ? rows_t * (Nr / 32) : 0u);
 
@@ -307,7 +307,9 @@ __device__ __forceinline__ void pp_epilogue(const GemmArgs &a, unsigned char *sm
     else if constexpr (PAD) rows(std::false_type{});
 }
 
-template <int BM, int BN, int WGM, int WGN, bool W_T, int FORM>
+// H8: the pre-activation is kept in 8 bits (a kernel of its own: a test of it in the
+// epilogue took the others 8 % of a 2048 -> 8192 step at n_dyad 8)
+template <int BM, int BN, int WGM, int WGN, bool W_T, int FORM, bool H8>
 __global__ void __launch_bounds__(kPPThreads, 1) dyad_gemm_pp(GemmArgs a) {
     using C = PPCfg<BM, BN, WGM, WGN, W_T>;
     using SA = typename C::A;
@@ -424,7 +426,7 @@ __global__ void __launch_bounds__(kPPThreads, 1) dyad_gemm_pp(GemmArgs a) {
         units, wave, acc, issue_a, issue_b, addr, both);
     const int no = kRes ? r * (int)(a.Nout / a.D) + g * (bn / D) + t0 : n0;
     pp_epilogue<C, BM, BN, FORM == kPPSlice, FORM == kPPAdd || FORM == kPPPadAdd,
-                FORM == kPPPadAdd || FORM == kPPPadPair, kRes>(a, smem, acc, m0, no, g, jb, rows_left, lane, wave, wm0,
+                FORM == kPPPadAdd || FORM == kPPPadPair, kRes, H8>(a, smem, acc, m0, no, g, jb, rows_left, lane, wave, wm0,
                                                                wn0, g * bn + r + D * t0);
 }
 
@@ -443,7 +445,14 @@ hipError_t launch_pp_tile(GemmArgs a, hipStream_t s) {
     // input block; with blocks of two to four tiles 8 panels share more.
     const int64_t per_block = a.bn / BN;
     a.group_m = per_block >= 2 && per_block < 8 ? 8 : 4;
-    dyad_gemm_pp<BM, BN, WGM, WGN, W_T, FORM><<<a.tiles_total, kPPThreads, 0, s>>>(a);
+    if (a.h8) {
+        if constexpr (FORM == kPPPair || FORM == kPPPairOne || FORM == kPPAdd)
+            dyad_gemm_pp<BM, BN, WGM, WGN, W_T, FORM, true><<<a.tiles_total, kPPThreads, 0, s>>>(a);
+        else
+            return hipErrorNotSupported;
+    } else {
+        dyad_gemm_pp<BM, BN, WGM, WGN, W_T, FORM, false><<<a.tiles_total, kPPThreads, 0, s>>>(a);
+    }
     return hipGetLastError();
 }
 
