@@ -76,7 +76,8 @@ __device__ __forceinline__ void store_h8(__amdgpu_buffer_rsrc_t codes, __amdgpu_
 // ADD: before the epilogue each sum gets the fp32 value of slice a.slice0 of
 // a.part at its column, or with a.unperm at the block-order place of it
 // (column g*bn + j for column j*D + g).
-template <class C, int BM, int BN, int D, bool OUT_T, bool PARTIAL, bool ADD = false>
+// H8: the pre-activation is kept in 8 bits.
+template <class C, int BM, int BN, int D, bool OUT_T, bool PARTIAL, bool ADD = false, bool H8 = false>
 __device__ __forceinline__ void gemm_epilogue_as(const GemmArgs &a, unsigned char *smem,
                                                  const f32x4_t (&acc)[C::kSubM][C::kSubN], int64_t m0, int n0,
                                                  int64_t rows_left, int tid, int lane, int wave, int wn0,
@@ -109,7 +110,7 @@ __device__ __forceinline__ void gemm_epilogue_as(const GemmArgs &a, unsigned cha
     const __amdgpu_buffer_rsrc_t rH = buffer_rsrc((hbase ? hbase : a.out) + m0 * a.Nout, o_bytes);
     // the pre-activation in 8 bits: a byte a value and one for 32, so a value at
     // byte v of the bf16 rows is at v / 2 of the codes and v / 64 of the scales
-    const bool h8 = !PARTIAL && a.h8 != nullptr;
+    constexpr bool h8 = H8;
     const __amdgpu_buffer_rsrc_t rH8 = buffer_rsrc(h8 ? a.h8 + m0 * a.Nout : nullptr, h8 ? o_bytes / 2 : 0u);
     const __amdgpu_buffer_rsrc_t rHs = buffer_rsrc(h8 ? a.hs + m0 * (a.Nout / 32) : nullptr, h8 ? o_bytes / 64 : 0u);
     auto load_h = [&](uint32_t vo) __attribute__((always_inline)) -> uint4 {
@@ -405,13 +406,17 @@ __device__ __forceinline__ void gemm_epilogue_pad(const GemmArgs &a, unsigned ch
 }
 
 // The epilogue, or with a split reduction (a.part set) the fp32 partial sums:
-// two inlined instances, so the bias / GELU / GELU' path carries no test of it.
+// inlined instances, so the bias / GELU / GELU' path carries no test of it, nor of
+// an 8-bit pre-activation (tests of which took 3 % of OPT-350m's training step).
 template <class C, int BM, int BN, int D, bool OUT_T>
 __device__ __forceinline__ void gemm_epilogue(const GemmArgs &a, unsigned char *smem,
                                               const f32x4_t (&acc)[C::kSubM][C::kSubN], int64_t m0, int n0,
                                               int64_t rows_left, int tid, int lane, int wave, int wn0, int split) {
     if (a.part)
         gemm_epilogue_as<C, BM, BN, D, OUT_T, true>(a, smem, acc, m0, n0, rows_left, tid, lane, wave, wn0, split);
+    else if (a.h8)
+        gemm_epilogue_as<C, BM, BN, D, OUT_T, false, false, true>(a, smem, acc, m0, n0, rows_left, tid, lane, wave, wn0,
+                                                                  split);
     else
         gemm_epilogue_as<C, BM, BN, D, OUT_T, false>(a, smem, acc, m0, n0, rows_left, tid, lane, wave, wn0, split);
 }

@@ -348,9 +348,14 @@ dyad_gemm_mfma2(GemmArgs a) {
         __syncthreads();
     }
 
-    if constexpr (ONLY == 3)
-        gemm_epilogue_as<C, BM, BN, D, OUT_T, false, true>(a, smem, acc, m0, n0, rows_left, tid, lane, wave, wn0,
-                                                           split);
+    if constexpr (ONLY == 3) {
+        if (a.h8)
+            gemm_epilogue_as<C, BM, BN, D, OUT_T, false, true, true>(a, smem, acc, m0, n0, rows_left, tid, lane, wave,
+                                                                     wn0, split);
+        else
+            gemm_epilogue_as<C, BM, BN, D, OUT_T, false, true>(a, smem, acc, m0, n0, rows_left, tid, lane, wave, wn0,
+                                                               split);
+    }
     else if constexpr (ONLY >= 4)
         gemm_epilogue_pad<C, BM, BN, ONLY == 4>(a, smem, acc, m0, n0, rows_left, tid, lane, wave, wn0);
     else
