@@ -253,8 +253,7 @@ int dyad_mx4_forward(dyad_variant variant, int64_t n_in, int64_t n_out, int64_t 
  * dyad_mx_quantize writes them, along each token's row):
  *   dyad_forward_mx8      dyad_forward with GELU, whose pre-activation H is kept as
  *                         H8 / Hs, the quantised value of what H would hold (in
- *                         fp32, blocks of a multiple of 4 that need no padding: of
- *                         H summed in 64 bits and rounded once)
+ *                         fp32: of H summed in 64 bits and rounded once)
  *   dyad_backward_dx_mx8  dyad_backward_dx with act_in GELU at the kept H:
  *                         dX = (W^T dZ) * GELU'(H8).  A, when not NULL, receives
  *                         GELU(H8) [M][n_in], this layer's input, for the weight

@@ -45,7 +45,7 @@ struct GemmPass {
     // (mx_common.h), written in place of h_out or read in place of h_in; null: none
     uint8_t *h8, *hs;
     void *a_out;     // kEpiGeluGrad with h8: receives GELU(h); null: not wanted
-    bool wide_sums;  // fp32 forward on the matrix instructions: sums in 64 bits
+    bool wide_sums;  // fp32 forward: sums in 64 bits
 };
 
 // Weight/bias gradient of one layer (forward-variant flags in_t/out_t):

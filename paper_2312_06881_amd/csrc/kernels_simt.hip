@@ -1,7 +1,7 @@
 // General kernels: any n_dyad, any block sizes, widths that n_dyad does not
 // divide (zero-padded), both dtypes.  Every shape the matrix-core kernels do
 // not cover uses them.  Arithmetic is fp32 FMA on the vector ALUs,
-// tiled through LDS.
+// tiled through LDS (64-bit FMA in an fp32 forward pass that asks for it).
 //
 // Grouped GEMM (forward and input gradient).  The output columns of a pass
 // fall into classes (g1, g2): g1 = f / bn is the BlockDiag group of column f
@@ -31,8 +31,9 @@ constexpr int kKC = 8;    // K chunk staged in LDS
 __device__ __forceinline__ int sub_of(int t4, int i) { return (i < 4 ? 0 : 64) + 4 * t4 + (i & 3); }
 
 // acc[i][j] += a[i] * b[j] over one staged chunk; a and b are LDS rows of kT floats.
+template <typename Sum>
 __device__ __forceinline__ void fma_block(const float *arow, const float *brow, int ty, int tx, float (&a)[8],
-                                          float (&b)[8], float (&acc)[8][8]) {
+                                          float (&b)[8], Sum (&acc)[8][8]) {
     const float4 a0 = *reinterpret_cast<const float4 *>(arow + 4 * ty);
     const float4 a1 = *reinterpret_cast<const float4 *>(arow + 64 + 4 * ty);
     const float4 b0 = *reinterpret_cast<const float4 *>(brow + 4 * tx);
@@ -42,7 +43,7 @@ __device__ __forceinline__ void fma_block(const float *arow, const float *brow, 
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[i][j] = fmaf(a[i], b[j], acc[i][j]);
+        for (int j = 0; j < 8; ++j) acc[i][j] = fma((Sum)a[i], (Sum)b[j], acc[i][j]);
 }
 
 // One class of output columns of a grouped-GEMM pass.
@@ -69,7 +70,11 @@ __device__ __forceinline__ ColClass col_class(const GemmPass &p, int64_t cls) {
     return c;
 }
 
-template <typename T>
+// Sum: double for GemmPass::wide_sums, rounded to 32 bits once the bias is in.  A
+// pre-activation kept in 8 bits then takes the exact sum's code here too: of 1.8
+// million values (600 tokens of 768 -> 3072, n_dyad 5) sums in 32 bits moved 6, and
+// fc2's weight gradient by 7e-5.  That pass 111 -> 123 us, 241 -> 331 at 4096 tokens.
+template <typename T, typename Sum>
 __global__ void __launch_bounds__(256, 2) general_gemm_kernel(GemmPass p, int64_t col_tiles, int64_t row_tiles) {
     __shared__ __attribute__((aligned(16))) float As[2][kKC][kT];
     __shared__ __attribute__((aligned(16))) float Bs[2][kKC][kT];
@@ -144,11 +149,11 @@ __global__ void __launch_bounds__(256, 2) general_gemm_kernel(GemmPass p, int64_
         }
     };
 
-    float acc[8][8];
+    Sum acc[8][8];
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[i][j] = 0.f;
+        for (int j = 0; j < 8; ++j) acc[i][j] = 0;
 
     fetch(0);
     stash(0);
@@ -176,11 +181,11 @@ __global__ void __launch_bounds__(256, 2) general_gemm_kernel(GemmPass p, int64_
             if (t >= cc.count) continue;
             const int64_t f = cc.col(t);
             const int64_t e = m * p.Nout + f;
-            float v = acc[i][j];
+            float v = (float)acc[i][j];
             if (p.epilogue == kEpiGeluGrad) {
                 v *= gelu_grad_f32(load_f32(static_cast<const T *>(p.h_in), e));
             } else {
-                if (p.bias) v += load_f32(static_cast<const T *>(p.bias), f);
+                if (p.bias) v = (float)(acc[i][j] + load_f32(static_cast<const T *>(p.bias), f));
                 if (p.epilogue == kEpiBiasGelu) {
                     if (p.h_out) store_f32(static_cast<T *>(p.h_out), e, v);
                     v = gelu_f32(v);
@@ -335,10 +340,12 @@ hipError_t launch_simt_gemm(const GemmPass &p, hipStream_t s) {
     const int64_t row_tiles = (p.M + kT - 1) / kT;
     const int64_t blocks = classes * col_tiles * row_tiles;
     if (blocks >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
-    if (p.dtype == kF32)
-        general_gemm_kernel<float><<<(unsigned)blocks, 256, 0, s>>>(p, col_tiles, row_tiles);
+    if (p.dtype == kF32 && p.wide_sums)
+        general_gemm_kernel<float, double><<<(unsigned)blocks, 256, 0, s>>>(p, col_tiles, row_tiles);
+    else if (p.dtype == kF32)
+        general_gemm_kernel<float, float><<<(unsigned)blocks, 256, 0, s>>>(p, col_tiles, row_tiles);
     else
-        general_gemm_kernel<uint16_t><<<(unsigned)blocks, 256, 0, s>>>(p, col_tiles, row_tiles);
+        general_gemm_kernel<uint16_t, float><<<(unsigned)blocks, 256, 0, s>>>(p, col_tiles, row_tiles);
     return hipGetLastError();
 }
 
