@@ -40,12 +40,36 @@ def _same_device(x, *ts):
 class MXTensor:
     """A tensor quantised along its last dimension: ``codes`` (int8 [rows, cols], or fp4
     pairs uint8 [rows, ceil(cols/2)]), ``scales`` uint8 [rows, ceil(cols/32)], and the
-    ``shape`` and ``dtype`` of what they stand for."""
+    ``shape`` and ``dtype`` of what they stand for.  Codes and scales that are not as
+    many as that are refused, here and where they are read."""
 
     __slots__ = ("codes", "scales", "shape", "dtype", "format")
 
     def __init__(self, codes, scales, shape, dtype, format):
+        if format not in FORMATS:
+            raise ValueError("format is int8 or fp4")
         self.codes, self.scales, self.shape, self.dtype, self.format = codes, scales, torch.Size(shape), dtype, format
+        self._check()
+
+    @classmethod
+    def _of(cls, codes, scales, shape, dtype, format):
+        """One whose parts were made for it (what reads it checks them)."""
+        q = cls.__new__(cls)
+        q.codes, q.scales, q.shape, q.dtype, q.format = codes, scales, torch.Size(shape), dtype, format
+        return q
+
+    def _check(self):
+        # the calls take no lengths: they read what the shape says
+        codes, scales, shape = self.codes, self.scales, self.shape
+        cols = shape[-1] if shape else 0
+        rows = shape.numel() // cols if cols else -1
+        width, kind = (cols, torch.int8) if self.format == "int8" else ((cols + 1) // 2, torch.uint8)
+        if not (codes.numel() == rows * width and scales.numel() == rows * -(-cols // BLOCK) and codes.dtype is kind
+                and scales.dtype is torch.uint8 and codes.device == scales.device and codes.is_contiguous()
+                and scales.is_contiguous()):
+            raise ValueError(f"an MXTensor in {self.format} of shape {tuple(shape)} does not have codes {codes.dtype} "
+                             f"{tuple(codes.shape)} on {codes.device} and scales {scales.dtype} {tuple(scales.shape)} on "
+                             f"{scales.device}")
 
     @property
     def nbytes(self):
@@ -53,6 +77,7 @@ class MXTensor:
 
     def dequantize(self, dtype=None):
         """The values, in ``dtype`` (float32 or bfloat16; default: the quantised tensor's)."""
+        self._check()
         y = torch.empty(self.shape, dtype=dtype or self.dtype, device=self.codes.device)
         if y.numel():
             rows, cols = y.numel() // self.shape[-1], self.shape[-1]
@@ -64,7 +89,7 @@ class MXTensor:
 def _empty(rows, cols, shape, dtype, format, device):
     codes = (torch.empty((rows, cols), dtype=torch.int8, device=device) if format == "int8" else
              torch.empty((rows, (cols + 1) // 2), dtype=torch.uint8, device=device))
-    return MXTensor(codes, torch.empty((rows, -(-cols // BLOCK)), dtype=torch.uint8, device=device), shape, dtype, format)
+    return MXTensor._of(codes, torch.empty((rows, -(-cols // BLOCK)), dtype=torch.uint8, device=device), shape, dtype, format)
 
 
 def quantize(x, format="int8"):
@@ -139,7 +164,8 @@ def _kept(q, M, cols, like):
     if q.format != "int8" or tuple(q.shape) != (M, cols) or q.dtype != like.dtype:
         raise ValueError(f"expected an int8 MXTensor of shape {(M, cols)} and {like.dtype}, got {q.format} "
                          f"{tuple(q.shape)} of {q.dtype}")
-    _same_device(like, q.codes, q.scales)
+    q._check()
+    _same_device(like, q.codes)
 
 
 def forward_gelu(x, w1, w2, bias=None, variant="IT", n_out=None):

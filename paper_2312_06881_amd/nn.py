@@ -131,7 +131,7 @@ def _parts(q):
 
 
 def _kept(parts, like, cols):
-    return mx.MXTensor(*parts, (like.shape[0], cols), like.dtype, "int8")
+    return mx.MXTensor._of(*parts, (like.shape[0], cols), like.dtype, "int8")
 
 
 class _DyadLinearStashFn(torch.autograd.Function):

@@ -1,0 +1,56 @@
+"""Tensors that do not hold what a microscaled call would read are refused before it."""
+import pytest
+import torch
+
+from paper_2312_06881_amd import mx
+
+BF16 = torch.bfloat16
+
+
+def parts(rows, cols, fmt="int8"):
+    codes = (torch.zeros(rows, cols, dtype=torch.int8) if fmt == "int8" else
+             torch.zeros(rows, (cols + 1) // 2, dtype=torch.uint8))
+    return codes, torch.zeros(rows, -(-cols // 32), dtype=torch.uint8)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp4"])
+@pytest.mark.parametrize("shape", [(4, 64), (3, 33), (2, 5, 40), (7,), (0, 40), (1, 1)])
+def test_tensor_holds_its_shape(shape, fmt):
+    rows, cols = torch.Size(shape[:-1]).numel(), shape[-1]
+    codes, scales = parts(rows, cols, fmt)
+    q = mx.MXTensor(codes, scales, shape, BF16, fmt)
+    assert q.shape == torch.Size(shape) and q.nbytes == codes.numel() + scales.numel()
+    wrong = [(torch.cat([codes, codes.new_zeros(1, codes.shape[1])]), scales),
+             (codes, torch.cat([scales, scales.new_zeros(1, scales.shape[1])])),
+             (codes.to(torch.int16), scales), (codes, scales.to(torch.int8)), (codes, scales.to("meta")),
+             (codes.view(torch.uint8 if fmt == "int8" else torch.int8), scales)]
+    if rows > 0:
+        wrong += [(codes[:-1], scales), (codes, scales[:-1]), (codes.flatten()[:-1], scales)]
+    if rows > 1 and codes.shape[1] > 1:
+        wrong.append((codes.t().contiguous().t(), scales))
+    for c, s in wrong:
+        with pytest.raises(ValueError, match="MXTensor"):
+            mx.MXTensor(c, s, shape, BF16, fmt)
+
+
+def test_tensor_of_no_format_or_columns():
+    with pytest.raises(ValueError, match="int8 or fp4"):
+        mx.MXTensor(*parts(2, 8), (2, 8), BF16, "int4")
+    for shape in ((), (2, 0)):
+        with pytest.raises(ValueError, match="MXTensor"):
+            mx.MXTensor(*parts(2, 8), shape, BF16, "int8")
+
+
+def test_tensor_changed_since():
+    """What was replaced or resized after the tensor was made is found when it is read."""
+    q = mx.MXTensor(*parts(4, 64), (4, 64), BF16, "int8")
+    dz = torch.zeros(4, 64, dtype=BF16)
+    q.codes = q.codes[:3]
+    for call in (q.dequantize, lambda: mx.backward_dw(dz, q, 4),
+                 lambda: mx.backward_dx_gelu(dz, torch.zeros(4, 16, 16, dtype=BF16), torch.zeros(4, 16, 16, dtype=BF16), q)):
+        with pytest.raises(ValueError, match="MXTensor"):
+            call()
+    q = mx.MXTensor(*parts(4, 64), (4, 64), BF16, "int8")
+    q.scales.resize_(4, 1)
+    with pytest.raises(ValueError, match="MXTensor"):
+        q.dequantize()
