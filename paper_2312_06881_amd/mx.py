@@ -141,7 +141,7 @@ def forward(x, weights, bias=None, act="none", workspace=None):
         raise ValueError(f"x has {n_in} columns, the weights {w.n_in}")
     if bias is not None and bias.shape != (w.n_out,):
         raise ValueError(f"bias has shape {tuple(bias.shape)}, the layer {w.n_out} outputs")
-    _same_device(x, w.packed, bias)
+    _same_device(x, w.packed, bias, workspace)
     v, dt, xp = _variant(w.variant), _dtype(x, bias), _ptr(x)
     y = torch.empty((M, w.n_out), dtype=x.dtype, device=x.device)
     if workspace is None:
@@ -168,12 +168,22 @@ def _kept(q, M, cols, like):
     _same_device(like, q.codes)
 
 
+def _layer(x, w1, w2, bias=None, n_out=None):
+    """Both components of one shape, the bias of the layer's width, all where x is."""
+    if w2.shape != w1.shape:
+        raise ValueError("W1 and W2 must have one shape")
+    if bias is not None and bias.shape != (n_out,):
+        raise ValueError(f"bias has shape {tuple(bias.shape)}, the layer {n_out} outputs")
+    _same_device(x, w1, w2, bias)
+
+
 def forward_gelu(x, w1, w2, bias=None, variant="IT", n_out=None):
     """(GELU(h), MXTensor of h) with h = W x + b, x [M, n_in]."""
     D, bo, bi = w1.shape
     M, n_in = x.shape
     _width(n_in, D, bi, "n_in")
     n_out = _width(n_out if n_out is not None or bias is None else bias.shape[0], D, bo, "n_out")
+    _layer(x, w1, w2, bias, n_out)
     v, dt = _variant(variant), _dtype(x, w1, w2, bias)
     xp = _ptr(x)
     y = torch.empty((M, n_out), dtype=x.dtype, device=x.device)
@@ -192,6 +202,7 @@ def backward_dx_gelu(dz, w1, w2, h, variant="IT", want_act=False):
     n_in = _width(h.shape[1], D, bi, "n_in")
     _width(n_out, D, bo, "n_out")
     _kept(h, M, n_in, dz)
+    _layer(dz, w1, w2)
     v, dt, zp = _variant(variant), _dtype(dz, w1, w2), _ptr(dz)
     dx = torch.empty((M, n_in), dtype=dz.dtype, device=dz.device)
     a = torch.empty_like(dx) if want_act else None

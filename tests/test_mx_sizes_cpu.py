@@ -54,3 +54,20 @@ def test_tensor_changed_since():
     q.scales.resize_(4, 1)
     with pytest.raises(ValueError, match="MXTensor"):
         q.dequantize()
+
+
+def test_operands_of_other_sizes_or_devices():
+    x, w = torch.zeros(4, 64, dtype=BF16), torch.zeros(4, 16, 16, dtype=BF16)
+    q = mx.MXTensor(*parts(4, 64), (4, 64), BF16, "int8")
+    packed = mx.MX4Weights(torch.zeros(8, dtype=torch.uint8), "IT", 64, 64, 4)
+    with pytest.raises(ValueError, match="one shape"):
+        mx.forward_gelu(x, w, w[:, :8])
+    with pytest.raises(ValueError, match="one shape"):
+        mx.backward_dx_gelu(x, w, w[:3], q)
+    with pytest.raises(ValueError, match="bias"):
+        mx.forward_gelu(x, w, w, torch.zeros(60, dtype=BF16), n_out=64)
+    for call in (lambda: mx.forward_gelu(x, w, w.to("meta")), lambda: mx.forward_gelu(x, w, w, torch.zeros(64, dtype=BF16, device="meta")),
+                 lambda: mx.backward_dx_gelu(x, w.to("meta"), w, q), lambda: mx.backward_dw(x.to("meta"), q, 4),
+                 lambda: mx.forward(x, packed, workspace=torch.zeros(8, dtype=torch.uint8, device="meta"))):
+        with pytest.raises(ValueError, match="one device"):
+            call()
