@@ -58,12 +58,12 @@ __device__ __forceinline__ float mx_int8_step(uint32_t s) {
 }
 
 // Values of four codes.  The bytes become unsigned (code + 128), which convert
-// in one instruction; one fused multiply-add takes the 128 off again, exactly.
+// in one instruction; the 128 goes off before the step comes on, where the
+// largest blocks (127 * 2^121) stay finite, as 128 * 2^121 does not.  Both are exact.
 __device__ __forceinline__ void mx_int8_values(uint32_t codes, float step, float (&x)[4]) {
     const uint32_t u = codes ^ 0x80808080u;
-    const float off = -128.f * step;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = fmaf((float)((u >> (8 * e)) & 255u), step, off);
+    for (int e = 0; e < 4; ++e) x[e] = ((float)((u >> (8 * e)) & 255u) - 128.f) * step;
 }
 
 // Eight codes as packed bf16, which holds each exactly.
