@@ -10,7 +10,8 @@ k / 64) or 4 (``"fp4"``: 0, .5, 1, 1.5, 2, 3, 4, 6); see ``include/dyad.h``.
   activations are checkpointed as int8 ``MXTensor``s.
 
 Outputs and workspaces come from torch's allocator on the inputs' device and
-every call runs on torch's current stream there.
+every call runs on torch's current stream there.  Autograd does not see these calls;
+the modules in ``nn`` are what it does.
 """
 from __future__ import annotations
 

@@ -59,14 +59,19 @@ class _DyadLinearFn(torch.autograd.Function):
         return dx, dw1, dw2, db, None, None
 
 
-def _plain(*ts):
-    """Whether a call records nothing and may skip autograd: gradients are off, no forward-mode
-    level, functorch transform or tracer is active, and every argument is a plain tensor."""
-    if torch.is_grad_enabled() or forward_ad._current_level >= 0 or torch._C._are_functorch_transforms_active():
+def _untracked(*ts):
+    """Whether no forward-mode level, functorch transform or tracer is active, and every argument
+    is a plain tensor."""
+    if forward_ad._current_level >= 0 or torch._C._are_functorch_transforms_active():
         return False
     if torch.compiler.is_compiling() or torch.jit.is_tracing():
         return False
     return all(t is None or type(t) in (torch.Tensor, torch.nn.Parameter) for t in ts)
+
+
+def _plain(*ts):
+    """Whether a call records nothing and may skip autograd: gradients are off, and it is untracked."""
+    return not torch.is_grad_enabled() and _untracked(*ts)
 
 
 _REFUSED = (-2, -4)   # DYAD_ERR_SHAPE, DYAD_ERR_DTYPE: no fused kernel for this layer
@@ -322,9 +327,27 @@ class DyadFF(torch.nn.Module):
                        (self.fc2.w1, self.fc2.w2, self.fc2.bias), self.variant, self.ffn, self.fused, self.stash)
 
 
+class _MX4Fn(torch.autograd.Function):
+    """The fp4 product where autograd, forward mode or a tracer looks on: it has no gradient, and
+    one that would have to pass through it is refused."""
+
+    @staticmethod
+    def forward(ctx, x, packed, bias, variant, n_in, n_out, n_dyad, act):
+        return mx.forward(x, mx.MX4Weights(packed, variant, n_in, n_out, n_dyad), bias, act)
+
+    @staticmethod
+    def backward(ctx, dy):
+        raise NotImplementedError("the fp4 product has no gradient")
+
+    @staticmethod
+    def jvp(ctx, *tangents):
+        raise NotImplementedError("the fp4 product has no gradient, forward-mode ones included")
+
+
 class MX4DyadLinear(torch.nn.Module):
     """A ``DyadLinear`` for inference on fp4 weights, its input quantised to fp4 within the
-    call; the weights are quantised once, here.  act: "none" or "gelu"."""
+    call; the weights are quantised once, here.  act: "none" or "gelu".  It has no gradient:
+    a backward pass or a tangent that reaches it raises."""
 
     def __init__(self, layer: DyadLinear, act="none"):
         super().__init__()
@@ -338,8 +361,14 @@ class MX4DyadLinear(torch.nn.Module):
         self.register_buffer("bias", None if layer.bias is None else layer.bias.detach().clone())
 
     def forward(self, x):
-        w = mx.MX4Weights(self.packed, self.variant, self.in_features, self.out_features, self.n_dyad)
-        return mx.forward(_tokens(x), w, self.bias, self.act).reshape(*x.shape[:-1], self.out_features)
+        t = _tokens(x)
+        if _untracked(x, self.bias) and not (torch.is_grad_enabled() and x.requires_grad):
+            w = mx.MX4Weights(self.packed, self.variant, self.in_features, self.out_features, self.n_dyad)
+            y = mx.forward(t, w, self.bias, self.act)
+        else:
+            y = _MX4Fn.apply(t, self.packed, self.bias, self.variant, self.in_features, self.out_features, self.n_dyad,
+                             self.act)
+        return y.reshape(*x.shape[:-1], self.out_features)
 
     def extra_repr(self):
         return (f"in_features={self.in_features}, out_features={self.out_features}, n_dyad={self.n_dyad}, "
