@@ -109,6 +109,9 @@ def quantize(x, format="int8"):
 
 # ---- the fp4 product --------------------------------------------------------------
 
+LAYOUT = 1   # of packed fp4 weights (csrc/mx_internal.h), raised whenever that changes
+
+
 class MX4Weights:
     """One layer's W1 and W2 in fp4, in the library's own layout (``packed``)."""
 

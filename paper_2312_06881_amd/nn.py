@@ -29,7 +29,7 @@ import math
 import torch
 from torch.autograd import forward_ad
 
-from . import DyadError, backward_dw, backward_dx, forward, mx
+from . import VARIANTS, DyadError, backward_dw, backward_dx, forward, mx
 
 __all__ = ["DyadLinear", "DyadFF", "MX4DyadLinear", "MX4DyadFF", "dyad_linear", "dyad_ff"]
 
@@ -347,7 +347,8 @@ class _MX4Fn(torch.autograd.Function):
 class MX4DyadLinear(torch.nn.Module):
     """A ``DyadLinear`` for inference on fp4 weights, its input quantised to fp4 within the
     call; the weights are quantised once, here.  act: "none" or "gelu".  It has no gradient:
-    a backward pass or a tangent that reaches it raises."""
+    a backward pass or a tangent that reaches it raises.  Packed weights are as many bytes for
+    every variant, so a state dict says what they are of, and loading another layer's raises."""
 
     def __init__(self, layer: DyadLinear, act="none"):
         super().__init__()
@@ -359,6 +360,20 @@ class MX4DyadLinear(torch.nn.Module):
                                 layer.out_features)
         self.register_buffer("packed", w.packed)
         self.register_buffer("bias", None if layer.bias is None else layer.bias.detach().clone())
+        self.register_buffer("layout", torch.tensor(self._layout(), device=w.packed.device))
+
+    def _layout(self):
+        return [mx.LAYOUT, VARIANTS[self.variant], self.in_features, self.out_features, self.n_dyad]
+
+    def _load_from_state_dict(self, state_dict, prefix, local_metadata, strict, missing_keys, unexpected_keys, error_msgs):
+        layout = state_dict.get(prefix + "layout")
+        if layout is not None and layout.tolist() != self._layout():
+            error_msgs.append(f"{prefix}packed holds weights of (layout, variant, in, out, n_dyad) {layout.tolist()}, "
+                              f"the module's are {self._layout()}")
+            return
+        super()._load_from_state_dict(state_dict, prefix, local_metadata, strict, missing_keys, unexpected_keys, error_msgs)
+        if layout is None and prefix + "layout" in missing_keys:
+            missing_keys.remove(prefix + "layout")       # saved without it: nothing to compare
 
     def forward(self, x):
         t = _tokens(x)
