@@ -267,6 +267,8 @@ class DyadLinear(torch.nn.Module):
     n_dyad inputs each).  ``stash="mx8"`` keeps the input in 8 bits for the backward pass.
     """
 
+    stash = None        # of modules pickled without one
+
     def __init__(self, in_features, out_features, n_dyad, variant="IT", bias=True, device=None,
                  dtype=torch.bfloat16, stash=None):
         super().__init__()
@@ -307,6 +309,8 @@ class DyadFF(torch.nn.Module):
     writes only its pre-activation and fc2's kernels apply GELU as they stage it.
     ``stash="mx8"``: the input and the pre-activation are kept in 8 bits for the backward
     pass (not with ``fused``)."""
+
+    stash = None        # of modules pickled without one
 
     def __init__(self, d, ffn, n_dyad, variant="IT", bias=True, device=None, dtype=torch.bfloat16,
                  fused=False, stash=None):
