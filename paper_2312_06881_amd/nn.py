@@ -364,20 +364,23 @@ class MX4DyadLinear(torch.nn.Module):
                                 layer.out_features)
         self.register_buffer("packed", w.packed)
         self.register_buffer("bias", None if layer.bias is None else layer.bias.detach().clone())
-        self.register_buffer("layout", torch.tensor(self._layout(), device=w.packed.device))
 
     def _layout(self):
         return [mx.LAYOUT, VARIANTS[self.variant], self.in_features, self.out_features, self.n_dyad]
 
+    def _save_to_state_dict(self, destination, prefix, keep_vars):
+        super()._save_to_state_dict(destination, prefix, keep_vars)
+        destination[prefix + "layout"] = torch.tensor(self._layout())
+
     def _load_from_state_dict(self, state_dict, prefix, local_metadata, strict, missing_keys, unexpected_keys, error_msgs):
-        layout = state_dict.get(prefix + "layout")
+        layout = state_dict.get(prefix + "layout")           # None: saved without it, nothing to compare
         if layout is not None and layout.tolist() != self._layout():
             error_msgs.append(f"{prefix}packed holds weights of (layout, variant, in, out, n_dyad) {layout.tolist()}, "
                               f"the module's are {self._layout()}")
             return
         super()._load_from_state_dict(state_dict, prefix, local_metadata, strict, missing_keys, unexpected_keys, error_msgs)
-        if layout is None and prefix + "layout" in missing_keys:
-            missing_keys.remove(prefix + "layout")       # saved without it: nothing to compare
+        if prefix + "layout" in unexpected_keys:
+            unexpected_keys.remove(prefix + "layout")        # no parameter or buffer of the module
 
     def forward(self, x):
         t = _tokens(x)

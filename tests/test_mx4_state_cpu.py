@@ -58,5 +58,5 @@ def test_a_block_and_states_without_the_layout():
     assert torch.equal(a.fc2.packed, b.fc2.packed)
     with pytest.raises(RuntimeError, match="packed"):
         MX4DyadFF(DyadFF(64, 256, 4, ("IT", "DT"))).load_state_dict(state)
-    # moved or cast, the layout stays what it is
-    assert torch.equal(a.bfloat16().fc1.layout, state["fc1.layout"])
+    # no part of the module itself: what it holds is its weights and bias
+    assert [n for n, _ in a.named_buffers()] == ["fc1.packed", "fc1.bias", "fc2.packed", "fc2.bias"]
