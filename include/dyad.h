@@ -262,7 +262,9 @@ int dyad_mx4_forward(dyad_variant variant, int64_t n_in, int64_t n_out, int64_t 
  *                         GELU the layer's input is GELU(X8)
  * H8 [M][n_out] for the forward pass, [M][n_in] for the input gradient; X8 [M][n_in].
  * The workspace holds dyad_mx8_workspace_bytes() bytes for the pass (act_in
- * counts for the weight gradient only).
+ * counts for the weight gradient only): none for forward passes and input
+ * gradients whose kernels keep and read 8 bits themselves (most bf16 layers
+ * without padding), at most 64 MB or 1024 tokens of them for the others.
  */
 typedef enum { DYAD_MX8_FORWARD = 0, DYAD_MX8_DX = 1, DYAD_MX8_DW = 2 } dyad_mx8_pass;
 size_t dyad_mx8_workspace_bytes(dyad_mx8_pass pass, dyad_variant variant, int64_t n_in, int64_t n_out, int64_t n_dyad,

@@ -46,6 +46,9 @@ struct GemmPass {
     uint8_t *h8, *hs;
     void *a_out;     // kEpiGeluGrad with h8: receives GELU(h); null: not wanted
     bool wide_sums;  // fp32 forward: sums in 64 bits
+    // launch_mfma_gemm launches nothing and says whether it would take the pass
+    // with no workspace to be had; makes no HIP call
+    bool plan;
 };
 
 // Weight/bias gradient of one layer (forward-variant flags in_t/out_t):

@@ -64,6 +64,7 @@ hipError_t launch_tile(const GemmPass &p, hipStream_t s, int splits = 0) {
     if (tiles_m * tiles_n >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
     a.tiles_n = (int)tiles_n;
     a.tiles_total = (int)(tiles_m * tiles_n);
+    if (p.plan) return hipSuccess;
     gemm_split_ws(p, splits > 0 ? splits : gemm_splits(p, a.tiles_total, PF), s, a);
     dyad_gemm_mfma<BM, BN, WGM, WGN, D, IN_T, OUT_T, W_T, occupancy<C>(), PF, GELU_IN>
         <<<a.tiles_total * a.splits, C::kThreads, 0, s>>>(a);
@@ -97,6 +98,7 @@ hipError_t launch_tile2(const GemmPass &p, hipStream_t s) {
     if (tiles_m * tiles_n >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
     a.tiles_n = (int)tiles_n;
     a.tiles_total = (int)(tiles_m * tiles_n);
+    if (p.plan) return hipSuccess;
     gemm_split_ws(p, gemm_splits(p, a.tiles_total, 1), s, a);
     dyad_gemm_mfma2<BM, BN, WGM, WGN, D, IN_T, OUT_T, W_T><<<a.tiles_total * a.splits, C::kThreads, 0, s>>>(a);
     hipError_t e = hipGetLastError();
@@ -211,7 +213,7 @@ hipError_t launch_components(const GemmPass &p, hipStream_t s) {
         if constexpr (!k64 && !k32) {
             return hipErrorNotSupported;
         } else {
-            if (p.bn % 64 != 0 || p.Nout % 256 != 0) return hipErrorNotSupported;
+            if (p.plan || p.bn % 64 != 0 || p.Nout % 256 != 0) return hipErrorNotSupported;
             // the two fp32 slices stay with the stream: at most 2 GiB of them
             const size_t bytes = 2 * (size_t)p.M * (size_t)p.Nout * sizeof(float);
             if (bytes > ((size_t)2 << 30)) return hipErrorNotSupported;
@@ -317,7 +319,7 @@ hipError_t launch_permuted(const GemmPass &p, hipStream_t s) {
     if constexpr ((D < 8 && !odd_residues<D>()) || (D >= 8 && 64 % D != 0) || (!IN_T && !OUT_T)) {
         return hipErrorNotSupported;
     } else {
-        if (p.bk % kStageK != 0 || p.Nout % 8 != 0) return hipErrorNotSupported;
+        if (p.plan || p.bk % kStageK != 0 || p.Nout % 8 != 0) return hipErrorNotSupported;
         // up to 1024 tokens, 128-token tiles: twice the workgroups, the weights
         // read twice; 128 x 128 where 128 x 256 would not give every CU a tile
         // (1.2x at 256 and 512 tokens, wide layer fc2 forward / fc1 input

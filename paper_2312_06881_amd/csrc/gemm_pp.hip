@@ -102,7 +102,7 @@ hipError_t launch_interleave(const uint16_t *in, uint16_t *out, int64_t M, int64
 
 hipError_t launch_permuted_pp(const GemmPass &p, hipStream_t s) {
     const PPPlan pl = pp_plan(p);
-    if (!pl.form) return hipErrorNotSupported;
+    if (!pl.form || p.plan) return hipErrorNotSupported;
     const int D = (int)p.D;
     const bool res = pl.form == kPPRes, slices = pl.form == kPPSlice;
     const int64_t mc = pl.chunk;

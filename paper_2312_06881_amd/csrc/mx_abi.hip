@@ -34,20 +34,38 @@ static int64_t chunk_tokens(int64_t n, int64_t M, int dtype) {
     return M < c ? M : c;
 }
 
-// Bytes of the copy in front of the inner call's own workspace.
-static size_t kept_bytes(int pass, int64_t n_in, int64_t n_out, int64_t M, int dtype) {
-    if (pass == DYAD_MX8_DW) return round256((size_t)M * (size_t)n_in * elem(dtype));
-    const int64_t n = pass == DYAD_MX8_FORWARD ? n_out : n_in;
-    return round256((size_t)chunk_tokens(n, M, dtype) * (size_t)n * elem(dtype));
+// A pass whose pre-activation is kept in 8 bits, but for its operands.
+static GemmPass h8_pass(int pass, int variant, int64_t n_in, int64_t n_out, int64_t n_dyad, int64_t M, int dtype) {
+    const bool fwd = pass == DYAD_MX8_FORWARD;
+    GemmPass p{};
+    p.M = M; p.D = n_dyad; p.dtype = dtype;
+    p.Kin = fwd ? n_in : n_out; p.Nout = fwd ? n_out : n_in;
+    p.bk = block(p.Kin, n_dyad); p.bn = block(p.Nout, n_dyad);
+    p.in_t = fwd ? in_transposed(variant) : out_transposed(variant);
+    p.out_t = fwd ? out_transposed(variant) : in_transposed(variant);
+    p.w_t = !fwd;
+    p.epilogue = fwd ? dyad::kEpiBiasGelu : dyad::kEpiGeluGrad;
+    return p;
 }
 
 // A pass on the kernels that take its pre-activation in 8 bits.
 static hipError_t run_h8(const GemmPass &p, hipStream_t s) {
     if (p.dtype != DYAD_BF16 || p.Nout % 32 != 0 || p.Nout != p.D * p.bn) return hipErrorNotSupported;
     const dyad::WorkspaceHold hold;
-    hipError_t e = dyad::skinny_ok(p) ? dyad::launch_skinny_gemm(p, s) : hipErrorNotSupported;
+    hipError_t e = !p.plan && dyad::skinny_ok(p) ? dyad::launch_skinny_gemm(p, s) : hipErrorNotSupported;
     if (e == hipErrorNotSupported) e = dyad::launch_mfma_gemm(p, s);
     return e;
+}
+
+// Bytes of the copy in front of the inner call's own workspace: none where an
+// epilogue does its work whatever else there is no memory for (so also while a
+// graph is captured on a stream that no call has warmed up).
+static size_t kept_bytes(int pass, int variant, int64_t n_in, int64_t n_out, int64_t n_dyad, int64_t M, int dtype) {
+    if (pass == DYAD_MX8_DW) return round256((size_t)M * (size_t)n_in * elem(dtype));
+    GemmPass p = h8_pass(pass, variant, n_in, n_out, n_dyad, M, dtype);
+    p.plan = true;
+    if (M == 0 || run_h8(p, nullptr) == hipSuccess) return 0;
+    return round256((size_t)chunk_tokens(p.Nout, M, dtype) * (size_t)p.Nout * elem(dtype));
 }
 
 static const void *rows(const void *p, int64_t m, int64_t n, size_t e) { return static_cast<const char *>(p) + (size_t)m * (size_t)n * e; }
@@ -132,7 +150,7 @@ size_t dyad_mx8_workspace_bytes(dyad_mx8_pass pass_arg, dyad_variant variant, in
     if (check_sizes(enum_value(variant), n_in, n_out, n_dyad, M, dtype)) return 0;
     if (pass != DYAD_MX8_FORWARD && pass != DYAD_MX8_DX && pass != DYAD_MX8_DW) return 0;
     if (act != DYAD_ACT_NONE && act != DYAD_ACT_GELU) return 0;
-    const size_t kept = kept_bytes(pass, n_in, n_out, M, dtype);
+    const size_t kept = kept_bytes(pass, enum_value(variant), n_in, n_out, n_dyad, M, dtype);
     if (pass != DYAD_MX8_DW) return kept;
     return kept + dyad_dw_workspace_bytes(variant, n_in, n_out, n_dyad, M, dtype_arg);
 }
@@ -150,13 +168,11 @@ int dyad_forward_mx8(dyad_variant variant_arg, int64_t n_in, int64_t n_out, int6
     if (M == 0) return DYAD_OK;
     const size_t need = dyad_mx8_workspace_bytes(DYAD_MX8_FORWARD, variant_arg, n_in, n_out, n_dyad, M, dtype_arg, DYAD_ACT_NONE);
     if (need > 0 && (!workspace || workspace_bytes < need)) return DYAD_ERR_WORKSPACE;
-    GemmPass p{};
-    p.M = M; p.Kin = n_in; p.Nout = n_out; p.D = n_dyad; p.bk = block(n_in, n_dyad); p.bn = block(n_out, n_dyad);
-    p.in_t = in_transposed(variant); p.out_t = out_transposed(variant); p.dtype = dtype; p.epilogue = dyad::kEpiBiasGelu;
+    GemmPass p = h8_pass(DYAD_MX8_FORWARD, variant, n_in, n_out, n_dyad, M, dtype);
     p.in = X; p.W1 = W1; p.W2 = W2; p.bias = bias; p.out = Y;
     p.h8 = static_cast<uint8_t *>(H8); p.hs = static_cast<uint8_t *>(Hs);
     const hipError_t e = run_h8(p, stream);
-    if (e != hipErrorNotSupported) return launch_status(e);
+    if (e != hipErrorNotSupported || need == 0) return launch_status(e);
     const int64_t chunk = chunk_tokens(n_out, M, dtype);
     for (int64_t m = 0; m < M; m += chunk) {
         const int64_t c = M - m < chunk ? M - m : chunk;
@@ -190,15 +206,12 @@ int dyad_backward_dx_mx8(dyad_variant variant_arg, int64_t n_in, int64_t n_out, 
     if (M == 0) return DYAD_OK;
     const size_t need = dyad_mx8_workspace_bytes(DYAD_MX8_DX, variant_arg, n_in, n_out, n_dyad, M, dtype_arg, DYAD_ACT_NONE);
     if (need > 0 && (!workspace || workspace_bytes < need)) return DYAD_ERR_WORKSPACE;
-    GemmPass p{};
-    p.M = M; p.Kin = n_out; p.Nout = n_in; p.D = n_dyad; p.bk = block(n_out, n_dyad); p.bn = block(n_in, n_dyad);
-    p.in_t = out_transposed(variant); p.out_t = in_transposed(variant); p.w_t = true; p.dtype = dtype;
-    p.epilogue = dyad::kEpiGeluGrad;
+    GemmPass p = h8_pass(DYAD_MX8_DX, variant, n_in, n_out, n_dyad, M, dtype);
     p.in = dZ; p.W1 = W1; p.W2 = W2; p.out = dX;
     p.h8 = static_cast<uint8_t *>(const_cast<void *>(H8)); p.hs = static_cast<uint8_t *>(const_cast<void *>(Hs));
     p.a_out = A;
     const hipError_t e = run_h8(p, stream);
-    if (e != hipErrorNotSupported) return launch_status(e);
+    if (e != hipErrorNotSupported || need == 0) return launch_status(e);
     const int64_t chunk = chunk_tokens(n_in, M, dtype);
     for (int64_t m = 0; m < M; m += chunk) {
         const int64_t c = M - m < chunk ? M - m : chunk;
@@ -229,7 +242,7 @@ int dyad_backward_dw_mx8(dyad_variant variant_arg, int64_t n_in, int64_t n_out, 
         return DYAD_ERR_ALIGN;
     const size_t need = dyad_mx8_workspace_bytes(DYAD_MX8_DW, variant_arg, n_in, n_out, n_dyad, M, dtype_arg, act_in_arg);
     if (need > 0 && (!workspace || workspace_bytes < need)) return DYAD_ERR_WORKSPACE;
-    const size_t kept = kept_bytes(DYAD_MX8_DW, n_in, n_out, M, dtype);
+    const size_t kept = kept_bytes(DYAD_MX8_DW, variant, n_in, n_out, n_dyad, M, dtype);
     if (M > 0) {
         const hipError_t e =
             dyad::launch_mx_dequantize(DYAD_MX_INT8, M, n_in, dtype, X8, Xs, act_in == DYAD_ACT_GELU, workspace, stream);
