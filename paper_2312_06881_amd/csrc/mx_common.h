@@ -57,13 +57,12 @@ __device__ __forceinline__ float mx_int8_step(uint32_t s) {
     return s == 255u ? __uint_as_float(0x7fc00000u) : ldexpf(1.f, (int)s - 133);
 }
 
-// Values of four codes.  The bytes become unsigned (code + 128), which convert
-// in one instruction; the 128 goes off before the step comes on, where the
-// largest blocks (127 * 2^121) stay finite, as 128 * 2^121 does not.  Both are exact.
+// Values of four codes, each a signed byte converted in place (one instruction)
+// and multiplied, exactly.  (An offset taken off after the step would leave
+// fp32's range in the largest blocks, 128 * 2^121.)
 __device__ __forceinline__ void mx_int8_values(uint32_t codes, float step, float (&x)[4]) {
-    const uint32_t u = codes ^ 0x80808080u;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = ((float)((u >> (8 * e)) & 255u) - 128.f) * step;
+    for (int e = 0; e < 4; ++e) x[e] = (float)(int8_t)(codes >> (8 * e)) * step;
 }
 
 // Eight codes as packed bf16, which holds each exactly.
