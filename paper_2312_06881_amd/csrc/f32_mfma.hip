@@ -371,21 +371,21 @@ __global__ void __launch_bounds__(kFThreads, 2) f32_dw_kernel(DwPass p, int jt_n
 struct FTile {
     int index;
     int64_t rows, cols, count;
-    // f(m, n); MIXED: 128 x 64 is among the sizes.
-    template <bool MIXED, class F> void with(F f) const {
+    // f(m, n); DW: 64 x 128 is among the sizes.
+    template <bool DW, class F> void with(F f) const {
         switch (index) {
         case 0: return f(std::integral_constant<int, 128>{}, std::integral_constant<int, 128>{});
-        case 1:
-            if constexpr (MIXED) f(std::integral_constant<int, 128>{}, std::integral_constant<int, 64>{});
-            return;
+        case 1: return f(std::integral_constant<int, 128>{}, std::integral_constant<int, 64>{});
         case 2: return f(std::integral_constant<int, 64>{}, std::integral_constant<int, 64>{});
         case 3: return f(std::integral_constant<int, 64>{}, std::integral_constant<int, 32>{});
-        default: return f(std::integral_constant<int, 32>{}, std::integral_constant<int, 32>{});
+        case 4: return f(std::integral_constant<int, 32>{}, std::integral_constant<int, 32>{});
+        default:
+            if constexpr (DW) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 128>{});
         }
     }
 };
 constexpr int kTiles = 5;
-constexpr int kTileM[kTiles] = {128, 128, 64, 64, 32}, kTileN[kTiles] = {128, 64, 64, 32, 32};
+constexpr int kTileM[kTiles + 1] = {128, 128, 64, 64, 32, 64}, kTileN[kTiles + 1] = {128, 64, 64, 32, 32, 128};
 
 FTile tile_at(int index, int64_t each, int64_t m, int64_t n) {
     const int64_t rt = (m + kTileM[index] - 1) / kTileM[index], ct = (n + kTileN[index] - 1) / kTileN[index];
@@ -401,13 +401,29 @@ FTile tile_at(int index, int64_t each, int64_t m, int64_t n) {
 //                                           forward pass    168, 107, 98, 102, 103
 //   768 -> 3072, n_dyad 4, IT, 4096 tokens: forward pass    96, 102, 96, 111, 112
 // wide: no more than 128 x 64, whose sums in 64 bits stay in registers.
-FTile gemm_tile(int64_t each, int64_t m, int64_t n, bool wide) {
+// Rows of the input that an input transpose gathers value by value, n_dyad apart,
+// are loaded again by every narrower tile, more lines for it the larger n_dyad is.
+// So without an output transpose the largest tile stays, where it pads nothing
+// more than 64 x 64 and fills a round over the CUs, from n_dyad 8 in the forward
+// pass and 32 in both (from there also more rounds, the last half full).
+// Measured on 128 x 128 and on what the time above picks (us):
+//   forward pass, 8192 -> 2048, n_dyad 8, 2048 tokens      201, 221
+//                 16384 -> 4096, n_dyad 32, 1024 tokens    141, 173
+//   input gradient, 16384 -> 4096, n_dyad 32, 1100 tokens  158, 180
+//                 8192 -> 2048, n_dyad 8, 512 tokens        64, 61
+FTile gemm_tile(const GemmPass &p, int64_t each, int64_t n) {
     constexpr double per_value[kTiles] = {1., 1., 1.05, 1.2, 1.3};
+    const FTile large = tile_at(0, each, p.M, n);
+    const bool even = (p.M + 63) / 64 % 2 == 0 && (n + 63) / 64 % 2 == 0;
+    if (p.in_t && !p.out_t && even && !p.wide_sums && p.D >= (p.w_t ? 32 : 8)) {
+        const bool last_half = (large.count - 1) % 256 >= 127;
+        if ((large.count > 224 && large.count <= 256) || (p.D >= 32 && large.count > 256 && last_half)) return large;
+    }
     FTile best{};
     double least = 0;
-    const int from = wide ? 1 : 0;
+    const int from = p.wide_sums ? 1 : 0;
     for (int i = from; i < kTiles; ++i) {
-        const FTile t = tile_at(i, each, m, n);
+        const FTile t = tile_at(i, each, p.M, n);
         const double one = 0.85 / 8192 * kTileM[i] * kTileN[i], k = (double)((t.count + 255) / 256);
         const double busy = k * one * per_value[i], cost = busy > 0.45 + one ? busy : 0.45 + one;
         if (i == from || cost < least) { best = t; least = cost; }
@@ -423,9 +439,19 @@ FTile gemm_tile(int64_t each, int64_t m, int64_t n, bool wide) {
 //   1024 -> 4096, n_dyad 4, DT, 640 tokens (128)               79, 47, 61, 84
 //   768 -> 3072, n_dyad 4, IT, 4096 tokens (pads 192 to 256)   164, 119, 125, 144
 //   1024 -> 1024, n_dyad 4, OT, 500 tokens (32)                54, 22, 17, 15
-FTile dw_tile(int64_t each, int64_t m, int64_t n) {
+// From n_dyad 32 a gathered value is a cache line of its own, which every tile
+// that needs it loads: the widest tile of either side that pads nothing more,
+// from 192 of them (2048 -> 8192, n_dyad 32, IT, 2048 tokens, 512 tiles of 128 x
+// 64: 85 us, of 64 x 64 146; DT, 4096 tokens 241 and 313; 4096 -> 4096, DT, 1536
+// tokens, 192 tiles of 128 x 128 155, of 64 x 64 205; 2048 -> 8192, OT, 512 tokens,
+// 128 tiles of 128 x 64 67, of 64 x 64 44).
+FTile dw_tile(int64_t D, int64_t each, int64_t m, int64_t n) {
+    const bool even_m = (m + 63) / 64 % 2 == 0, even_n = (n + 63) / 64 % 2 == 0;
     const FTile large = tile_at(0, each, m, n);
-    if ((m + 63) / 64 % 2 == 0 && (n + 63) / 64 % 2 == 0 && large.count >= 256) return large;
+    const int64_t enough = D >= 32 ? 192 : 256;
+    if (even_m && even_n && large.count >= enough) return large;
+    if (D >= 32 && even_m != even_n)
+        if (const FTile t = tile_at(even_m ? 1 : kTiles, each, m, n); t.count >= enough) return t;
     for (int i = 2; i < kTiles - 1; ++i)
         if (const FTile t = tile_at(i, each, m, n); t.count >= 256) return t;
     return tile_at(kTiles - 1, each, m, n);
@@ -446,13 +472,13 @@ hipError_t launch_f32_gemm(const GemmPass &p, hipStream_t s) {
     if (128 * p.Kin * 4 >= lim || 32 * p.bn * 4 >= lim || 128 * p.D * p.bk * 4 >= lim) return hipErrorNotSupported;
     const int64_t classes = p.out_t ? p.D * p.D : p.D;
     const int64_t per_class = p.out_t ? (p.bn + p.D - 1) / p.D : p.bn;
-    const FTile tile = gemm_tile(classes, p.M, per_class, p.wide_sums);
+    const FTile tile = gemm_tile(p, classes, per_class);
     if (tile.count >= ((int64_t)1 << 31)) return hipErrorNotSupported;
     auto go = [&](auto in_t, auto out_t, auto w_t) {
         constexpr bool I = decltype(in_t)::value, O = decltype(out_t)::value, W = decltype(w_t)::value;
         const unsigned n = (unsigned)tile.count;
         const int ct = (int)tile.cols;
-        tile.with<true>([&](auto bm, auto bn) {
+        tile.with<false>([&](auto bm, auto bn) {
             constexpr int BM = decltype(bm)::value, BN = decltype(bn)::value;
             constexpr bool wide = !W && BN < 128;
             if (wide && p.wide_sums) f32_gemm_kernel<BM, BN, I, O, W, wide><<<n, kFThreads, 0, s>>>(p, ct);
@@ -471,12 +497,12 @@ hipError_t launch_f32_gemm(const GemmPass &p, hipStream_t s) {
 hipError_t launch_f32_dw_tiles(const DwPass &p, int64_t splits, int64_t tps, float *part, hipStream_t s) {
     if (p.dtype != kF32 || !f32_mfma_ok(p.n_in, p.n_out, p.D, p.bi, p.bo)) return hipErrorNotSupported;
     if (32 * (p.n_in > p.n_out ? p.n_in : p.n_out) * 4 >= (int64_t)1 << 31) return hipErrorNotSupported;
-    const FTile tile = dw_tile(splits * 2 * p.D, p.bo, p.bi);
+    const FTile tile = dw_tile(p.D, splits * 2 * p.D, p.bo, p.bi);
     if (tile.count >= ((int64_t)1 << 31)) return hipErrorNotSupported;
     const unsigned n = (unsigned)tile.count;
     auto go = [&](auto in_t, auto out_t) {
         constexpr bool I = decltype(in_t)::value, O = decltype(out_t)::value;
-        tile.with<false>([&](auto bj, auto bk) {
+        tile.with<true>([&](auto bj, auto bk) {
             f32_dw_kernel<decltype(bj)::value, decltype(bk)::value, I, O><<<n, kFThreads, 0, s>>>(
                 p, (int)tile.rows, (int)tile.cols, (int)splits, tps, part);
         });
