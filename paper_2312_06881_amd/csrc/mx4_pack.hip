@@ -6,7 +6,9 @@
 // LDS, from which the contiguous blocks and the residues k*D + g are taken.
 // The lanes of a wave write 1 KB of a fragment in a row.  What bounds it is that
 // traffic: 8192 tokens of 4096 in both orders, 25 us (4.1 TB/s), where one wave a
-// fragment that loads its values itself took 162.
+// fragment that loads its values itself took 162.  The weights, once for a model, do
+// that all the same: 4096 -> 16384, n_dyad 4, 75 us (1.1 TB/s), 183 in the order of
+// residues.
 #include "mx_common.h"
 
 namespace dyad {
