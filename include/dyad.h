@@ -84,7 +84,7 @@ typedef enum { DYAD_ACT_NONE = 0, DYAD_ACT_GELU = 1 } dyad_act; /* GELU(x) = x *
 typedef enum {
     DYAD_OK = 0,
     DYAD_ERR_INVALID_ARG = -1, /* unknown enum, size < 0 (M) or <= 0 (n_in, n_out, n_dyad), size overflow, NULL required pointer */
-    DYAD_ERR_SHAPE = -2,       /* only the _ex calls with an input activation and dyad_mx4_forward: no kernel for this shape */
+    DYAD_ERR_SHAPE = -2,       /* the _ex calls with an input activation, dyad_mx4_forward, dyad_add_norm_* and dyad_linear_ce_*: no kernel for this shape */
     DYAD_ERR_ALIGN = -3,       /* a non-NULL pointer is not 16-byte aligned */
     DYAD_ERR_DTYPE = -4,       /* unknown dtype */
     DYAD_ERR_WORKSPACE = -5,   /* a workspace (or the packed weights) NULL or smaller than its _bytes() call says */
@@ -278,6 +278,108 @@ int dyad_backward_dx_mx8(dyad_variant variant, int64_t n_in, int64_t n_out, int6
 int dyad_backward_dw_mx8(dyad_variant variant, int64_t n_in, int64_t n_out, int64_t n_dyad, int64_t M,
                          dyad_dtype dtype, dyad_act act_in, const void *dZ, const void *X8, const void *Xs, void *dW1,
                          void *dW2, void *dbias, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * ---- Around the Dyad layers of a language model --------------------------------
+ *
+ * Dropout, the residual stream with its norms, and the loss over a vocabulary.  The
+ * calls only enqueue work on `stream`, allocate nothing, overwrite their outputs, and
+ * check every argument before any HIP call; every non-NULL pointer is 16-byte
+ * aligned (offset_dev: 8); sums are fp32 and results are rounded once, and repeat bit by bit.
+ *
+ * Dropout draws its mask from a counter, so that none is stored: of a matrix of
+ * `cols` columns, value j of octet o = row * ceil(cols / 8) + col / 8 (j = col % 8)
+ * has bits 16 (j % 2) .. + 15 of word j / 2 of Philox-4x32-10 at the counter
+ * (o, offset) and the key seed, 64 bits each, low words first.  It is dropped where
+ * they are below t = rint(65536 p); the others are scaled by 65536 / (65536 - t).
+ * (p is so a multiple of 2^-16, and the scale goes with what is dropped; p == 1
+ * drops everything.)  What is dropped becomes 0 whatever it was.  offset_dev, when
+ * not NULL, is a value in device memory that is added to offset: a captured call
+ * draws another mask at every replay if the program changes it in between.
+ */
+
+/* Y = X dropped and scaled; the gradient is the same call on dY.  Y may be X. */
+int dyad_dropout(int64_t rows, int64_t cols, dyad_dtype dtype, const void *X, double p, uint64_t seed, uint64_t offset,
+                 const uint64_t *offset_dev, void *Y, hipStream_t stream);
+
+/*
+ *   h   = x_scale x + y_scale gate * drop(post(y))
+ *   out = norm(h)
+ * x is the residual stream [M][n], y a block's output; out is the next block's input.
+ * LAYER: norm(v) = (v - mean) / sqrt(mean((v - mean)^2) + eps) weight + bias over a
+ * row, RMS: v / sqrt(mean(v^2) + eps) weight + bias.  8 <= n <= 16384, else
+ * DYAD_ERR_SHAPE.
+ *
+ * x and h have stream_dtype, y and out dtype: both bf16, both fp32, or an fp32 stream
+ * with bf16 blocks (else DYAD_ERR_DTYPE).  The parameters (weights, biases, gate) have
+ * param_dtype, fp32 or, with bf16 blocks, bf16.  out is the norm of h before it is
+ * rounded.
+ *
+ * May be NULL: y (then h = x_scale x, and post, gate and p have no effect); h; weight,
+ * bias, post_weight, post_bias (1 and 0); gate (1); stats and post_stats, which a
+ * backward pass needs.  gate is [groups][n]: row m takes gate row m / (M / groups), and
+ * groups divides M.  norm == NONE: out is not written.  h may be x, and out y where
+ * their types agree.
+ */
+typedef enum { DYAD_NORM_NONE = 0, DYAD_NORM_LAYER = 1, DYAD_NORM_RMS = 2 } dyad_norm;
+typedef struct {
+    int64_t M, n, groups;
+    dyad_dtype stream_dtype, dtype, param_dtype;
+    dyad_norm norm, post;
+    float x_scale, y_scale, eps;
+    double p;                    /* dropout of post(y); 0: none */
+    uint64_t seed, offset;
+    const uint64_t *offset_dev;
+    const void *x, *y, *weight, *bias, *post_weight, *post_bias, *gate;
+    void *h, *out;
+    float *stats, *post_stats;   /* [M][2]: mean and 1 / sqrt(...) of h's rows, and of y's */
+} dyad_add_norm_args;
+int dyad_add_norm_forward(const dyad_add_norm_args *args, hipStream_t stream);
+
+/*
+ * The gradients.  args is the forward call's, with what it wrote: h (read; x where y
+ * was NULL and x_scale 1), stats (with a norm) and post_stats (with a post norm); x
+ * and out are not read.  dh is the gradient that reaches h, dout that which reaches
+ * out; either may be NULL (none).  Of the results any may be NULL: dx [M][n] of
+ * stream_dtype, dy [M][n] of dtype, those of the parameters (of param_dtype), dgate
+ * [groups][n].  dx may be dh, and dy dout where their types agree.  The workspace holds
+ * dyad_add_norm_workspace_bytes() bytes for the same arguments (0 for invalid ones).
+ * M == 0 gives zero gradients of the parameters.
+ */
+typedef struct {
+    const void *dh, *dout;
+    void *dx, *dy, *dweight, *dbias, *dpost_weight, *dpost_bias, *dgate;
+} dyad_add_norm_grads;
+size_t dyad_add_norm_workspace_bytes(const dyad_add_norm_args *args, const dyad_add_norm_grads *grads);
+int dyad_add_norm_backward(const dyad_add_norm_args *args, const dyad_add_norm_grads *grads, void *workspace,
+                           size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Softmax cross entropy of the logits Z = X W^T, which are never kept: X [M][n] the
+ * tokens, W [V][n] the vocabulary's rows.  A token's loss is log(sum_v exp Z[m][v]) -
+ * Z[m][target]; a target that is ignore_index, or lies outside 0 .. V - 1, counts for
+ * nothing: loss 0, no gradient.  reduction NONE: loss [M]; SUM, MEAN over the tokens
+ * that count (0 where none does): loss [1].  lse [M] and, for MEAN, count [1] (the
+ * tokens that count) are what the backward pass needs of the forward one.
+ *
+ * Backward: dloss, of loss's length, is the gradient that reaches it; dX [M][n] and
+ * dW [V][n], either of which may be NULL, are the gradients.  The logits are formed
+ * again, a piece of the vocabulary at a time; their gradient is rounded to dtype
+ * where it enters the products with W and X, whose sums are fp32.
+ *
+ * M, V <= 2^22 and n <= 2^20, else DYAD_ERR_SHAPE.  The workspace holds
+ * dyad_linear_ce_workspace_bytes() bytes for the pass (0 for invalid arguments).
+ */
+typedef enum { DYAD_REDUCE_NONE = 0, DYAD_REDUCE_SUM = 1, DYAD_REDUCE_MEAN = 2 } dyad_reduction;
+typedef enum { DYAD_CE_FORWARD = 0, DYAD_CE_BACKWARD = 1 } dyad_ce_pass;
+size_t dyad_linear_ce_workspace_bytes(dyad_ce_pass pass, int64_t M, int64_t n, int64_t V, dyad_dtype dtype);
+int dyad_linear_ce_forward(int64_t M, int64_t n, int64_t V, dyad_dtype dtype, const void *X, const void *W,
+                           const int64_t *targets, int64_t ignore_index, dyad_reduction reduction, float *loss,
+                           float *lse, float *count, void *workspace, size_t workspace_bytes, hipStream_t stream);
+int dyad_linear_ce_backward(int64_t M, int64_t n, int64_t V, dyad_dtype dtype, const void *X, const void *W,
+                            const int64_t *targets, int64_t ignore_index, dyad_reduction reduction, const float *lse,
+                            const float *count, const float *dloss, void *dX, void *dW, void *workspace,
+                            size_t workspace_bytes, hipStream_t stream);
 
 /* Static, human-readable text for a dyad_status value. */
 const char *dyad_strerror(int status);

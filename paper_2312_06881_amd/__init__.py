@@ -11,7 +11,8 @@ Two levels:
   * ``forward``, ``backward_dx``, ``backward_dw``: tensor-level helpers that
     allocate outputs with torch on the inputs' device, call the C-ABI on
     torch's current stream, and raise ``DyadError`` on a non-zero status.
-    Those of the microscaled formats are in ``mx``.
+    Those of the microscaled formats are in ``mx``, those of dropout, the residual
+    stream's norms and the loss in ``lm``.
 
 There is no CPU fallback: if ``libdyad.so`` is missing or fails to load, every
 call raises.
@@ -31,6 +32,9 @@ __all__ = [
     "MX_INT8", "MX_FP4", "MX8_FORWARD", "MX8_DX", "MX8_DW", "dyad_mx_quantize", "dyad_mx_dequantize",
     "dyad_mx4_weight_bytes", "dyad_mx4_quantize_weights", "dyad_mx4_workspace_bytes", "dyad_mx4_forward",
     "dyad_mx8_workspace_bytes", "dyad_forward_mx8", "dyad_backward_dx_mx8", "dyad_backward_dw_mx8",
+    "NORM_NONE", "NORM_LAYER", "NORM_RMS", "REDUCE_NONE", "REDUCE_SUM", "REDUCE_MEAN", "CE_FORWARD", "CE_BACKWARD",
+    "AddNormArgs", "AddNormGrads", "dyad_dropout", "dyad_add_norm_forward", "dyad_add_norm_workspace_bytes",
+    "dyad_add_norm_backward", "dyad_linear_ce_workspace_bytes", "dyad_linear_ce_forward", "dyad_linear_ce_backward",
 ]
 
 IT, OT, DT = 0, 1, 2
@@ -38,6 +42,9 @@ F32, BF16 = 0, 1
 ACT_NONE, ACT_GELU = 0, 1
 MX_INT8, MX_FP4 = 0, 1
 MX8_FORWARD, MX8_DX, MX8_DW = 0, 1, 2
+NORM_NONE, NORM_LAYER, NORM_RMS = 0, 1, 2
+REDUCE_NONE, REDUCE_SUM, REDUCE_MEAN = 0, 1, 2
+CE_FORWARD, CE_BACKWARD = 0, 1
 VARIANTS = {"IT": IT, "OT": OT, "DT": DT}
 ACTS = {"none": ACT_NONE, "gelu": ACT_GELU}
 STATUS = {0: "DYAD_OK", -1: "DYAD_ERR_INVALID_ARG", -2: "DYAD_ERR_SHAPE", -3: "DYAD_ERR_ALIGN",
@@ -50,6 +57,22 @@ _lib = None
 _i64 = ctypes.c_int64
 _vp = ctypes.c_void_p
 _int = ctypes.c_int
+_u64 = ctypes.c_uint64
+
+
+class AddNormArgs(ctypes.Structure):
+    """``dyad_add_norm_args``."""
+    _fields_ = ([(n, _i64) for n in ("M", "n", "groups")] +
+                [(n, _int) for n in ("stream_dtype", "dtype", "param_dtype", "norm", "post")] +
+                [(n, ctypes.c_float) for n in ("x_scale", "y_scale", "eps")] + [("p", ctypes.c_double)] +
+                [(n, _u64) for n in ("seed", "offset")] +
+                [(n, _vp) for n in ("offset_dev", "x", "y", "weight", "bias", "post_weight", "post_bias", "gate", "h",
+                                    "out", "stats", "post_stats")])
+
+
+class AddNormGrads(ctypes.Structure):
+    """``dyad_add_norm_grads``."""
+    _fields_ = [(n, _vp) for n in ("dh", "dout", "dx", "dy", "dweight", "dbias", "dpost_weight", "dpost_bias", "dgate")]
 
 
 class DyadError(RuntimeError):
@@ -102,7 +125,15 @@ def _load():
             ("dyad_mx8_workspace_bytes", size, [_int, _int, _i64, _i64, _i64, _i64, _int, _int]),
             ("dyad_forward_mx8", _int, [_int, _i64, _i64, _i64, _i64, _int, *[_vp] * 8, size, _vp]),
             ("dyad_backward_dx_mx8", _int, [_int, _i64, _i64, _i64, _i64, _int, *[_vp] * 8, size, _vp]),
-            ("dyad_backward_dw_mx8", _int, [_int, _i64, _i64, _i64, _i64, _int, _int, *[_vp] * 7, size, _vp])):
+            ("dyad_backward_dw_mx8", _int, [_int, _i64, _i64, _i64, _i64, _int, _int, *[_vp] * 7, size, _vp]),
+            ("dyad_dropout", _int, [_i64, _i64, _int, _vp, ctypes.c_double, _u64, _u64, _vp, _vp, _vp]),
+            ("dyad_add_norm_forward", _int, [_vp, _vp]),
+            ("dyad_add_norm_workspace_bytes", size, [_vp, _vp]),
+            ("dyad_add_norm_backward", _int, [_vp, _vp, _vp, size, _vp]),
+            ("dyad_linear_ce_workspace_bytes", size, [_int, _i64, _i64, _i64, _int]),
+            ("dyad_linear_ce_forward", _int, [_i64, _i64, _i64, _int, _vp, _vp, _vp, _i64, _int, *[_vp] * 4, size, _vp]),
+            ("dyad_linear_ce_backward", _int,
+             [_i64, _i64, _i64, _int, _vp, _vp, _vp, _i64, _int, *[_vp] * 6, size, _vp])):
         fn = getattr(lib, name)
         fn.restype, fn.argtypes = restype, args
     lib.dyad_strerror.restype = ctypes.c_char_p
@@ -203,6 +234,42 @@ def dyad_backward_dw_mx8(variant, n_in, n_out, n_dyad, M, dtype, act_in, dZ, X8,
                          workspace_bytes, stream) -> int:
     return _load().dyad_backward_dw_mx8(variant, n_in, n_out, n_dyad, M, dtype, act_in, dZ, X8, Xs, dW1, dW2, dbias,
                                         workspace, workspace_bytes, stream)
+
+
+def dyad_dropout(rows, cols, dtype, X, p, seed, offset, offset_dev, Y, stream) -> int:
+    return _load().dyad_dropout(rows, cols, dtype, X, p, seed, offset, offset_dev, Y, stream)
+
+
+def _ref(s):
+    return None if s is None else ctypes.addressof(s)
+
+
+def dyad_add_norm_forward(args, stream) -> int:
+    return _load().dyad_add_norm_forward(_ref(args), stream)
+
+
+def dyad_add_norm_workspace_bytes(args, grads) -> int:
+    return _load().dyad_add_norm_workspace_bytes(_ref(args), _ref(grads))
+
+
+def dyad_add_norm_backward(args, grads, workspace, workspace_bytes, stream) -> int:
+    return _load().dyad_add_norm_backward(_ref(args), _ref(grads), workspace, workspace_bytes, stream)
+
+
+def dyad_linear_ce_workspace_bytes(pass_, M, n, V, dtype) -> int:
+    return _load().dyad_linear_ce_workspace_bytes(pass_, M, n, V, dtype)
+
+
+def dyad_linear_ce_forward(M, n, V, dtype, X, W, targets, ignore_index, reduction, loss, lse, count, workspace,
+                           workspace_bytes, stream) -> int:
+    return _load().dyad_linear_ce_forward(M, n, V, dtype, X, W, targets, ignore_index, reduction, loss, lse, count,
+                                          workspace, workspace_bytes, stream)
+
+
+def dyad_linear_ce_backward(M, n, V, dtype, X, W, targets, ignore_index, reduction, lse, count, dloss, dX, dW,
+                            workspace, workspace_bytes, stream) -> int:
+    return _load().dyad_linear_ce_backward(M, n, V, dtype, X, W, targets, ignore_index, reduction, lse, count, dloss,
+                                           dX, dW, workspace, workspace_bytes, stream)
 
 
 def dyad_strerror(status: int) -> str:

@@ -1,0 +1,573 @@
+// h = x_scale x + y_scale gate * drop(post(y)),  out = norm(h): a block's output joins the
+// residual stream, and the next block's input is normed, in one pass over the rows; and the
+// gradients.  Everything is memory traffic: each operand is read once, each result written
+// once, and a row lives in registers between the sums over it.
+//
+// norm(v) = (v - mean) r w + b with r = 1 / sqrt(mean((v - mean)^2) + eps) (layer), or
+// v r w + b with r = 1 / sqrt(mean(v^2) + eps) (rms).  Sums are fp32, the mean taken out
+// before squaring.  out is the norm of the fp32 sum h, not of h as rounded to the stream's
+// type: one rounding fewer, and no dependence of out on that type.
+//
+// Backward, with u = (h - mean) r and d = dout w:
+//   g    = dh + r (d - mean(d) - u mean(d u))      (rms: without mean(d))
+//   dx   = x_scale g
+//   dz   = y_scale g gate, zero where dropped, else scaled;  dgate = sum y_scale g drop(z)
+//   dy   = dz, or through the post norm as above with its own u and d = dz pw
+//   dw   = sum dout u,  db = sum dout;  dpw = sum dz u_y,  dpb = sum dz
+// The sums over rows are kept in registers over a workgroup's rows, written as fp32 partials
+// and added by a second kernel in a fixed order, so results repeat bit by bit.
+//
+// A team of TPR threads takes a row, NV vectors of 8 columns a thread; up to 1024 columns a
+// team is a wave, which needs no barrier.
+#include "lm_internal.h"
+#include "philox.h"
+#include "row_io.h"
+
+namespace dyad {
+
+namespace {
+
+struct Norm {
+    AddNormPass p;
+    DropArgs d;
+    int n, octets, npad;
+    int64_t rows_per_gate;       // M when there is one gate row, or none
+    bool drop;
+    // backward
+    int64_t units, per_group;    // units of rows; those of one gate row
+    int64_t unit_rows;           // rows of a gate row (or M), split into per_group units
+    float *part[4];              // dw, db, dpw, dpb: [workgroups][npad]; null: not wanted
+    float *gpart;                // [units][npad]
+};
+
+constexpr int threads_of(int tpr) { return tpr < 256 ? (tpr == 64 ? 256 : tpr) : tpr; }
+constexpr int teams_of(int tpr) { return threads_of(tpr) / tpr; }
+
+template <bool RAG>
+__device__ __forceinline__ void load_param(const void *base, bool f32, int64_t row, int c, int n, float (&v)[8]) {
+    if (f32) load_cols<RAG>(static_cast<const float *>(base) + row * n, c, n, v);
+    else load_cols<RAG>(static_cast<const uint16_t *>(base) + row * n, c, n, v);
+}
+
+// Sums of a and b over a team, the same bits in each of its threads.
+template <int TPR>
+struct TeamSum {
+    float2 *lds;     // [2][TPR / 64] for teams of several waves
+    int parity;      // of the buffer: a wave is at most one sum ahead of another
+    __device__ __forceinline__ void operator()(float &a, float &b) {
+#pragma unroll
+        for (int m = 32; m > 0; m >>= 1) {
+            a += __shfl_xor(a, m);
+            b += __shfl_xor(b, m);
+        }
+        if constexpr (TPR > 64) {
+            float2 *buf = lds + parity * (TPR / 64);
+            parity ^= 1;
+            if ((threadIdx.x & 63) == 0) buf[threadIdx.x / 64] = make_float2(a, b);
+            __syncthreads();
+            a = b = 0.f;
+#pragma unroll
+            for (int w = 0; w < TPR / 64; ++w) {
+                const float2 t = buf[w];
+                a += t.x;
+                b += t.y;
+            }
+        }
+    }
+};
+
+// Mean (zero for rms) and 1 / deviation of a row held as v[NV][8].
+template <int TPR, int NV>
+__device__ __forceinline__ float2 row_stats(const float (&v)[NV][8], int kind, const Norm &a, int c0, TeamSum<TPR> &sum) {
+    const float inv = 1.f / (float)a.n;
+    float s = 0.f, unused = 0.f, mean = 0.f;
+    if (kind == kNormLayer) {
+#pragma unroll
+        for (int q = 0; q < NV; ++q)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s += v[q][e];      // columns past n hold zero
+        sum(s, unused);
+        mean = s * inv;
+    }
+    s = 0.f;
+#pragma unroll
+    for (int q = 0; q < NV; ++q)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float t = v[q][e] - mean;
+            s += c0 + q * 8 * TPR + e < a.n ? t * t : 0.f;
+        }
+    sum(s, unused);
+    return make_float2(mean, 1.f / sqrtf(s * inv + a.p.eps));
+}
+
+template <class TS, class TB, int TPR, int NV, bool RAG>
+__global__ void __launch_bounds__(threads_of(TPR)) add_norm_kernel(Norm a) {
+    __shared__ float2 lds[TPR > 64 ? 2 * (TPR / 64) : 1];
+    TeamSum<TPR> sum{lds, 0};
+    const int lane = threadIdx.x % TPR, n = a.n, c0 = lane * 8;
+    const bool pf32 = a.p.param_dtype == kF32;
+    const uint64_t offset = a.drop ? drop_offset(a.d) : 0;
+    for (int64_t row = (int64_t)blockIdx.x * teams_of(TPR) + threadIdx.x / TPR; row < a.p.M;
+         row += (int64_t)gridDim.x * teams_of(TPR)) {
+        float h[NV][8];
+        const TS *xr = static_cast<const TS *>(a.p.x) + row * n;
+        float x[NV][8];
+#pragma unroll
+        for (int q = 0; q < NV; ++q) load_cols<RAG>(xr, c0 + q * 8 * TPR, n, x[q]);
+        if (a.p.y) {
+            const TB *yr = static_cast<const TB *>(a.p.y) + row * n;
+#pragma unroll
+            for (int q = 0; q < NV; ++q) load_cols<RAG>(yr, c0 + q * 8 * TPR, n, h[q]);
+            if (a.p.post != kNormNone) {
+                const float2 st = row_stats<TPR, NV>(h, a.p.post, a, c0, sum);
+                if (a.p.post_stats && lane == 0) reinterpret_cast<float2 *>(a.p.post_stats)[row] = st;
+#pragma unroll
+                for (int q = 0; q < NV; ++q) {
+                    float w[8], b[8];
+                    const int c = c0 + q * 8 * TPR;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) h[q][e] = (h[q][e] - st.x) * st.y;
+                    if (a.p.pw) {
+                        load_param<RAG>(a.p.pw, pf32, 0, c, n, w);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) h[q][e] *= w[e];
+                    }
+                    if (a.p.pb) {
+                        load_param<RAG>(a.p.pb, pf32, 0, c, n, b);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) h[q][e] += b[e];
+                    }
+                }
+            }
+            const int64_t grow = a.p.gate && a.p.groups > 1 ? row / a.rows_per_gate : 0;
+#pragma unroll
+            for (int q = 0; q < NV; ++q) {
+                const int c = c0 + q * 8 * TPR;
+                if (a.drop && c < n)
+                    apply_drop(h[q], keep_bits(philox(a.d.seed, offset, (uint64_t)(row * a.octets + (c >> 3))), a.d.thr),
+                               a.d.scale);
+                if (a.p.gate) {
+                    float g[8];
+                    load_param<RAG>(a.p.gate, pf32, grow, c, n, g);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) h[q][e] *= g[e];
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) h[q][e] = c + e < n ? fmaf(h[q][e], a.p.y_scale, x[q][e] * a.p.x_scale) : 0.f;
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < NV; ++q)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) h[q][e] = x[q][e] * a.p.x_scale;
+        }
+        if (a.p.h) {
+            TS *hr = static_cast<TS *>(a.p.h) + row * n;
+#pragma unroll
+            for (int q = 0; q < NV; ++q) store_cols<RAG>(hr, c0 + q * 8 * TPR, n, h[q]);
+        }
+        if (a.p.norm == kNormNone) continue;
+        const float2 st = row_stats<TPR, NV>(h, a.p.norm, a, c0, sum);
+        if (a.p.stats && lane == 0) reinterpret_cast<float2 *>(a.p.stats)[row] = st;
+        TB *o = static_cast<TB *>(a.p.out) + row * n;
+#pragma unroll
+        for (int q = 0; q < NV; ++q) {
+            const int c = c0 + q * 8 * TPR;
+            float w[8], b[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) h[q][e] = (h[q][e] - st.x) * st.y;
+            if (a.p.w) {
+                load_param<RAG>(a.p.w, pf32, 0, c, n, w);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) h[q][e] *= w[e];
+            }
+            if (a.p.b) {
+                load_param<RAG>(a.p.b, pf32, 0, c, n, b);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) h[q][e] += b[e];
+            }
+            store_cols<RAG>(o, c, n, h[q]);
+        }
+    }
+}
+
+// The gradient through a norm: d[q][e] (already times the weight) becomes the gradient of the
+// normed values, u being their unit form.
+template <int TPR, int NV>
+__device__ __forceinline__ void norm_grad(float (&d)[NV][8], const float (&u)[NV][8], float r, int kind, int n,
+                                          TeamSum<TPR> &sum) {
+    float s = 0.f, t = 0.f;
+#pragma unroll
+    for (int q = 0; q < NV; ++q)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            s += d[q][e];
+            t = fmaf(d[q][e], u[q][e], t);
+        }
+    sum(s, t);
+    const float inv = 1.f / (float)n;
+    s = kind == kNormLayer ? s * inv : 0.f;
+    t *= inv;
+#pragma unroll
+    for (int q = 0; q < NV; ++q)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d[q][e] = r * (d[q][e] - s - u[q][e] * t);
+}
+
+// A workgroup's sums of one kind over its teams, in team order, to dst [npad]; clears them.
+template <int TPR, int NV>
+__device__ __forceinline__ void flush(float (&acc)[NV][8], float *dst, int npad, float *buf) {
+    const int lane = threadIdx.x % TPR, team = threadIdx.x / TPR;
+    if constexpr (teams_of(TPR) > 1) {
+        for (int t = 0; t < teams_of(TPR); ++t) {
+            __syncthreads();
+            if (t == team) {
+#pragma unroll
+                for (int q = 0; q < NV; ++q)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        float *b = buf + (q * 8 + e) * TPR + lane;
+                        if (t > 0) acc[q][e] += *b;
+                        *b = acc[q][e];
+                    }
+            }
+        }
+    }
+    if (team == teams_of(TPR) - 1) {
+#pragma unroll
+        for (int q = 0; q < NV; ++q) {
+            const int c = (lane + q * TPR) * 8;
+            if (c < npad) store8(dst + c, acc[q]);
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < NV; ++q)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[q][e] = 0.f;
+}
+
+// FULL: there is a post norm or a gate whose gradient is wanted, so y is read.
+template <class TS, class TB, int TPR, int NV, bool FULL, bool RAG>
+__global__ void __launch_bounds__(threads_of(TPR)) add_norm_grad_kernel(Norm a) {
+    __shared__ float2 lds[TPR > 64 ? 2 * (TPR / 64) : 1];
+    __shared__ float buf[teams_of(TPR) > 1 ? NV * 8 * TPR : 1];
+    TeamSum<TPR> sum{lds, 0};
+    const int lane = threadIdx.x % TPR, team = threadIdx.x / TPR, n = a.n, c0 = lane * 8;
+    const bool pf32 = a.p.param_dtype == kF32;
+    const uint64_t offset = a.drop ? drop_offset(a.d) : 0;
+    float dw[NV][8] = {}, db[NV][8] = {};
+    float dpw[FULL ? NV : 1][8] = {}, dpb[FULL ? NV : 1][8] = {}, dgate[FULL ? NV : 1][8] = {};
+    const int64_t u1 = (int64_t)(blockIdx.x + 1) * a.units / gridDim.x;
+    for (int64_t unit = (int64_t)blockIdx.x * a.units / gridDim.x; unit < u1; ++unit) {
+        const int64_t group = unit / a.per_group, piece = unit - group * a.per_group;
+        const int64_t first = group * a.unit_rows + piece * a.unit_rows / a.per_group;
+        const int64_t last = group * a.unit_rows + (piece + 1) * a.unit_rows / a.per_group;
+        for (int64_t row = first + team; row < last; row += teams_of(TPR)) {
+            float g[NV][8], u[NV][8];
+            float y[FULL ? NV : 1][8];
+            if constexpr (FULL) {
+                const TB *yr = static_cast<const TB *>(a.p.y) + row * n;
+#pragma unroll
+                for (int q = 0; q < NV; ++q) load_cols<RAG>(yr, c0 + q * 8 * TPR, n, y[q]);
+            }
+            float dh[NV][8];
+            if (a.p.dh) {
+                const TS *r = static_cast<const TS *>(a.p.dh) + row * n;
+#pragma unroll
+                for (int q = 0; q < NV; ++q) load_cols<RAG>(r, c0 + q * 8 * TPR, n, dh[q]);
+            }
+            if (a.p.dout) {
+                const TB *dr = static_cast<const TB *>(a.p.dout) + row * n;
+                const TS *hr = static_cast<const TS *>(a.p.h) + row * n;
+                const float2 st = reinterpret_cast<const float2 *>(a.p.stats)[row];
+#pragma unroll
+                for (int q = 0; q < NV; ++q) {
+                    const int c = c0 + q * 8 * TPR;
+                    load_cols<RAG>(dr, c, n, g[q]);
+                    load_cols<RAG>(hr, c, n, u[q]);
+                }
+#pragma unroll
+                for (int q = 0; q < NV; ++q) {
+                    const int c = c0 + q * 8 * TPR;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        u[q][e] = (u[q][e] - st.x) * st.y;
+                        db[q][e] += g[q][e];
+                        dw[q][e] = fmaf(g[q][e], u[q][e], dw[q][e]);
+                    }
+                    if (a.p.w) {
+                        float w[8];
+                        load_param<RAG>(a.p.w, pf32, 0, c, n, w);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) g[q][e] *= w[e];
+                    }
+                }
+                norm_grad<TPR, NV>(g, u, st.y, a.p.norm, n, sum);
+                if (a.p.dh) {
+#pragma unroll
+                    for (int q = 0; q < NV; ++q)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) g[q][e] += dh[q][e];
+                }
+            } else {
+#pragma unroll
+                for (int q = 0; q < NV; ++q)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) g[q][e] = a.p.dh ? dh[q][e] : 0.f;
+            }
+            if (a.p.dx) {
+                TS *dx = static_cast<TS *>(a.p.dx) + row * n;
+#pragma unroll
+                for (int q = 0; q < NV; ++q) {
+                    float t[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) t[e] = g[q][e] * a.p.x_scale;
+                    store_cols<RAG>(dx, c0 + q * 8 * TPR, n, t);
+                }
+            }
+            if (!FULL && !a.p.dy) continue;
+            float2 ps = make_float2(0.f, 1.f);
+            if (FULL && a.p.post != kNormNone) ps = reinterpret_cast<const float2 *>(a.p.post_stats)[row];
+            const int64_t grow = a.p.gate && a.p.groups > 1 ? row / a.rows_per_gate : 0;
+#pragma unroll
+            for (int q = 0; q < NV; ++q) {
+                const int c = c0 + q * 8 * TPR;
+                float pw[8];
+                const bool scaled = FULL && a.p.post != kNormNone && a.p.pw;
+                if (scaled) load_param<RAG>(a.p.pw, pf32, 0, c, n, pw);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) g[q][e] = c + e < n ? g[q][e] * a.p.y_scale : 0.f;
+                if (a.drop && c < n)
+                    apply_drop(g[q], keep_bits(philox(a.d.seed, offset, (uint64_t)(row * a.octets + (c >> 3))), a.d.thr),
+                               a.d.scale);
+                if constexpr (FULL) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) u[q][e] = c + e < n ? (y[q][e] - ps.x) * ps.y : 0.f;
+                    if (a.gpart) {
+                        float z[8], pb[8];
+                        const bool shifted = a.p.post != kNormNone && a.p.pb;
+                        if (shifted) load_param<RAG>(a.p.pb, pf32, 0, c, n, pb);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            z[e] = scaled ? u[q][e] * pw[e] : u[q][e];
+                            if (shifted) z[e] += pb[e];
+                            // what is dropped counts for nothing, whatever it was
+                            dgate[q][e] += g[q][e] != 0.f ? g[q][e] * z[e] : 0.f;
+                        }
+                    }
+                }
+                if (a.p.gate) {
+                    float t[8];
+                    load_param<RAG>(a.p.gate, pf32, grow, c, n, t);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) g[q][e] *= t[e];
+                }
+                if constexpr (FULL) {
+                    if (a.p.post != kNormNone) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            dpb[q][e] += g[q][e];
+                            dpw[q][e] = fmaf(g[q][e], u[q][e], dpw[q][e]);
+                            if (scaled) g[q][e] *= pw[e];
+                        }
+                    }
+                }
+            }
+            if (FULL && a.p.post != kNormNone) norm_grad<TPR, NV>(g, u, ps.y, a.p.post, n, sum);
+            if (a.p.dy) {
+                TB *dy = static_cast<TB *>(a.p.dy) + row * n;
+#pragma unroll
+                for (int q = 0; q < NV; ++q) store_cols<RAG>(dy, c0 + q * 8 * TPR, n, g[q]);
+            }
+        }
+        if constexpr (FULL)
+            if (a.gpart) flush<TPR, NV>(dgate, a.gpart + unit * a.npad, a.npad, buf);
+    }
+    if (a.part[0]) flush<TPR, NV>(dw, a.part[0] + (int64_t)blockIdx.x * a.npad, a.npad, buf);
+    if (a.part[1]) flush<TPR, NV>(db, a.part[1] + (int64_t)blockIdx.x * a.npad, a.npad, buf);
+    if constexpr (FULL) {
+        if (a.part[2]) flush<TPR, NV>(dpw, a.part[2] + (int64_t)blockIdx.x * a.npad, a.npad, buf);
+        if (a.part[3]) flush<TPR, NV>(dpb, a.part[3] + (int64_t)blockIdx.x * a.npad, a.npad, buf);
+    }
+}
+
+// Sums over the partials of each vector, in a fixed order: 32 columns by 32 ranges of them.
+struct Sums {
+    const float *part[5];
+    void *out[5];
+    int64_t count[5], batch[5];   // partials of an output row; output rows
+    int n, npad;
+    bool f32;
+};
+
+__global__ void __launch_bounds__(1024) add_norm_sum_kernel(Sums s) {
+    __shared__ float buf[32][33];
+    const int k = blockIdx.z, col = threadIdx.x & 31, range = threadIdx.x >> 5;
+    const int c = blockIdx.x * 32 + col;
+    for (int64_t row = blockIdx.y; row < s.batch[k]; row += gridDim.y) {
+        float t = 0.f;
+        if (c < s.n)
+#pragma unroll 8
+            for (int64_t i = range; i < s.count[k]; i += 32) t += s.part[k][(row * s.count[k] + i) * s.npad + c];
+        buf[range][col] = t;
+        __syncthreads();
+        if (range == 0 && c < s.n) {
+            t = 0.f;
+#pragma unroll
+            for (int r = 0; r < 32; ++r) t += buf[r][col];
+            if (s.f32) static_cast<float *>(s.out[k])[row * s.n + c] = t;
+            else static_cast<uint16_t *>(s.out[k])[row * s.n + c] = f32_to_bf16(t);
+        }
+        __syncthreads();
+    }
+}
+
+// Threads and vectors of a row: a wave as far as 16 columns a thread go, then more waves.
+// With a post norm or a gate's gradient five sums over rows share the registers with a row's
+// operands, and a thread takes 8 columns.
+struct Shape {
+    int tpr, nv;
+};
+Shape shape_of(int64_t n, bool full) {
+    const int64_t per = full ? 8 : 16;
+    int tpr = 64;
+    while (tpr < 1024 && tpr * per < n) tpr *= 2;
+    return {tpr, tpr * 8 < n ? 2 : 1};
+}
+
+struct Plan {
+    int64_t grid, units, per_group, unit_rows, npad;
+    bool gate, full;
+};
+
+Plan plan_of(const AddNormPass &p) {
+    Plan l;
+    l.npad = (p.n + 7) / 8 * 8;
+    l.gate = p.y && p.gate && p.dgate;
+    l.full = p.y && (p.post != kNormNone || l.gate);
+    const Shape sh = shape_of(p.n, l.full);
+    const int64_t teams = teams_of(sh.tpr);
+    // two rows a team at least, and no more workgroups than the GPU holds at once
+    int64_t most = 256 * (1024 / threads_of(sh.tpr));
+    if (most > 768) most = 768;
+    int64_t want = (p.M + 2 * teams - 1) / (2 * teams);
+    if (want > most) want = most;
+    if (want < 1) want = 1;
+    const int64_t groups = l.gate ? p.groups : 1;
+    l.unit_rows = p.M / groups;
+    l.per_group = (want + groups - 1) / groups;
+    if (l.per_group > l.unit_rows) l.per_group = l.unit_rows > 0 ? l.unit_rows : 1;
+    l.units = groups * l.per_group;
+    l.grid = l.units < want ? l.units : want;
+    return l;
+}
+
+template <class TS, class TB, int TPR, int NV, bool RAG>
+void run_fwd(const Norm &a, hipStream_t s) {
+    const int64_t blocks = (a.p.M + teams_of(TPR) - 1) / teams_of(TPR);
+    const unsigned grid = (unsigned)(blocks < 4096 ? blocks : 4096);
+    add_norm_kernel<TS, TB, TPR, NV, RAG><<<grid, threads_of(TPR), 0, s>>>(a);
+}
+
+template <class TS, class TB, int TPR, int NV, bool FULL, bool RAG>
+void run_bwd(const Norm &a, const Plan &l, hipStream_t s) {
+    add_norm_grad_kernel<TS, TB, TPR, NV, FULL, RAG><<<(unsigned)l.grid, threads_of(TPR), 0, s>>>(a);
+}
+
+template <class TS, class TB, bool RAG>
+hipError_t run(const Norm &a, const Plan *l, hipStream_t s) {
+    const bool full = l && l->full;
+    const Shape sh = shape_of(a.n, full);
+    const auto is = [&](int tpr, int nv) { return sh.tpr == tpr && sh.nv == nv; };
+    if (!l) {
+        if (is(64, 1)) run_fwd<TS, TB, 64, 1, RAG>(a, s);
+        else if (is(64, 2)) run_fwd<TS, TB, 64, 2, RAG>(a, s);
+        else if (is(128, 2)) run_fwd<TS, TB, 128, 2, RAG>(a, s);
+        else if (is(256, 2)) run_fwd<TS, TB, 256, 2, RAG>(a, s);
+        else if (is(512, 2)) run_fwd<TS, TB, 512, 2, RAG>(a, s);
+        else run_fwd<TS, TB, 1024, 2, RAG>(a, s);
+    } else if (full) {
+        if (is(64, 1)) run_bwd<TS, TB, 64, 1, true, RAG>(a, *l, s);
+        else if (is(128, 1)) run_bwd<TS, TB, 128, 1, true, RAG>(a, *l, s);
+        else if (is(256, 1)) run_bwd<TS, TB, 256, 1, true, RAG>(a, *l, s);
+        else if (is(512, 1)) run_bwd<TS, TB, 512, 1, true, RAG>(a, *l, s);
+        else if (is(1024, 1)) run_bwd<TS, TB, 1024, 1, true, RAG>(a, *l, s);
+        else run_bwd<TS, TB, 1024, 2, true, RAG>(a, *l, s);
+    } else {
+        if (is(64, 1)) run_bwd<TS, TB, 64, 1, false, RAG>(a, *l, s);
+        else if (is(64, 2)) run_bwd<TS, TB, 64, 2, false, RAG>(a, *l, s);
+        else if (is(128, 2)) run_bwd<TS, TB, 128, 2, false, RAG>(a, *l, s);
+        else if (is(256, 2)) run_bwd<TS, TB, 256, 2, false, RAG>(a, *l, s);
+        else if (is(512, 2)) run_bwd<TS, TB, 512, 2, false, RAG>(a, *l, s);
+        else run_bwd<TS, TB, 1024, 2, false, RAG>(a, *l, s);
+    }
+    return hipGetLastError();
+}
+
+hipError_t run_types(const Norm &a, const Plan *l, hipStream_t s) {
+    const bool rag = a.n % 8 != 0;
+    if (a.p.stream_dtype == kBF16) return rag ? run<uint16_t, uint16_t, true>(a, l, s) : run<uint16_t, uint16_t, false>(a, l, s);
+    if (a.p.dtype == kBF16) return rag ? run<float, uint16_t, true>(a, l, s) : run<float, uint16_t, false>(a, l, s);
+    return rag ? run<float, float, true>(a, l, s) : run<float, float, false>(a, l, s);
+}
+
+Norm norm_of(const AddNormPass &p, const DropArgs &d) {
+    Norm a{};
+    a.p = p;
+    a.d = d;
+    a.n = (int)p.n;
+    a.octets = (int)((p.n + 7) / 8);
+    a.npad = a.octets * 8;
+    a.rows_per_gate = p.M / p.groups;
+    a.drop = p.y && d.thr > 0;
+    return a;
+}
+
+}  // namespace
+
+hipError_t launch_add_norm(const AddNormPass &p, const DropArgs &d, hipStream_t s) {
+    return run_types(norm_of(p, d), nullptr, s);
+}
+
+// Partials of dw, db, dpw, dpb, then of the gate's gradient.
+size_t add_norm_workspace(const AddNormPass &p) {
+    const Plan l = plan_of(p);
+    const int64_t vectors = (p.dw != nullptr) + (p.db != nullptr) + (p.dpw != nullptr) + (p.dpb != nullptr);
+    return (size_t)((vectors * l.grid + (l.gate ? l.units : 0)) * l.npad) * sizeof(float);
+}
+
+hipError_t launch_add_norm_grad(const AddNormPass &p, const DropArgs &d, hipStream_t s) {
+    const Plan l = plan_of(p);
+    Norm a = norm_of(p, d);
+    a.units = l.units;
+    a.per_group = l.per_group;
+    a.unit_rows = l.unit_rows;
+    void *const out[5] = {p.dw, p.db, p.dpw, p.dpb, l.gate ? p.dgate : nullptr};
+    Sums t{};
+    t.n = a.n;
+    t.npad = a.npad;
+    t.f32 = p.param_dtype == kF32;
+    int count = 0;
+    int64_t rows = 1;
+    float *at = static_cast<float *>(p.ws);
+    for (int k = 0; k < 5; ++k) {
+        if (!out[k]) continue;
+        const bool gate = k == 4;
+        (gate ? a.gpart : a.part[k]) = at;
+        t.part[count] = at;
+        t.out[count] = out[k];
+        t.count[count] = gate ? l.per_group : l.grid;
+        t.batch[count] = gate ? p.groups : 1;
+        if (t.batch[count] > rows) rows = t.batch[count];
+        at += (gate ? l.units : l.grid) * a.npad;
+        ++count;
+    }
+    hipError_t e = run_types(a, &l, s);
+    if (e != hipSuccess || count == 0) return e;
+    if (rows > 4096) rows = 4096;
+    add_norm_sum_kernel<<<dim3((unsigned)((a.n + 31) / 32), (unsigned)rows, (unsigned)count), 1024, 0, s>>>(t);
+    return hipGetLastError();
+}
+
+}  // namespace dyad

@@ -1,0 +1,134 @@
+// Softmax cross entropy of z = X W^T against targets, z never kept: loss = lse(z) - z_target.
+// Forward: tiles of logits leave (largest, sum of exponentials) per token, joined here.
+// Backward, a piece of the vocabulary at a time: the tiles' logits again, as
+// G = dloss (exp(z - lse) - onehot), then dX += G W and dW = G^T X of the piece.  Forming z
+// twice is 8 M n V operations for the four products where 6 M n V would do with z kept, which
+// takes M V values written and read at 4 bytes (as long, at the rates of this card, as the
+// product) and the memory for them.
+#include "lm_internal.h"
+
+namespace dyad {
+
+namespace {
+
+// A wave a token: joins the tiles' statistics.
+__global__ void __launch_bounds__(256) loss_join_kernel(LossEpi e, int64_t M, float *loss, float *lse) {
+    const int lane = threadIdx.x & 63;
+    for (int64_t m = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); m < M; m += (int64_t)gridDim.x * 4) {
+        float2 s = make_float2(-INFINITY, 0.f);
+        for (int t = lane; t < e.tiles; t += 64) s = join_stats(s, e.part[m * e.tiles + t]);
+#pragma unroll
+        for (int w = 32; w > 0; w >>= 1) s = join_stats(s, make_float2(__shfl_xor(s.x, w), __shfl_xor(s.y, w)));
+        if (lane == 0) {
+            const float l = s.x + logf(s.y);
+            lse[m] = l;
+            loss[m] = loss_counts(e, e.targets[m]) ? l - e.at_target[m] : 0.f;
+        }
+    }
+}
+
+// Sum over the tokens, in 64 bits and a fixed order, and how many count; the mean of none is 0.
+__global__ void __launch_bounds__(1024) loss_sum_kernel(LossEpi e, int64_t M, const float *each, bool mean, float *loss,
+                                                        float *count) {
+    __shared__ double sums[16];
+    __shared__ int64_t counts[16];
+    double s = 0.0;
+    int64_t c = 0;
+    for (int64_t m = threadIdx.x; m < M; m += 1024) {
+        s += (double)each[m];
+        c += loss_counts(e, e.targets[m]) ? 1 : 0;
+    }
+#pragma unroll
+    for (int w = 32; w > 0; w >>= 1) {
+        s += __shfl_xor(s, w);
+        c += __shfl_xor(c, w);
+    }
+    if ((threadIdx.x & 63) == 0) {
+        sums[threadIdx.x >> 6] = s;
+        counts[threadIdx.x >> 6] = c;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        s = 0.0;
+        c = 0;
+        for (int w = 0; w < 16; ++w) {
+            s += sums[w];
+            c += counts[w];
+        }
+        *loss = (float)(mean && c > 0 ? s / (double)c : s);
+        if (count) *count = (float)c;
+    }
+}
+
+__global__ void __launch_bounds__(256) zero_kernel(uint16_t *p, int64_t n) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = 0;
+}
+
+int64_t up(int64_t v, int64_t q) { return (v + q - 1) / q * q; }
+
+// Vocabulary columns of a piece in fp32: G within 256 MB, but for very many tokens.
+int64_t f32_piece(int64_t M, int64_t V) {
+    int64_t vp = ((int64_t)256 << 20) / (4 * (M > 0 ? M : 1)) / 128 * 128;
+    if (vp < 1024) vp = 1024;
+    return vp < V ? vp : V;
+}
+
+LossEpi epi_of(const LossPass &p) {
+    LossEpi e{};
+    e.targets = p.targets;
+    e.ignore = p.ignore;
+    e.V = p.V;
+    e.lse = p.lse;
+    e.dloss = p.dloss;
+    e.count = p.count;
+    e.reduction = p.reduction;
+    return e;
+}
+
+}  // namespace
+
+// Forward: every token's loss, its target's logit, the tiles' statistics, then what the bf16
+// products need.  Backward: G of a piece (fp32), or what the bf16 pieces need.
+size_t loss_workspace(bool backward, int64_t M, int64_t n, int64_t V, int dtype) {
+    if (M == 0) return 0;
+    if (backward) return dtype == kF32 ? (size_t)(M * f32_piece(M, V)) * 4 : 0;
+    const int64_t tiles = dtype == kF32 ? loss_f32_tiles(M, V) : 0;
+    return (size_t)(2 * up(M, 4) * 4 + M * tiles * 8);
+}
+
+hipError_t launch_loss_forward(const LossPass &p, hipStream_t s) {
+    LossEpi e = epi_of(p);
+    float *each = static_cast<float *>(p.ws);
+    if (p.M > 0) {
+        e.at_target = each + up(p.M, 4);
+        e.part = reinterpret_cast<float2 *>(e.at_target + up(p.M, 4));
+        if (p.reduction == kReduceNone) each = p.loss;
+        e.tiles = loss_f32_tiles(p.M, p.V);
+        hipError_t err = p.dtype == kF32 ? launch_loss_f32_stats(p, e, s) : hipErrorNotSupported;
+        if (err != hipSuccess) return err;
+        const int64_t blocks = (p.M + 3) / 4;
+        loss_join_kernel<<<(unsigned)(blocks < 8192 ? blocks : 8192), 256, 0, s>>>(e, p.M, each, p.lse);
+    }
+    if (p.reduction != kReduceNone)
+        loss_sum_kernel<<<1, 1024, 0, s>>>(e, p.M, each, p.reduction == kReduceMean, p.loss, p.count);
+    return hipGetLastError();
+}
+
+hipError_t launch_loss_backward(const LossPass &p, hipStream_t s) {
+    if (p.M == 0) {
+        if (!p.dW) return hipSuccess;
+        zero_kernel<<<1024, 256, 0, s>>>(static_cast<uint16_t *>(p.dW), p.n * p.V * (p.dtype == kF32 ? 2 : 1));
+        return hipGetLastError();
+    }
+    const LossEpi e = epi_of(p);
+    if (p.dtype != kF32) return hipErrorNotSupported;
+    const int64_t piece = f32_piece(p.M, p.V);
+    for (int64_t v0 = 0; v0 < p.V; v0 += piece) {
+        const hipError_t err = launch_loss_f32_piece(p, e, v0, p.V - v0 < piece ? p.V - v0 : piece,
+                                                     static_cast<float *>(p.ws), v0 == 0, s);
+        if (err != hipSuccess) return err;
+    }
+    return hipSuccess;
+}
+
+}  // namespace dyad

@@ -1,0 +1,48 @@
+// Rows of any length and alignment, eight columns a lane.
+#pragma once
+
+#include "mfma_common.h"
+
+namespace dyad {
+
+// Eight values from p as fp32.  Rows of a width that 8 does not divide start at any
+// element, so the access is declared with the element's alignment; global memory
+// takes 16-byte instructions at such addresses, and at aligned ones they are the
+// same instructions.
+__device__ __forceinline__ void load8(const float *p, float (&v)[8]) { __builtin_memcpy(v, p, 32); }
+__device__ __forceinline__ void load8(const uint16_t *p, float (&v)[8]) {
+    uint32_t w[4];
+    __builtin_memcpy(w, p, 16);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = unpack_bf16(w[e >> 1], e & 1);
+}
+__device__ __forceinline__ void store8(float *p, const float (&v)[8]) { __builtin_memcpy(p, v, 32); }
+__device__ __forceinline__ void store8(uint16_t *p, const float (&v)[8]) {
+    const uint32_t w[4] = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+    __builtin_memcpy(p, w, 16);
+}
+
+// Columns c .. c + 7 of a row of n; columns past it read zero and are not written.  RAG:
+// n may end inside the eight (the element-wise ends double a kernel's registers, so
+// rows of whole vectors have instances without them).
+template <bool RAG, class T>
+__device__ __forceinline__ void load_cols(const T *row, int c, int n, float (&v)[8]) {
+    if (c + 8 <= n) {
+        load8(row + c, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = RAG && c + e < n ? load_f32(row, c + e) : 0.f;
+    }
+}
+template <bool RAG, class T>
+__device__ __forceinline__ void store_cols(T *row, int c, int n, const float (&v)[8]) {
+    if (c + 8 <= n) {
+        store8(row + c, v);
+    } else if constexpr (RAG) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (c + e < n) store_f32(row, c + e, v[e]);
+    }
+}
+
+}  // namespace dyad

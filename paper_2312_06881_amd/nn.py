@@ -15,6 +15,12 @@
   the pre-activation) as 8-bit microscaled blocks; the gradients see the kept values.
 * ``MX4DyadLinear``, ``MX4DyadFF``: inference on fp4 weights and inputs.
 
+* ``dropout`` / ``Dropout``, ``add_norm`` / ``AddNorm``, ``linear_cross_entropy`` /
+  ``LinearCrossEntropy``: what stands around the layers in a language model.  A pre-norm
+  block is ``x, a = norm(x, y)`` (the last block's output joins the stream, which is normed)
+  and ``y = ff(a)``; after the last one the loss over the vocabulary, whose logits
+  are never kept.
+
 Autograd runs every pass through the C-ABI (forward, input gradient, weight and
 bias gradient); there is no torch fallback and CPU tensors are rejected.
 Leading input dimensions are flattened into the token dimension.  Weights
@@ -28,10 +34,12 @@ import math
 
 import torch
 from torch.autograd import forward_ad
+from torch.autograd.function import once_differentiable
 
-from . import VARIANTS, DyadError, backward_dw, backward_dx, forward, mx
+from . import VARIANTS, DyadError, backward_dw, backward_dx, forward, lm, mx
 
-__all__ = ["DyadLinear", "DyadFF", "MX4DyadLinear", "MX4DyadFF", "dyad_linear", "dyad_ff"]
+__all__ = ["DyadLinear", "DyadFF", "MX4DyadLinear", "MX4DyadFF", "dyad_linear", "dyad_ff", "Dropout", "AddNorm",
+           "LinearCrossEntropy", "dropout", "add_norm", "linear_cross_entropy"]
 
 
 def _tokens(x: torch.Tensor) -> torch.Tensor:
@@ -406,3 +414,215 @@ class MX4DyadFF(torch.nn.Module):
 
     def forward(self, x):
         return self.fc2(self.fc1(x))
+
+
+# ---- around the layers: dropout, the residual stream's norms, the loss ----------------------
+
+def _saved_offset(offset):
+    """(what autograd saves, what it does not) of an offset: a tensor's value has to be the
+    forward pass's when the backward pass draws the mask again, and autograd checks that."""
+    return (offset, None) if isinstance(offset, torch.Tensor) else (None, offset)
+
+
+class _DropoutFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, p, seed, offset):
+        ctx.p, ctx.seed = p, seed
+        kept, ctx.offset = _saved_offset(offset)
+        ctx.save_for_backward(kept)
+        return lm.dropout(x, p, seed, offset)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        kept, = ctx.saved_tensors
+        return lm.dropout(dy.contiguous(), ctx.p, ctx.seed, ctx.offset if kept is None else kept), None, None, None
+
+
+def dropout(x, p, seed, offset=0, training=True):
+    """x with values dropped with probability p and the others scaled; x itself when not training.  The mask
+    follows from (seed, offset) and each value's row and column, and is drawn again for the gradient.  offset: a whole
+    number, or a one-element int64 tensor on x's device, which a captured graph reads at every replay; between the
+    passes it must not change."""
+    if not training:
+        return x
+    x = x.contiguous()
+    if _plain(x):
+        return lm.dropout(x, p, seed, offset)
+    return _DropoutFn.apply(x, p, seed, offset)
+
+
+class _AddNormFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, y, weight, bias, post_weight, post_bias, gate, offset, norm, post_norm, dtype, kw):
+        h, out, stats, post_stats = lm.add_norm(x, y, norm, weight, bias, post_norm=post_norm, post_weight=post_weight,
+                                                post_bias=post_bias, gate=gate, offset=offset, dtype=dtype, keep=True, **kw)
+        kept, ctx.offset = _saved_offset(offset)
+        # of y only its type counts where nothing reads it again
+        reads_y = post_norm is not None or gate is not None
+        ctx.y = None if y is None or reads_y else y.dtype
+        ctx.norm, ctx.post_norm, ctx.dtype, ctx.kw = norm, post_norm, dtype, kw
+        ctx.set_materialize_grads(False)
+        ctx.save_for_backward(h, y if reads_y else None, weight, bias, post_weight, post_bias, gate, stats, post_stats, kept)
+        if h is x:
+            h = x.view_as(x)
+        return (h, out) if norm else (h,)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dh, dout=None):
+        h, y, weight, bias, post_weight, post_bias, gate, stats, post_stats, kept = ctx.saved_tensors
+        if dh is None and dout is None:
+            return (None,) * 12
+        names = ("x", "y", "weight", "bias", "post_weight", "post_bias", "gate")
+        want = [n for n, need in zip(names, ctx.needs_input_grad) if need]
+        if ctx.y is not None:
+            y = h if ctx.y == h.dtype else torch.empty(h.shape, dtype=ctx.y, device=h.device)
+        g = lm.add_norm_backward(None if dh is None else dh.contiguous(), None if dout is None else dout.contiguous(), h,
+                                 stats, post_stats, y, ctx.norm, weight, bias, post_norm=ctx.post_norm,
+                                 post_weight=post_weight, post_bias=post_bias, gate=gate,
+                                 offset=ctx.offset if kept is None else kept, dtype=ctx.dtype, want=want, **ctx.kw)
+        return (*(g.get(n) for n in names), None, None, None, None, None)
+
+
+def add_norm(x, y=None, norm="layer", weight=None, bias=None, *, post_norm=None, post_weight=None, post_bias=None, gate=None,
+             x_scale=1.0, y_scale=1.0, eps=1e-5, p=0.0, seed=0, offset=0, dtype=None):
+    """(h, out): h = x_scale x + y_scale gate * dropout(post_norm(y)), the residual stream with a block's output,
+    and out = norm(h), the next block's input.  x and y [..., n]; see ``lm.add_norm``.  out is None without a norm."""
+    shape = x.shape
+    xt, yt = _tokens(x), None if y is None else _tokens(y)
+    if y is not None and y.shape != shape:
+        raise ValueError(f"x and y have one shape, got {tuple(shape)} and {tuple(y.shape)}")
+    kw = dict(x_scale=float(x_scale), y_scale=float(y_scale), eps=float(eps), p=float(p), seed=seed)
+    if _plain(x, y, weight, bias, post_weight, post_bias, gate):
+        h, out = lm.add_norm(xt, yt, norm, weight, bias, post_norm=post_norm, post_weight=post_weight,
+                             post_bias=post_bias, gate=gate, offset=offset, dtype=dtype, **kw)
+    else:
+        h, *out = _AddNormFn.apply(xt, yt, weight, bias, post_weight, post_bias, gate, offset, norm, post_norm, dtype, kw)
+        out = out[0] if out else None
+    return h.reshape(shape), None if out is None else out.reshape(shape)
+
+
+class _LinearCrossEntropyFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, targets, ignore_index, reduction):
+        loss, lse, count = lm.linear_cross_entropy(x, weight, targets, ignore_index, reduction, keep=True)
+        ctx.ignore_index, ctx.reduction = ignore_index, reduction
+        ctx.save_for_backward(x, weight, targets, lse, count)
+        return loss
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dloss):
+        x, weight, targets, lse, count = ctx.saved_tensors
+        dx, dw = lm.linear_cross_entropy_backward(dloss.contiguous(), x, weight, targets, lse, count, ctx.ignore_index,
+                                                  ctx.reduction, *ctx.needs_input_grad[:2])
+        return dx, dw, None, None, None
+
+
+def linear_cross_entropy(x, weight, targets, ignore_index=-100, reduction="mean"):
+    """Softmax cross entropy of the logits x W^T against targets, x [..., n], weight [V, n], targets [...] int64:
+    float32, of targets' shape for reduction "none", else a scalar.  The logits are formed in tiles, in both
+    passes, and never kept.  See ``lm.linear_cross_entropy``."""
+    if targets.shape != x.shape[:-1]:
+        raise ValueError(f"targets have shape {tuple(x.shape[:-1])}, got {tuple(targets.shape)}")
+    xt, t = _tokens(x), targets.reshape(-1).contiguous()
+    if _plain(x, weight):
+        loss = lm.linear_cross_entropy(xt, weight, t, ignore_index, reduction)
+    else:
+        loss = _LinearCrossEntropyFn.apply(xt, weight, t, ignore_index, reduction)
+    return loss.reshape(targets.shape) if reduction == "none" else loss
+
+
+class Dropout(torch.nn.Module):
+    """Dropout whose mask is drawn from a counter and never stored.  Every call in training takes the next
+    offset.  seed: by default one drawn from torch's CPU generator; layers that share one drop the same places.
+    capturable: the counter lives on the device (with the module), so that every replay of a captured call
+    draws another mask."""
+
+    def __init__(self, p=0.1, seed=None, capturable=False, device=None):
+        super().__init__()
+        if not 0.0 <= p <= 1.0:
+            raise ValueError(f"p is a probability, got {p}")
+        self.p, self.capturable = p, capturable
+        self.seed = int(torch.randint(2 ** 62, ()).item()) if seed is None else seed
+        self.calls = 0
+        if capturable:
+            del self.calls
+            self.register_buffer("calls", torch.zeros((1,), dtype=torch.int64, device=device))
+
+    def next_offset(self):
+        """The offset of the call that asks, and one more from here on."""
+        if not self.capturable:
+            self.calls += 1
+            return self.calls - 1
+        now = self.calls.clone()     # the backward pass draws this call's mask again
+        self.calls += 1
+        return now
+
+    def forward(self, x):
+        if not self.training or self.p == 0.0:
+            return x
+        return dropout(x, self.p, self.seed, self.next_offset())
+
+    def extra_repr(self):
+        return f"p={self.p}, capturable={self.capturable}"
+
+
+class AddNorm(torch.nn.Module):
+    """Joins a block's output with the residual stream and norms the stream for the next block:
+    ``h, out = add_norm(x, y)``, or ``add_norm(x)`` before the first block.
+
+    norm, post_norm: "layer", "rms" or None; gate: a learned scale of the block's output, one a column, from
+    ``gate_init``; p: dropout of the block's output (after post_norm) in training."""
+
+    def __init__(self, d, norm="layer", post_norm=None, gate=False, gate_init=1.0, x_scale=1.0, y_scale=1.0, eps=1e-5,
+                 p=0.0, bias=True, seed=None, capturable=False, device=None, dtype=torch.bfloat16):
+        super().__init__()
+        for kind, what in ((norm, "norm"), (post_norm, "post_norm")):
+            lm._norm_kind(kind, what)
+        self.d, self.norm, self.post_norm = d, norm, post_norm
+        self.x_scale, self.y_scale, self.eps = x_scale, y_scale, eps
+
+        def vector(wanted, value):
+            return torch.nn.Parameter(torch.full((d,), value, device=device, dtype=dtype)) if wanted else None
+
+        self.weight, self.bias = vector(norm, 1.0), vector(norm == "layer" and bias, 0.0)
+        self.post_weight, self.post_bias = vector(post_norm, 1.0), vector(post_norm == "layer" and bias, 0.0)
+        self.gate = vector(gate, gate_init)
+        self.dropout = Dropout(p, seed, capturable, device)
+
+    def forward(self, x, y=None):
+        if y is None:
+            return add_norm(x, None, self.norm, self.weight, self.bias, eps=self.eps,
+                            dtype=None if self.weight is None or x.dtype != torch.float32 else self.weight.dtype)
+        random = {}
+        if self.training and self.dropout.p:
+            random = {"p": self.dropout.p, "seed": self.dropout.seed, "offset": self.dropout.next_offset()}
+        return add_norm(x, y, self.norm, self.weight, self.bias, post_norm=self.post_norm, post_weight=self.post_weight,
+                        post_bias=self.post_bias, gate=self.gate, x_scale=self.x_scale, y_scale=self.y_scale, eps=self.eps,
+                        **random)
+
+    def extra_repr(self):
+        return f"{self.d}, norm={self.norm}, post_norm={self.post_norm}, gate={self.gate is not None}"
+
+
+class LinearCrossEntropy(torch.nn.Module):
+    """The last layer and the loss of a language model: softmax cross entropy of x W^T, W [vocab, d] (``weight``;
+    pass the embedding's to share it).  The logits are never kept."""
+
+    def __init__(self, d, vocab, weight=None, ignore_index=-100, reduction="mean", device=None, dtype=torch.bfloat16):
+        super().__init__()
+        if reduction not in lm.REDUCTIONS:
+            raise ValueError("reduction is none, sum or mean")
+        if weight is None:
+            weight = torch.nn.Parameter(torch.empty((vocab, d), device=device, dtype=dtype).normal_(std=0.02))
+        elif tuple(weight.shape) != (vocab, d):
+            raise ValueError(f"weight has shape {tuple(weight.shape)}, expected {(vocab, d)}")
+        self.weight, self.ignore_index, self.reduction = weight, ignore_index, reduction
+
+    def forward(self, x, targets):
+        return linear_cross_entropy(x, self.weight, targets, self.ignore_index, self.reduction)
+
+    def extra_repr(self):
+        return f"vocab={self.weight.shape[0]}, d={self.weight.shape[1]}, reduction={self.reduction}"
