@@ -147,4 +147,13 @@ hipError_t launch_loss_f32_stats(const LossPass &p, const LossEpi &e, hipStream_
 hipError_t launch_loss_f32_piece(const LossPass &p, const LossEpi &e, int64_t v0, int64_t vp, float *G, bool first,
                                  hipStream_t s);
 
+
+// bf16 (loss_mfma.hip).  The statistics (ws: forward_bytes), and the whole backward pass (the
+// call's workspace: backward_bytes).
+int loss_mfma_tiles(int64_t M, int64_t V);
+size_t loss_mfma_forward_bytes(int64_t M, int64_t n, int64_t V);
+size_t loss_mfma_backward_bytes(int64_t M, int64_t n, int64_t V);
+hipError_t launch_loss_mfma_stats(const LossPass &p, const LossEpi &e, void *ws, hipStream_t s);
+hipError_t launch_loss_mfma_grad(const LossPass &p, const LossEpi &e, hipStream_t s);
+
 }  // namespace dyad

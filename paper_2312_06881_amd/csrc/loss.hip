@@ -73,6 +73,9 @@ int64_t f32_piece(int64_t M, int64_t V) {
     return vp < V ? vp : V;
 }
 
+// Every token's loss, its target's logit and the tiles' statistics.
+size_t stats_bytes(int64_t M, int64_t tiles) { return (size_t)up(2 * up(M, 4) * 4 + M * tiles * 8, 256); }
+
 LossEpi epi_of(const LossPass &p) {
     LossEpi e{};
     e.targets = p.targets;
@@ -87,13 +90,11 @@ LossEpi epi_of(const LossPass &p) {
 
 }  // namespace
 
-// Forward: every token's loss, its target's logit, the tiles' statistics, then what the bf16
-// products need.  Backward: G of a piece (fp32), or what the bf16 pieces need.
 size_t loss_workspace(bool backward, int64_t M, int64_t n, int64_t V, int dtype) {
     if (M == 0) return 0;
-    if (backward) return dtype == kF32 ? (size_t)(M * f32_piece(M, V)) * 4 : 0;
-    const int64_t tiles = dtype == kF32 ? loss_f32_tiles(M, V) : 0;
-    return (size_t)(2 * up(M, 4) * 4 + M * tiles * 8);
+    const bool f32 = dtype == kF32;
+    if (backward) return f32 ? (size_t)(M * f32_piece(M, V)) * 4 : loss_mfma_backward_bytes(M, n, V);
+    return stats_bytes(M, f32 ? loss_f32_tiles(M, V) : loss_mfma_tiles(M, V)) + (f32 ? 0 : loss_mfma_forward_bytes(M, n, V));
 }
 
 hipError_t launch_loss_forward(const LossPass &p, hipStream_t s) {
@@ -103,8 +104,10 @@ hipError_t launch_loss_forward(const LossPass &p, hipStream_t s) {
         e.at_target = each + up(p.M, 4);
         e.part = reinterpret_cast<float2 *>(e.at_target + up(p.M, 4));
         if (p.reduction == kReduceNone) each = p.loss;
-        e.tiles = loss_f32_tiles(p.M, p.V);
-        hipError_t err = p.dtype == kF32 ? launch_loss_f32_stats(p, e, s) : hipErrorNotSupported;
+        const bool f32 = p.dtype == kF32;
+        e.tiles = f32 ? loss_f32_tiles(p.M, p.V) : loss_mfma_tiles(p.M, p.V);
+        const hipError_t err = f32 ? launch_loss_f32_stats(p, e, s)
+                                   : launch_loss_mfma_stats(p, e, static_cast<char *>(p.ws) + stats_bytes(p.M, e.tiles), s);
         if (err != hipSuccess) return err;
         const int64_t blocks = (p.M + 3) / 4;
         loss_join_kernel<<<(unsigned)(blocks < 8192 ? blocks : 8192), 256, 0, s>>>(e, p.M, each, p.lse);
@@ -121,7 +124,7 @@ hipError_t launch_loss_backward(const LossPass &p, hipStream_t s) {
         return hipGetLastError();
     }
     const LossEpi e = epi_of(p);
-    if (p.dtype != kF32) return hipErrorNotSupported;
+    if (p.dtype != kF32) return launch_loss_mfma_grad(p, e, s);
     const int64_t piece = f32_piece(p.M, p.V);
     for (int64_t v0 = 0; v0 < p.V; v0 += piece) {
         const hipError_t err = launch_loss_f32_piece(p, e, v0, p.V - v0 < piece ? p.V - v0 : piece,

@@ -1,0 +1,477 @@
+// The loss's matrix products in bf16, on the pipelined eight-wave tiles of pp_core.h:
+//   kStats  Z = X W^T, tokens by vocabulary: per token (largest, sum of exponentials) of the tile
+//   kGrad   Z^T = W X^T of a piece of the vocabulary, as G^T = dloss (exp(Z^T - lse) - onehot), in bf16
+//   kDw     dW = G^T X of the piece
+//   kDx     dX^T += W^T G of the piece, in fp32
+// Side A's rows run along the reduction, side B's do (W, X) or are its indices (X, G^T read
+// transposed out of LDS), so one copy of G serves both products.  What they need laid out
+// otherwise is laid out once a call: W^T, and X and W with rows of whole 64s where n is not.
+// Padded reduction indices are zero on one side and finite on the other.
+#include "lm_internal.h"
+#include "pp_core.h"
+#include "row_io.h"
+
+namespace dyad {
+
+namespace {
+
+enum Kind { kStats, kGrad, kDw, kDx };
+
+// What the gradient's epilogue needs of a token, tokens past the last too.
+struct Token {
+    float *scale, *lse2;   // 0 where the token does not count; lse log2(e)
+    int *target;           // -1 where it does not
+};
+
+struct Args {
+    const uint16_t *A, *B;
+    int64_t lda, ldb, I, J, K;   // K: a multiple of 64
+    int64_t rows_b;              // side B's rows where they are the reduction's indices
+    int tiles_i, tiles_j, group;
+    LossEpi e;
+    Token tok;
+    int64_t v0;
+    uint16_t *out;
+    float *acc;
+    int64_t ldo;
+    bool first;
+};
+
+template <int BM, int BN, int WGM, int WGN, bool TB>
+struct Cfg {
+    static constexpr int WM = BM / WGM, WN = BN / WGN, kSubM = WM / 16, kSubN = WN / 16;
+    using A = PPSide<BM, false>;
+    using B = PPSide<BN, TB>;
+    static constexpr bool kTwo = BM * BN <= 128 * 128;   // two workgroups share a CU
+    static constexpr int kSlotA = kTwo ? 2 : 3, kSlotB = 2;
+    static constexpr int kOffB = kSlotA * A::kBytes, kLds = kOffB + kSlotB * B::kBytes;
+    static_assert(WGM * WGN == kPPWaves && kLds <= 160 * 1024, "eight waves, LDS budget");
+};
+
+// Swaps the odd 16-lane rows of a with the even ones of b.
+__device__ __forceinline__ void swap_lane_rows(uint32_t &a, uint32_t &b) {
+    typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
+    const u32x2_t r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+    a = r.x;
+    b = r.y;
+}
+
+// x: a lane's four sums of column block 2 jp and of the next.  After the swap it holds 8
+// consecutive columns, from lane_piece() of the pair on.
+__device__ __forceinline__ uint4 pack_pair(const float (&x)[8]) {
+    uint32_t d0 = pack_bf16(x[0], x[1]), d1 = pack_bf16(x[2], x[3]), s0 = pack_bf16(x[4], x[5]), s1 = pack_bf16(x[6], x[7]);
+    swap_lane_rows(d0, s0);
+    swap_lane_rows(d1, s1);
+    return make_uint4(d0, d1, s0, s1);
+}
+__device__ __forceinline__ int lane_piece(int lg) { return (lg & 1) * 16 + (lg >> 1) * 8; }
+
+template <int BM, int BN, int WGM, int WGN, bool TB, Kind KIND>
+__global__ void __launch_bounds__(kPPThreads, 1) loss_pp_kernel(Args g) {
+    using C = Cfg<BM, BN, WGM, WGN, TB>;
+    using SA = typename C::A;
+    using SB = typename C::B;
+    constexpr int SM = C::kSubM, SN = C::kSubN;
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[C::kLds];
+    lds_u8 *lds = (lds_u8 *)smem;
+    const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // runs of `group` panels of side A, side A fastest
+    const int item = xcd_tile(blockIdx.x, g.tiles_i * g.tiles_j), run = g.group * g.tiles_j;
+    const int first = item / run * g.group;
+    const int gm = g.tiles_i - first < g.group ? g.tiles_i - first : g.group;
+    const int64_t i0 = (int64_t)(first + item % run % gm) * BM;
+    const int tile_j = item % run / gm;
+    const int64_t j0 = (int64_t)tile_j * BN;
+    const int64_t left_i = g.I - i0 < BM ? g.I - i0 : BM, left_j = g.J - j0 < BN ? g.J - j0 : BN;
+    const int units = (int)(g.K / kPPK);
+
+    const __amdgpu_buffer_rsrc_t rA = buffer_rsrc(g.A + i0 * g.lda, (uint32_t)(left_i * g.lda * 2));
+    const __amdgpu_buffer_rsrc_t rB0 = buffer_rsrc(g.B + j0 * g.ldb, TB ? 0u : (uint32_t)(left_j * g.ldb * 2));
+    uint32_t voA[SA::kPer], voB[SB::kPer], loA[SA::kPer], loB[SB::kPer];
+#pragma unroll
+    for (int q = 0; q < SA::kPer; ++q) {
+        int row, byte;
+        const int i = pp_instr(wave, q);
+        pp_source<BM, false>(i, lane, row, byte);
+        voA[q] = (uint32_t)row * (uint32_t)g.lda * 2u + (uint32_t)byte;
+        loA[q] = 1024u * (uint32_t)i;
+    }
+#pragma unroll
+    for (int q = 0; q < SB::kPer; ++q) {
+        int row, byte;
+        const int i = pp_instr(wave, q);
+        pp_source<BN, TB>(i, lane, row, byte);
+        voB[q] = (uint32_t)row * (uint32_t)g.ldb * 2u + (uint32_t)byte;
+        loB[q] = (uint32_t)C::kOffB + 1024u * (uint32_t)i;
+    }
+    const auto clamp = [&](int d) { return d < units ? d : units - 1; };
+    auto issue_a = [&](int d) {
+        lds_u8 *slot = lds + d % C::kSlotA * SA::kBytes;
+        const uint32_t so = (uint32_t)clamp(d) * (uint32_t)(2 * kPPK);
+#pragma unroll
+        for (int q = 0; q < SA::kPer; ++q) dma16(rA, slot + loA[q], voA[q], so);
+    };
+    auto issue_b = [&](int d) {
+        lds_u8 *slot = lds + d % C::kSlotB * SB::kBytes;
+        __amdgpu_buffer_rsrc_t r = rB0;
+        uint32_t so = 0;
+        if constexpr (TB) {
+            // the rows of this unit: their offsets pass 32 bits over the reduction, and those
+            // past the last read zero
+            const int64_t k0 = (int64_t)clamp(d) * kPPK;
+            const int64_t rows = g.rows_b - k0 < kPPK ? g.rows_b - k0 : kPPK;
+            r = buffer_rsrc(g.B + k0 * g.ldb + j0, rows > 0 ? (uint32_t)((rows * g.ldb - j0) * 2) : 0u);
+        } else {
+            so = (uint32_t)clamp(d) * (uint32_t)(2 * kPPK);
+        }
+#pragma unroll
+        for (int q = 0; q < SB::kPer; ++q) dma16(r, slot + loB[q], voB[q], so);
+    };
+    const int wm0 = (wave / WGN) * C::WM, wn0 = (wave % WGN) * C::WN;
+    const uint32_t base = (uint32_t)(uintptr_t)lds;
+    const uint32_t fa = base + pp_frag<BM, false>(wm0, 0, lane);
+    uint32_t fb[TB ? SN : 1];
+#pragma unroll
+    for (int j = 0; j < (TB ? SN : 1); ++j) fb[j] = base + (uint32_t)C::kOffB + pp_frag<BN, TB>(wn0, j, lane);
+    auto addr = [&](int d, int h, uint32_t &pa, uint32_t (&pb)[TB ? SN : 1]) {
+        pa = pp_step<BM, false>(fa + (uint32_t)(d % C::kSlotA * SA::kBytes), h);
+#pragma unroll
+        for (int j = 0; j < (TB ? SN : 1); ++j) pb[j] = pp_step<BN, TB>(fb[j] + (uint32_t)(d % C::kSlotB * SB::kBytes), h);
+    };
+    f32x4_t acc[SM][SN];
+#pragma unroll
+    for (int i = 0; i < SM; ++i)
+#pragma unroll
+        for (int j = 0; j < SN; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    pp_loop<SM, SN, TB, 4 * SB::kPitch, SA::kPer, SB::kPer, C::kSlotA, C::kSlotB>(units, wave, acc, issue_a, issue_b, addr,
+                                                                                [](int) { return true; });
+    // acc[i][j][v]: side A's row wm0 + 16 i + lr, side B's wn0 + 16 j + 4 lg + v
+    if constexpr (KIND == kStats) {
+        loss_stats<SM, SN, BM, WGN>(g.e, acc, i0, g.I, j0, tile_j, wm0, wn0, wave % WGN, reinterpret_cast<float2 *>(smem));
+    } else if constexpr (KIND == kGrad) {
+        const int v_lane = (int)(g.v0 + i0) + wm0 + lr;
+#pragma unroll
+        for (int jp = 0; jp < SN / 2; ++jp) {
+            float scale[8], lse2[8];
+            int target[8];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int64_t t = j0 + wn0 + 32 * jp + 16 * h + 4 * lg;   // tokens are laid out for whole tiles
+                __builtin_memcpy(scale + 4 * h, __builtin_assume_aligned(g.tok.scale + t, 16), 16);
+                __builtin_memcpy(lse2 + 4 * h, __builtin_assume_aligned(g.tok.lse2 + t, 16), 16);
+                __builtin_memcpy(target + 4 * h, __builtin_assume_aligned(g.tok.target + t, 16), 16);
+            }
+            const int64_t col = j0 + wn0 + 32 * jp + lane_piece(lg);
+            uint16_t *o = g.out + (i0 + wm0 + lr) * g.ldo + col;
+#pragma unroll
+            for (int i = 0; i < SM; ++i) {
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float z = acc[i][2 * jp + (e >> 2)][e & 3];
+                    const float p = __builtin_amdgcn_exp2f(fmaf(z, kLog2e, -lse2[e])) - (target[e] == v_lane + 16 * i ? 1.f : 0.f);
+                    x[e] = scale[e] != 0.f ? scale[e] * p : 0.f;          // zero whatever p is
+                }
+                const uint4 w = pack_pair(x);
+                if (col < g.ldo) *reinterpret_cast<uint4 *>(o + (int64_t)(16 * i) * g.ldo) = w;
+            }
+        }
+    } else if constexpr (KIND == kDw) {
+#pragma unroll
+        for (int i = 0; i < SM; ++i) {
+            const int64_t row = i0 + wm0 + 16 * i + lr;
+#pragma unroll
+            for (int jp = 0; jp < SN / 2; ++jp) {
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = acc[i][2 * jp + (e >> 2)][e & 3];
+                const uint4 w = pack_pair(x);
+                const int64_t col = j0 + wn0 + 32 * jp + lane_piece(lg);
+                if (row >= g.I) continue;
+                uint16_t *o = g.out + row * g.ldo + col;
+                if (col + 8 <= g.J) {
+                    __builtin_memcpy(o, &w, 16);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (col + e < g.J) o[e] = (uint16_t)(word_of(w, e >> 1) >> (16 * (e & 1)));
+                }
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < SM; ++i) {
+            const int64_t row = i0 + wm0 + 16 * i + lr;
+#pragma unroll
+            for (int j = 0; j < SN; ++j) {
+                const int64_t col = j0 + wn0 + 16 * j + 4 * lg;
+                if (row >= g.I || col >= g.ldo) continue;
+                f32x4_t *o = reinterpret_cast<f32x4_t *>(g.acc + row * g.ldo + col);
+                f32x4_t s = acc[i][j];
+                if (!g.first) {
+                    const f32x4_t t = *o;
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) s[v] += t[v];
+                }
+                *o = s;
+            }
+        }
+    }
+}
+
+// dst[r][c] = src[r][c] for c < n, else 0, c < np (a multiple of 64).
+__global__ void __launch_bounds__(256) pad_cols_kernel(const uint16_t *src, uint16_t *dst, int64_t rows, int n, int np) {
+    const int64_t total = rows * (np / 8);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / (np / 8);
+        const int c = (int)(i - r * (np / 8)) * 8;
+        float v[8];
+        load_cols<true>(src + r * n, c, n, v);
+        store8(dst + r * np + c, v);
+    }
+}
+
+// dst[c][r] = src[r][c] for r < rows, else 0, r < ld (a multiple of 64): 64 x 64 tiles.
+__global__ void __launch_bounds__(256) transpose_kernel(const uint16_t *src, uint16_t *dst, int64_t rows, int n, int64_t ld) {
+    __shared__ uint16_t t[64][66];
+    const int64_t r0 = (int64_t)blockIdx.x * 64;
+    const int c0 = blockIdx.y * 64, tid = threadIdx.x;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const int r = (tid + 256 * q) / 8, c = (tid + 256 * q) % 8 * 8;
+        uint16_t v[8];
+        if (r0 + r < rows && c0 + c + 8 <= n) {
+            __builtin_memcpy(v, src + (r0 + r) * n + c0 + c, 16);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = r0 + r < rows && c0 + c + e < n ? src[(r0 + r) * n + c0 + c + e] : (uint16_t)0;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t[c + e][r] = v[e];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const int c = (tid + 256 * q) / 8, r = (tid + 256 * q) % 8 * 8;
+        if (c0 + c >= n) continue;
+        uint16_t v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = t[c][r + e];
+        __builtin_memcpy(__builtin_assume_aligned(dst + (int64_t)(c0 + c) * ld + r0 + r, 16), v, 16);
+    }
+}
+
+// dX[m][c] = the fp32 sums acc[c][m], rounded: 64 x 64 tiles.
+__global__ void __launch_bounds__(256) round_transpose_kernel(const float *acc, uint16_t *dst, int64_t M, int n, int64_t ld) {
+    __shared__ float t[64][65];
+    const int64_t m0 = (int64_t)blockIdx.x * 64;
+    const int c0 = blockIdx.y * 64, tid = threadIdx.x;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int c = (tid + 256 * q) / 16, m = (tid + 256 * q) % 16 * 4;
+        f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+        if (c0 + c < n) v = *reinterpret_cast<const f32x4_t *>(acc + (int64_t)(c0 + c) * ld + m0 + m);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t[m + e][c] = v[e];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const int m = (tid + 256 * q) / 8, c = (tid + 256 * q) % 8 * 8;
+        if (m0 + m >= M) continue;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = t[m][c + e];
+        store_cols<true>(dst + (m0 + m) * n, c0 + c, n, v);
+    }
+}
+
+__global__ void __launch_bounds__(256) token_kernel(LossEpi e, Token t, int64_t M, int64_t padded) {
+    const int64_t m = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (m >= padded) return;
+    float scale = 0.f, lse = 0.f;
+    int target = -1;
+    if (m < M) {
+        const int64_t v = e.targets[m];
+        if (loss_counts(e, v)) {
+            scale = loss_scale(e, m, v);
+            lse = e.lse[m];
+            target = (int)v;
+        }
+    }
+    t.scale[m] = scale;
+    t.lse2[m] = lse * kLog2e;
+    t.target[m] = target;
+}
+
+// Tiles: the widest that give the GPU's 256 CUs most of a round, else smaller ones, two to a CU.
+int tile_of(int64_t I, int64_t J) {
+    const auto count = [&](int64_t m, int64_t n) { return ((I + m - 1) / m) * ((J + n - 1) / n); };
+    if (count(256, 256) >= 128) return 0;
+    return count(128, 128) >= 128 ? 1 : 2;
+}
+int tile_bn(int t) { return t == 0 ? 256 : 128; }
+
+template <int BM, int BN, int WGM, int WGN, bool TB, Kind KIND>
+hipError_t launch_tile(Args &g, hipStream_t s) {
+    g.tiles_i = (int)((g.I + BM - 1) / BM);
+    g.tiles_j = (int)((g.J + BN - 1) / BN);
+    const int64_t tiles = (int64_t)g.tiles_i * g.tiles_j;
+    if (tiles >= (int64_t)1 << 31) return hipErrorNotSupported;
+    g.group = 8;
+    loss_pp_kernel<BM, BN, WGM, WGN, TB, KIND><<<(unsigned)tiles, kPPThreads, 0, s>>>(g);
+    return hipGetLastError();
+}
+
+template <bool TB, Kind KIND>
+hipError_t launch(Args g, hipStream_t s) {
+    switch (tile_of(g.I, g.J)) {
+    case 0: return launch_tile<256, 256, 2, 4, TB, KIND>(g, s);
+    case 1: return launch_tile<128, 128, 2, 4, TB, KIND>(g, s);
+    default: return launch_tile<64, 128, 2, 4, TB, KIND>(g, s);
+    }
+}
+
+int64_t up(int64_t v, int64_t q) { return (v + q - 1) / q * q; }
+size_t part(size_t bytes) { return (bytes + 255) / 256 * 256; }
+
+hipError_t pad_cols(const void *src, uint16_t *dst, int64_t rows, int64_t n, int64_t np, hipStream_t s) {
+    const int64_t blocks = (rows * (np / 8) + 255) / 256;
+    pad_cols_kernel<<<(unsigned)(blocks < 16384 ? blocks : 16384), 256, 0, s>>>(static_cast<const uint16_t *>(src), dst, rows,
+                                                                                (int)n, (int)np);
+    return hipGetLastError();
+}
+
+// Vocabulary columns of a piece, and the workspace of a backward pass.
+struct Layout {
+    int64_t np, Mp, Mq, Vp, vp;
+    size_t tokens, xp, wp, wt, gt, acc, total;
+};
+Layout layout_of(int64_t M, int64_t n, int64_t V) {
+    Layout l;
+    l.np = up(n, kPPK);
+    l.Mp = up(M, kPPK);
+    l.Mq = up(M, 256);
+    l.Vp = up(V, kPPK);
+    // G^T of a piece within 512 MB, but for very many tokens; pieces of one size, whole tiles
+    int64_t most = ((int64_t)512 << 20) / (2 * l.Mp) / 256 * 256;
+    if (most < 2048) most = 2048;
+    const int64_t pieces = (V + most - 1) / most;
+    l.vp = up((V + pieces - 1) / pieces, 256);
+    size_t at = 0;
+    const auto take = [&](size_t &where, size_t bytes) {
+        where = at;
+        at += part(bytes);
+    };
+    take(l.tokens, (size_t)l.Mq * 12);
+    take(l.xp, l.np != n ? (size_t)(M * l.np) * 2 : 0);
+    take(l.wp, l.np != n ? (size_t)(V * l.np) * 2 : 0);
+    take(l.wt, (size_t)(n * l.Vp) * 2);
+    take(l.gt, (size_t)(l.vp * l.Mp) * 2);
+    take(l.acc, (size_t)(n * l.Mp) * 4);
+    l.total = at;
+    return l;
+}
+
+}  // namespace
+
+int loss_mfma_tiles(int64_t M, int64_t V) {
+    const int bn = tile_bn(tile_of(M, V));
+    return (int)((V + bn - 1) / bn);
+}
+
+size_t loss_mfma_forward_bytes(int64_t M, int64_t n, int64_t V) {
+    return n % kPPK ? part((size_t)(M * up(n, kPPK)) * 2) + part((size_t)(V * up(n, kPPK)) * 2) : 0;
+}
+
+size_t loss_mfma_backward_bytes(int64_t M, int64_t n, int64_t V) { return layout_of(M, n, V).total; }
+
+hipError_t launch_loss_mfma_stats(const LossPass &p, const LossEpi &e, void *ws, hipStream_t s) {
+    Args g{};
+    g.e = e;
+    g.I = p.M;
+    g.J = p.V;
+    g.K = g.lda = g.ldb = up(p.n, kPPK);
+    g.A = static_cast<const uint16_t *>(p.X);
+    g.B = static_cast<const uint16_t *>(p.W);
+    if (g.K != p.n) {
+        uint16_t *xp = static_cast<uint16_t *>(ws);
+        uint16_t *wp = reinterpret_cast<uint16_t *>(static_cast<char *>(ws) + part((size_t)(p.M * g.K) * 2));
+        hipError_t err = pad_cols(p.X, xp, p.M, p.n, g.K, s);
+        if (err == hipSuccess) err = pad_cols(p.W, wp, p.V, p.n, g.K, s);
+        if (err != hipSuccess) return err;
+        g.A = xp;
+        g.B = wp;
+    }
+    return launch<false, kStats>(g, s);
+}
+
+hipError_t launch_loss_mfma_grad(const LossPass &p, const LossEpi &e, hipStream_t s) {
+    const Layout l = layout_of(p.M, p.n, p.V);
+    char *ws = static_cast<char *>(p.ws);
+    const auto at = [&](size_t o) { return reinterpret_cast<uint16_t *>(ws + o); };
+    Token tok;
+    tok.scale = reinterpret_cast<float *>(ws + l.tokens);
+    tok.lse2 = tok.scale + l.Mq;
+    tok.target = reinterpret_cast<int *>(tok.lse2 + l.Mq);
+    token_kernel<<<(unsigned)(l.Mq / 256), 256, 0, s>>>(e, tok, p.M, l.Mq);
+    const uint16_t *X = static_cast<const uint16_t *>(p.X), *W = static_cast<const uint16_t *>(p.W);
+    hipError_t err = hipGetLastError();
+    if (err == hipSuccess && l.np != p.n) {
+        err = pad_cols(p.X, at(l.xp), p.M, p.n, l.np, s);
+        if (err == hipSuccess) err = pad_cols(p.W, at(l.wp), p.V, p.n, l.np, s);
+        X = at(l.xp);
+        W = at(l.wp);
+    }
+    if (err == hipSuccess && p.dX) {
+        transpose_kernel<<<dim3((unsigned)(l.Vp / 64), (unsigned)(l.np / 64)), 256, 0, s>>>(
+            static_cast<const uint16_t *>(p.W), at(l.wt), p.V, (int)p.n, l.Vp);
+        err = hipGetLastError();
+    }
+    float *acc = reinterpret_cast<float *>(ws + l.acc);
+    for (int64_t v0 = 0; v0 < p.V && err == hipSuccess; v0 += l.vp) {
+        const int64_t vn = p.V - v0 < l.vp ? p.V - v0 : l.vp;
+        Args g{};
+        g.e = e;
+        g.tok = tok;
+        g.v0 = v0;
+        g.A = W + v0 * l.np;
+        g.B = X;
+        g.lda = g.ldb = g.K = l.np;
+        g.I = vn;
+        g.J = p.M;
+        g.out = at(l.gt);
+        g.ldo = l.Mp;
+        err = launch<false, kGrad>(g, s);
+        if (err == hipSuccess && p.dW) {
+            g.A = at(l.gt);
+            g.lda = g.K = l.Mp;
+            g.rows_b = p.M;
+            g.J = g.ldo = p.n;
+            g.out = static_cast<uint16_t *>(p.dW) + v0 * p.n;
+            err = launch<true, kDw>(g, s);
+        }
+        if (err == hipSuccess && p.dX) {
+            g.A = at(l.wt) + v0;
+            g.lda = l.Vp;
+            g.B = at(l.gt);
+            g.ldb = g.ldo = l.Mp;
+            g.I = p.n;
+            g.J = p.M;
+            g.K = up(vn, kPPK);
+            g.rows_b = vn;
+            g.acc = acc;
+            g.first = v0 == 0;
+            err = launch<true, kDx>(g, s);
+        }
+    }
+    if (err == hipSuccess && p.dX) {
+        round_transpose_kernel<<<dim3((unsigned)(l.Mp / 64), (unsigned)(l.np / 64)), 256, 0, s>>>(
+            acc, static_cast<uint16_t *>(p.dX), p.M, (int)p.n, l.Mp);
+        err = hipGetLastError();
+    }
+    return err;
+}
+
+}  // namespace dyad

@@ -14,7 +14,7 @@ from paper_2312_06881_amd import nn
 
 pytestmark = pytest.mark.gpu
 BF, F = torch.bfloat16, torch.float32
-DTYPES = [F]
+DTYPES = [F, BF]
 
 
 def make(M, n, V, dtype, seed=0, ignored=0.25, spread=2.0):
