@@ -337,9 +337,11 @@ typedef struct {
 int dyad_add_norm_forward(const dyad_add_norm_args *args, hipStream_t stream);
 
 /*
- * The gradients.  args is the forward call's, with what it wrote: h (read; x where y
- * was NULL and x_scale 1), stats (with a norm) and post_stats (with a post norm); x
- * and out are not read.  dh is the gradient that reaches h, dout that which reaches
+ * The gradients.  args is the forward call's, with stats (with a norm) and post_stats
+ * (with a post norm) as it wrote them.  h is formed again from x and y, or with x NULL
+ * read as the forward pass wrote it: a bf16 stream's rounding of h is then in the
+ * gradients of the norm's weights.  y's values are read where h is formed again, with a
+ * post norm, and for dgate.  out is not read.  dh is the gradient that reaches h, dout that which reaches
  * out; either may be NULL (none).  Of the results any may be NULL: dx [M][n] of
  * stream_dtype, dy [M][n] of dtype, those of the parameters (of param_dtype), dgate
  * [groups][n].  dx may be dh, and dy dout where their types agree.  The workspace holds

@@ -247,7 +247,19 @@ __device__ __forceinline__ void flush(float (&acc)[NV][8], float *dst, int npad,
         for (int e = 0; e < 8; ++e) acc[q][e] = 0.f;
 }
 
-// FULL: there is a post norm or a gate whose gradient is wanted, so y is read.
+template <class TS, class TB, int NV>
+struct Row {
+    Raw<TS> h[NV], dh[NV];
+    Raw<TB> g[NV], y[NV];
+    float2 st, ps;
+};
+
+// FULL: there is a post norm or a gate whose gradient is wanted.  h is read, or with x given
+// formed again from x and y: as rounded to a bf16 stream it would put 2^-8 of each of its values
+// into u, and so into dw (2.5e-3 off 64 bits in place of bf16's own 1.7e-3, or with fp32
+// parameters 1.7e-3 in place of 1e-7).  16384 tokens of 768 in bf16: 37 us for the 151 MB of dh,
+// dout, x, y, dx, dy (29 us at a large copy's rate); rows loaded one ahead and kept as they lie in
+// memory, 71 us without.
 template <class TS, class TB, int TPR, int NV, bool FULL, bool RAG>
 __global__ void __launch_bounds__(threads_of(TPR)) add_norm_grad_kernel(Norm a) {
     __shared__ float2 lds[TPR > 64 ? 2 * (TPR / 64) : 1];
@@ -255,7 +267,25 @@ __global__ void __launch_bounds__(threads_of(TPR)) add_norm_grad_kernel(Norm a) 
     TeamSum<TPR> sum{lds, 0};
     const int lane = threadIdx.x % TPR, team = threadIdx.x / TPR, n = a.n, c0 = lane * 8;
     const bool pf32 = a.p.param_dtype == kF32;
+    const bool again = a.p.x != nullptr, reads_y = FULL || (again && a.p.y != nullptr && a.p.dout != nullptr);
     const uint64_t offset = a.drop ? drop_offset(a.d) : 0;
+    const auto fetch = [&](int64_t row) __attribute__((always_inline)) {
+        Row<TS, TB, NV> r;
+#pragma unroll
+        for (int q = 0; q < NV; ++q) {
+            const int c = c0 + q * 8 * TPR;
+            if (a.p.dout) {
+                r.h[q] = load_raw<RAG>(static_cast<const TS *>(again ? a.p.x : a.p.h) + row * n, c, n);
+                r.g[q] = load_raw<RAG>(static_cast<const TB *>(a.p.dout) + row * n, c, n);
+            }
+            if (reads_y) r.y[q] = load_raw<RAG>(static_cast<const TB *>(a.p.y) + row * n, c, n);
+            if (a.p.dh) r.dh[q] = load_raw<RAG>(static_cast<const TS *>(a.p.dh) + row * n, c, n);
+            else r.dh[q] = Raw<TS>{};
+        }
+        if (a.p.dout) r.st = reinterpret_cast<const float2 *>(a.p.stats)[row];
+        if (FULL && a.p.post != kNormNone) r.ps = reinterpret_cast<const float2 *>(a.p.post_stats)[row];
+        return r;
+    };
     float dw[NV][8] = {}, db[NV][8] = {};
     float dpw[FULL ? NV : 1][8] = {}, dpb[FULL ? NV : 1][8] = {}, dgate[FULL ? NV : 1][8] = {};
     const int64_t u1 = (int64_t)(blockIdx.x + 1) * a.units / gridDim.x;
@@ -263,33 +293,77 @@ __global__ void __launch_bounds__(threads_of(TPR)) add_norm_grad_kernel(Norm a) 
         const int64_t group = unit / a.per_group, piece = unit - group * a.per_group;
         const int64_t first = group * a.unit_rows + piece * a.unit_rows / a.per_group;
         const int64_t last = group * a.unit_rows + (piece + 1) * a.unit_rows / a.per_group;
+        // a row's operands are loaded while the row before it is worked on, and wait as they lie in memory
+        Row<TS, TB, NV> next;
+        if (first + team < last) next = fetch(first + team);
         for (int64_t row = first + team; row < last; row += teams_of(TPR)) {
+            const Row<TS, TB, NV> cur = next;
+            next = fetch(row + teams_of(TPR) < last ? row + teams_of(TPR) : row);
             float g[NV][8], u[NV][8];
-            float y[FULL ? NV : 1][8];
-            if constexpr (FULL) {
-                const TB *yr = static_cast<const TB *>(a.p.y) + row * n;
+            uint32_t keep[NV];
+            const int64_t grow = a.p.gate && a.p.groups > 1 ? row / a.rows_per_gate : 0;
+            if (a.drop) {
 #pragma unroll
-                for (int q = 0; q < NV; ++q) load_cols<RAG>(yr, c0 + q * 8 * TPR, n, y[q]);
+                for (int q = 0; q < NV; ++q) {
+                    const int c = c0 + q * 8 * TPR;
+                    keep[q] = c < n ? keep_bits(philox(a.d.seed, offset, (uint64_t)(row * a.octets + (c >> 3))), a.d.thr) : 0;
+                }
             }
-            float dh[NV][8];
-            if (a.p.dh) {
-                const TS *r = static_cast<const TS *>(a.p.dh) + row * n;
+            const float2 ps = cur.ps;
+            // y of eight columns, normed where there is a post norm, without and with its weights
+            const auto unit_y = [&](int q, float (&z)[8]) __attribute__((always_inline)) {
+                unpack8(cur.y[q], z);
+                if (FULL && a.p.post != kNormNone) {
 #pragma unroll
-                for (int q = 0; q < NV; ++q) load_cols<RAG>(r, c0 + q * 8 * TPR, n, dh[q]);
+                    for (int e = 0; e < 8; ++e)
+                        z[e] = c0 + q * 8 * TPR + (RAG ? e : 0) < n ? (z[e] - ps.x) * ps.y : 0.f;
+                }
+            };
+            const auto post_y = [&](int q, float (&z)[8]) __attribute__((always_inline)) {
+                const int c = c0 + q * 8 * TPR;
+                unit_y(q, z);
+                if constexpr (FULL) {
+                    float t[8];
+                    if (a.p.pw) {
+                        load_param<RAG>(a.p.pw, pf32, 0, c, n, t);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) z[e] *= t[e];
+                    }
+                    if (a.p.pb) {
+                        load_param<RAG>(a.p.pb, pf32, 0, c, n, t);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) z[e] += t[e];
+                    }
+                }
+            };
+            if (a.p.dout) {
+#pragma unroll
+                for (int q = 0; q < NV; ++q) {
+                    unpack8(cur.h[q], u[q]);
+                    unpack8(cur.g[q], g[q]);
+                }
             }
             if (a.p.dout) {
-                const TB *dr = static_cast<const TB *>(a.p.dout) + row * n;
-                const TS *hr = static_cast<const TS *>(a.p.h) + row * n;
-                const float2 st = reinterpret_cast<const float2 *>(a.p.stats)[row];
+                const float2 st = cur.st;
 #pragma unroll
                 for (int q = 0; q < NV; ++q) {
                     const int c = c0 + q * 8 * TPR;
-                    load_cols<RAG>(dr, c, n, g[q]);
-                    load_cols<RAG>(hr, c, n, u[q]);
-                }
+                    if (again) {
 #pragma unroll
-                for (int q = 0; q < NV; ++q) {
-                    const int c = c0 + q * 8 * TPR;
+                        for (int e = 0; e < 8; ++e) u[q][e] *= a.p.x_scale;
+                        if (a.p.y) {
+                            float z[8], t[8];
+                            post_y(q, z);
+                            if (a.drop) apply_drop(z, keep[q], a.d.scale);
+                            if (a.p.gate) {
+                                load_param<RAG>(a.p.gate, pf32, grow, c, n, t);
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) z[e] *= t[e];
+                            }
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) u[q][e] = fmaf(z[e], a.p.y_scale, u[q][e]);
+                        }
+                    }
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         u[q][e] = (u[q][e] - st.x) * st.y;
@@ -306,15 +380,16 @@ __global__ void __launch_bounds__(threads_of(TPR)) add_norm_grad_kernel(Norm a) 
                 norm_grad<TPR, NV>(g, u, st.y, a.p.norm, n, sum);
                 if (a.p.dh) {
 #pragma unroll
-                    for (int q = 0; q < NV; ++q)
+                    for (int q = 0; q < NV; ++q) {
+                        float t[8];
+                        unpack8(cur.dh[q], t);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) g[q][e] += dh[q][e];
+                        for (int e = 0; e < 8; ++e) g[q][e] += t[e];
+                    }
                 }
             } else {
 #pragma unroll
-                for (int q = 0; q < NV; ++q)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) g[q][e] = a.p.dh ? dh[q][e] : 0.f;
+                for (int q = 0; q < NV; ++q) unpack8(cur.dh[q], g[q]);   // zero where there is none
             }
             if (a.p.dx) {
                 TS *dx = static_cast<TS *>(a.p.dx) + row * n;
@@ -327,34 +402,19 @@ __global__ void __launch_bounds__(threads_of(TPR)) add_norm_grad_kernel(Norm a) 
                 }
             }
             if (!FULL && !a.p.dy) continue;
-            float2 ps = make_float2(0.f, 1.f);
-            if (FULL && a.p.post != kNormNone) ps = reinterpret_cast<const float2 *>(a.p.post_stats)[row];
-            const int64_t grow = a.p.gate && a.p.groups > 1 ? row / a.rows_per_gate : 0;
 #pragma unroll
             for (int q = 0; q < NV; ++q) {
                 const int c = c0 + q * 8 * TPR;
-                float pw[8];
-                const bool scaled = FULL && a.p.post != kNormNone && a.p.pw;
-                if (scaled) load_param<RAG>(a.p.pw, pf32, 0, c, n, pw);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) g[q][e] = c + e < n ? g[q][e] * a.p.y_scale : 0.f;
-                if (a.drop && c < n)
-                    apply_drop(g[q], keep_bits(philox(a.d.seed, offset, (uint64_t)(row * a.octets + (c >> 3))), a.d.thr),
-                               a.d.scale);
+                for (int e = 0; e < 8; ++e) g[q][e] = c + (RAG ? e : 0) < n ? g[q][e] * a.p.y_scale : 0.f;
+                if (a.drop) apply_drop(g[q], keep[q], a.d.scale);
                 if constexpr (FULL) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) u[q][e] = c + e < n ? (y[q][e] - ps.x) * ps.y : 0.f;
                     if (a.gpart) {
-                        float z[8], pb[8];
-                        const bool shifted = a.p.post != kNormNone && a.p.pb;
-                        if (shifted) load_param<RAG>(a.p.pb, pf32, 0, c, n, pb);
+                        float z[8];
+                        post_y(q, z);
+                        // what is dropped counts for nothing, whatever it was
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            z[e] = scaled ? u[q][e] * pw[e] : u[q][e];
-                            if (shifted) z[e] += pb[e];
-                            // what is dropped counts for nothing, whatever it was
-                            dgate[q][e] += g[q][e] != 0.f ? g[q][e] * z[e] : 0.f;
-                        }
+                        for (int e = 0; e < 8; ++e) dgate[q][e] += g[q][e] != 0.f ? g[q][e] * z[e] : 0.f;
                     }
                 }
                 if (a.p.gate) {
@@ -365,11 +425,17 @@ __global__ void __launch_bounds__(threads_of(TPR)) add_norm_grad_kernel(Norm a) 
                 }
                 if constexpr (FULL) {
                     if (a.p.post != kNormNone) {
+                        unit_y(q, u[q]);           // the stream's u has had its turn
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
                             dpb[q][e] += g[q][e];
                             dpw[q][e] = fmaf(g[q][e], u[q][e], dpw[q][e]);
-                            if (scaled) g[q][e] *= pw[e];
+                        }
+                        if (a.p.pw) {
+                            float t[8];
+                            load_param<RAG>(a.p.pw, pf32, 0, c, n, t);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) g[q][e] *= t[e];
                         }
                     }
                 }
@@ -423,14 +489,14 @@ __global__ void __launch_bounds__(1024) add_norm_sum_kernel(Sums s) {
     }
 }
 
-// Threads and vectors of a row: a wave as far as 16 columns a thread go, then more waves.
-// With a post norm or a gate's gradient five sums over rows share the registers with a row's
-// operands, and a thread takes 8 columns.
+// Threads and vectors of a row.  Forward: a wave as far as 16 columns a thread go, then more
+// waves.  In the backward pass the sums over rows share the registers with a row's operands, and
+// a thread takes 8 columns.
 struct Shape {
     int tpr, nv;
 };
-Shape shape_of(int64_t n, bool full) {
-    const int64_t per = full ? 8 : 16;
+Shape shape_of(int64_t n, bool backward) {
+    const int64_t per = backward ? 8 : 16;
     int tpr = 64;
     while (tpr < 1024 && tpr * per < n) tpr *= 2;
     return {tpr, tpr * 8 < n ? 2 : 1};
@@ -446,11 +512,11 @@ Plan plan_of(const AddNormPass &p) {
     l.npad = (p.n + 7) / 8 * 8;
     l.gate = p.y && p.gate && p.dgate;
     l.full = p.y && (p.post != kNormNone || l.gate);
-    const Shape sh = shape_of(p.n, l.full);
+    const Shape sh = shape_of(p.n, true);
     const int64_t teams = teams_of(sh.tpr);
-    // two rows a team at least, and no more workgroups than the GPU holds at once
-    int64_t most = 256 * (1024 / threads_of(sh.tpr));
-    if (most > 768) most = 768;
+    // two rows a team at least, and no more workgroups than the GPU holds at once: 3 waves a
+    // SIMD, or 2 with the sums of a post norm (rows loaded ahead, so more would not help)
+    const int64_t most = 1024 * (l.full ? 2 : 3) / (threads_of(sh.tpr) / 64);
     int64_t want = (p.M + 2 * teams - 1) / (2 * teams);
     if (want > most) want = most;
     if (want < 1) want = 1;
@@ -470,37 +536,33 @@ void run_fwd(const Norm &a, hipStream_t s) {
     add_norm_kernel<TS, TB, TPR, NV, RAG><<<grid, threads_of(TPR), 0, s>>>(a);
 }
 
-template <class TS, class TB, int TPR, int NV, bool FULL, bool RAG>
+template <class TS, class TB, int TPR, int NV, bool RAG>
 void run_bwd(const Norm &a, const Plan &l, hipStream_t s) {
-    add_norm_grad_kernel<TS, TB, TPR, NV, FULL, RAG><<<(unsigned)l.grid, threads_of(TPR), 0, s>>>(a);
+    if (l.full) add_norm_grad_kernel<TS, TB, TPR, NV, true, RAG><<<(unsigned)l.grid, threads_of(TPR), 0, s>>>(a);
+    else add_norm_grad_kernel<TS, TB, TPR, NV, false, RAG><<<(unsigned)l.grid, threads_of(TPR), 0, s>>>(a);
 }
 
 template <class TS, class TB, bool RAG>
 hipError_t run(const Norm &a, const Plan *l, hipStream_t s) {
-    const bool full = l && l->full;
-    const Shape sh = shape_of(a.n, full);
-    const auto is = [&](int tpr, int nv) { return sh.tpr == tpr && sh.nv == nv; };
-    if (!l) {
-        if (is(64, 1)) run_fwd<TS, TB, 64, 1, RAG>(a, s);
-        else if (is(64, 2)) run_fwd<TS, TB, 64, 2, RAG>(a, s);
-        else if (is(128, 2)) run_fwd<TS, TB, 128, 2, RAG>(a, s);
-        else if (is(256, 2)) run_fwd<TS, TB, 256, 2, RAG>(a, s);
-        else if (is(512, 2)) run_fwd<TS, TB, 512, 2, RAG>(a, s);
-        else run_fwd<TS, TB, 1024, 2, RAG>(a, s);
-    } else if (full) {
-        if (is(64, 1)) run_bwd<TS, TB, 64, 1, true, RAG>(a, *l, s);
-        else if (is(128, 1)) run_bwd<TS, TB, 128, 1, true, RAG>(a, *l, s);
-        else if (is(256, 1)) run_bwd<TS, TB, 256, 1, true, RAG>(a, *l, s);
-        else if (is(512, 1)) run_bwd<TS, TB, 512, 1, true, RAG>(a, *l, s);
-        else if (is(1024, 1)) run_bwd<TS, TB, 1024, 1, true, RAG>(a, *l, s);
-        else run_bwd<TS, TB, 1024, 2, true, RAG>(a, *l, s);
+    const Shape sh = shape_of(a.n, l != nullptr);
+    if (l) {
+        switch (sh.tpr * sh.nv) {
+        case 64: run_bwd<TS, TB, 64, 1, RAG>(a, *l, s); break;
+        case 128: run_bwd<TS, TB, 128, 1, RAG>(a, *l, s); break;
+        case 256: run_bwd<TS, TB, 256, 1, RAG>(a, *l, s); break;
+        case 512: run_bwd<TS, TB, 512, 1, RAG>(a, *l, s); break;
+        case 1024: run_bwd<TS, TB, 1024, 1, RAG>(a, *l, s); break;
+        default: run_bwd<TS, TB, 1024, 2, RAG>(a, *l, s);
+        }
     } else {
-        if (is(64, 1)) run_bwd<TS, TB, 64, 1, false, RAG>(a, *l, s);
-        else if (is(64, 2)) run_bwd<TS, TB, 64, 2, false, RAG>(a, *l, s);
-        else if (is(128, 2)) run_bwd<TS, TB, 128, 2, false, RAG>(a, *l, s);
-        else if (is(256, 2)) run_bwd<TS, TB, 256, 2, false, RAG>(a, *l, s);
-        else if (is(512, 2)) run_bwd<TS, TB, 512, 2, false, RAG>(a, *l, s);
-        else run_bwd<TS, TB, 1024, 2, false, RAG>(a, *l, s);
+        switch (sh.tpr * sh.nv) {
+        case 64: run_fwd<TS, TB, 64, 1, RAG>(a, s); break;
+        case 128: run_fwd<TS, TB, 64, 2, RAG>(a, s); break;
+        case 256: run_fwd<TS, TB, 128, 2, RAG>(a, s); break;
+        case 512: run_fwd<TS, TB, 256, 2, RAG>(a, s); break;
+        case 1024: run_fwd<TS, TB, 512, 2, RAG>(a, s); break;
+        default: run_fwd<TS, TB, 1024, 2, RAG>(a, s);
+        }
     }
     return hipGetLastError();
 }

@@ -100,7 +100,7 @@ int dyad_add_norm_backward(const dyad_add_norm_args *args, const dyad_add_norm_g
     const int rc = norm_pass(args, grads, p);
     if (rc) return rc;
     if (p.M > 0) {
-        if (p.dout && (!p.h || !p.stats)) return DYAD_ERR_INVALID_ARG;
+        if (p.dout && ((!p.h && !p.x) || !p.stats)) return DYAD_ERR_INVALID_ARG;
         if (p.post != DYAD_NORM_NONE && !p.post_stats) return DYAD_ERR_INVALID_ARG;
     }
     if (!aligned16(workspace)) return DYAD_ERR_ALIGN;

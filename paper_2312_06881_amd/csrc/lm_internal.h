@@ -153,7 +153,12 @@ hipError_t launch_loss_f32_piece(const LossPass &p, const LossEpi &e, int64_t v0
 int loss_mfma_tiles(int64_t M, int64_t V);
 size_t loss_mfma_forward_bytes(int64_t M, int64_t n, int64_t V);
 size_t loss_mfma_backward_bytes(int64_t M, int64_t n, int64_t V);
-hipError_t launch_loss_mfma_stats(const LossPass &p, const LossEpi &e, void *ws, hipStream_t s);
+// Which token row c of the statistics is, and how many rows there are; null: c, and all.
+struct LossTokens {
+    const int *idx, *count;
+};
+hipError_t launch_loss_mfma_stats(const LossPass &p, const LossEpi &e, void *ws, float *each, LossTokens &tokens,
+                                  hipStream_t s);
 hipError_t launch_loss_mfma_grad(const LossPass &p, const LossEpi &e, hipStream_t s);
 
 }  // namespace dyad

@@ -12,17 +12,19 @@ namespace dyad {
 namespace {
 
 // A wave a token: joins the tiles' statistics.
-__global__ void __launch_bounds__(256) loss_join_kernel(LossEpi e, int64_t M, float *loss, float *lse) {
+__global__ void __launch_bounds__(256) loss_join_kernel(LossEpi e, int64_t M, LossTokens tokens, float *loss, float *lse) {
     const int lane = threadIdx.x & 63;
-    for (int64_t m = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); m < M; m += (int64_t)gridDim.x * 4) {
+    if (tokens.count) M = *tokens.count;
+    for (int64_t c = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); c < M; c += (int64_t)gridDim.x * 4) {
+        const int64_t m = tokens.idx ? tokens.idx[c] : c;
         float2 s = make_float2(-INFINITY, 0.f);
-        for (int t = lane; t < e.tiles; t += 64) s = join_stats(s, e.part[m * e.tiles + t]);
+        for (int t = lane; t < e.tiles; t += 64) s = join_stats(s, e.part[c * e.tiles + t]);
 #pragma unroll
         for (int w = 32; w > 0; w >>= 1) s = join_stats(s, make_float2(__shfl_xor(s.x, w), __shfl_xor(s.y, w)));
         if (lane == 0) {
             const float l = s.x + logf(s.y);
             lse[m] = l;
-            loss[m] = loss_counts(e, e.targets[m]) ? l - e.at_target[m] : 0.f;
+            loss[m] = loss_counts(e, e.targets[m]) ? l - e.at_target[c] : 0.f;
         }
     }
 }
@@ -106,11 +108,13 @@ hipError_t launch_loss_forward(const LossPass &p, hipStream_t s) {
         if (p.reduction == kReduceNone) each = p.loss;
         const bool f32 = p.dtype == kF32;
         e.tiles = f32 ? loss_f32_tiles(p.M, p.V) : loss_mfma_tiles(p.M, p.V);
+        LossTokens tokens{};
         const hipError_t err = f32 ? launch_loss_f32_stats(p, e, s)
-                                   : launch_loss_mfma_stats(p, e, static_cast<char *>(p.ws) + stats_bytes(p.M, e.tiles), s);
+                                   : launch_loss_mfma_stats(p, e, static_cast<char *>(p.ws) + stats_bytes(p.M, e.tiles), each,
+                                                            tokens, s);
         if (err != hipSuccess) return err;
         const int64_t blocks = (p.M + 3) / 4;
-        loss_join_kernel<<<(unsigned)(blocks < 8192 ? blocks : 8192), 256, 0, s>>>(e, p.M, each, p.lse);
+        loss_join_kernel<<<(unsigned)(blocks < 8192 ? blocks : 8192), 256, 0, s>>>(e, p.M, tokens, each, p.lse);
     }
     if (p.reduction != kReduceNone)
         loss_sum_kernel<<<1, 1024, 0, s>>>(e, p.M, each, p.reduction == kReduceMean, p.loss, p.count);

@@ -7,6 +7,10 @@
 // transposed out of LDS), so one copy of G serves both products.  What they need laid out
 // otherwise is laid out once a call: W^T, and X and W with rows of whole 64s where n is not.
 // Padded reduction indices are zero on one side and finite on the other.
+//
+// Tokens that do not count take no part: from kCompactFrom tokens the others are gathered, in
+// order, and the kernels take their number from device memory (prompts and padding are often half
+// of a batch: 3001 tokens of 1000 over 50021, half of them counting, 1.87 -> 0.75 ms a step).
 #include "lm_internal.h"
 #include "pp_core.h"
 #include "row_io.h"
@@ -27,7 +31,9 @@ struct Args {
     const uint16_t *A, *B;
     int64_t lda, ldb, I, J, K;   // K: a multiple of 64
     int64_t rows_b;              // side B's rows where they are the reduction's indices
-    int tiles_i, tiles_j, group;
+    int group;
+    int splits;                  // kDx: of the reduction, each into an acc of its own
+    const int *count;            // tokens, in place of the side that runs over them; null: as given
     LossEpi e;
     Token tok;
     int64_t v0;
@@ -76,15 +82,31 @@ __global__ void __launch_bounds__(kPPThreads, 1) loss_pp_kernel(Args g) {
     lds_u8 *lds = (lds_u8 *)smem;
     const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    // runs of `group` panels of side A, side A fastest
-    const int item = xcd_tile(blockIdx.x, g.tiles_i * g.tiles_j), run = g.group * g.tiles_j;
-    const int first = item / run * g.group;
-    const int gm = g.tiles_i - first < g.group ? g.tiles_i - first : g.group;
+    if (g.count) {
+        const int64_t tokens = *g.count;
+        if (KIND == kStats) g.I = tokens;
+        if (KIND == kGrad || KIND == kDx) g.J = tokens;
+        if (KIND == kDw) {
+            g.K = (tokens + kPPK - 1) / kPPK * kPPK;
+            g.rows_b = tokens;
+        }
+    }
+    const int tiles_i = (int)((g.I + BM - 1) / BM), tiles_j = (int)((g.J + BN - 1) / BN), tiles = tiles_i * tiles_j;
+    if ((int)blockIdx.x >= tiles * g.splits) return;
+    // runs of `group` panels of side A, side A fastest: the workgroups that run together on an
+    // XCD share both sides
+    int item = xcd_tile(blockIdx.x, tiles * g.splits);
+    const int split = KIND == kDx ? item / tiles : 0;
+    item -= split * tiles;
+    const int run = g.group * tiles_j, first = item / run * g.group;
+    const int gm = tiles_i - first < g.group ? tiles_i - first : g.group;
     const int64_t i0 = (int64_t)(first + item % run % gm) * BM;
     const int tile_j = item % run / gm;
     const int64_t j0 = (int64_t)tile_j * BN;
     const int64_t left_i = g.I - i0 < BM ? g.I - i0 : BM, left_j = g.J - j0 < BN ? g.J - j0 : BN;
-    const int units = (int)(g.K / kPPK);
+    const int all = (int)(g.K / kPPK);
+    const int u0 = KIND == kDx ? (int)((int64_t)all * split / g.splits) : 0;
+    const int units = (KIND == kDx ? (int)((int64_t)all * (split + 1) / g.splits) : all) - u0;
 
     const __amdgpu_buffer_rsrc_t rA = buffer_rsrc(g.A + i0 * g.lda, (uint32_t)(left_i * g.lda * 2));
     const __amdgpu_buffer_rsrc_t rB0 = buffer_rsrc(g.B + j0 * g.ldb, TB ? 0u : (uint32_t)(left_j * g.ldb * 2));
@@ -105,7 +127,7 @@ __global__ void __launch_bounds__(kPPThreads, 1) loss_pp_kernel(Args g) {
         voB[q] = (uint32_t)row * (uint32_t)g.ldb * 2u + (uint32_t)byte;
         loB[q] = (uint32_t)C::kOffB + 1024u * (uint32_t)i;
     }
-    const auto clamp = [&](int d) { return d < units ? d : units - 1; };
+    const auto clamp = [&](int d) { return u0 + (d < units ? d : units - 1); };
     auto issue_a = [&](int d) {
         lds_u8 *slot = lds + d % C::kSlotA * SA::kBytes;
         const uint32_t so = (uint32_t)clamp(d) * (uint32_t)(2 * kPPK);
@@ -144,8 +166,9 @@ __global__ void __launch_bounds__(kPPThreads, 1) loss_pp_kernel(Args g) {
     for (int i = 0; i < SM; ++i)
 #pragma unroll
         for (int j = 0; j < SN; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    pp_loop<SM, SN, TB, 4 * SB::kPitch, SA::kPer, SB::kPer, C::kSlotA, C::kSlotB>(units, wave, acc, issue_a, issue_b, addr,
-                                                                                [](int) { return true; });
+    if (units > 0)
+        pp_loop<SM, SN, TB, 4 * SB::kPitch, SA::kPer, SB::kPer, C::kSlotA, C::kSlotB>(units, wave, acc, issue_a, issue_b,
+                                                                                    addr, [](int) { return true; });
     // acc[i][j][v]: side A's row wm0 + 16 i + lr, side B's wn0 + 16 j + 4 lg + v
     if constexpr (KIND == kStats) {
         loss_stats<SM, SN, BM, WGN>(g.e, acc, i0, g.I, j0, tile_j, wm0, wn0, wave % WGN, reinterpret_cast<float2 *>(smem));
@@ -174,7 +197,7 @@ __global__ void __launch_bounds__(kPPThreads, 1) loss_pp_kernel(Args g) {
                     x[e] = scale[e] != 0.f ? scale[e] * p : 0.f;          // zero whatever p is
                 }
                 const uint4 w = pack_pair(x);
-                if (col < g.ldo) *reinterpret_cast<uint4 *>(o + (int64_t)(16 * i) * g.ldo) = w;
+                if (col < g.ldo && i0 + wm0 + 16 * i + lr < g.I) *reinterpret_cast<uint4 *>(o + (int64_t)(16 * i) * g.ldo) = w;
             }
         }
     } else if constexpr (KIND == kDw) {
@@ -207,7 +230,7 @@ __global__ void __launch_bounds__(kPPThreads, 1) loss_pp_kernel(Args g) {
             for (int j = 0; j < SN; ++j) {
                 const int64_t col = j0 + wn0 + 16 * j + 4 * lg;
                 if (row >= g.I || col >= g.ldo) continue;
-                f32x4_t *o = reinterpret_cast<f32x4_t *>(g.acc + row * g.ldo + col);
+                f32x4_t *o = reinterpret_cast<f32x4_t *>(g.acc + ((int64_t)split * g.I + row) * g.ldo + col);
                 f32x4_t s = acc[i][j];
                 if (!g.first) {
                     const f32x4_t t = *o;
@@ -220,15 +243,58 @@ __global__ void __launch_bounds__(kPPThreads, 1) loss_pp_kernel(Args g) {
     }
 }
 
-// dst[r][c] = src[r][c] for c < n, else 0, c < np (a multiple of 64).
-__global__ void __launch_bounds__(256) pad_cols_kernel(const uint16_t *src, uint16_t *dst, int64_t rows, int n, int np) {
+// The tokens that count, in order: their places idx, their targets and how many; the others'
+// loss and lse are zero (forward).  One workgroup, a run of tokens a thread.
+__global__ void __launch_bounds__(1024) compact_kernel(LossEpi e, int64_t M, int *idx, int64_t *targets, int *count,
+                                                       float *loss, float *lse) {
+    __shared__ int sums[16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t per = (M + 1023) / 1024, m0 = tid * per, m1 = m0 + per < M ? m0 + per : M;
+    int n = 0;
+    for (int64_t m = m0; m < m1; ++m) n += loss_counts(e, e.targets[m]) ? 1 : 0;
+    int before = n;
+#pragma unroll
+    for (int w = 1; w < 64; w <<= 1) {
+        const int t = __shfl_up(before, w);
+        if (lane >= w) before += t;
+    }
+    if (lane == 63) sums[wave] = before;
+    __syncthreads();
+    before -= n;
+    for (int w = 0; w < wave; ++w) before += sums[w];
+    if (tid == 1023) *count = before + n;
+    for (int64_t m = m0; m < m1; ++m) {
+        const int64_t t = e.targets[m];
+        if (loss_counts(e, t)) {
+            idx[before] = (int)m;
+            targets[before++] = t;
+        } else if (loss) {
+            loss[m] = 0.f;
+            lse[m] = 0.f;
+        }
+    }
+}
+
+// dst[r][c] = src[idx[r]][c] for c < n, else 0, c < np (a multiple of 64).  idx null: row r;
+// count null: all rows.
+__global__ void __launch_bounds__(256) gather_kernel(const uint16_t *src, uint16_t *dst, int64_t rows, int n, int np,
+                                                     const int *idx, const int *count) {
+    if (count) rows = *count;
     const int64_t total = rows * (np / 8);
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
         const int64_t r = i / (np / 8);
         const int c = (int)(i - r * (np / 8)) * 8;
         float v[8];
-        load_cols<true>(src + r * n, c, n, v);
+        load_cols<true>(src + (idx ? idx[r] : r) * n, c, n, v);
         store8(dst + r * np + c, v);
+    }
+}
+
+// Rows of tokens that do not count: their gradient is zero.
+__global__ void __launch_bounds__(256) zero_rows_kernel(LossEpi e, uint16_t *dx, int64_t M, int n) {
+    for (int64_t m = blockIdx.x; m < M; m += gridDim.x) {
+        if (loss_counts(e, e.targets[m])) continue;
+        for (int c = threadIdx.x; c < n; c += 256) dx[m * n + c] = 0;
     }
 }
 
@@ -262,16 +328,27 @@ __global__ void __launch_bounds__(256) transpose_kernel(const uint16_t *src, uin
     }
 }
 
-// dX[m][c] = the fp32 sums acc[c][m], rounded: 64 x 64 tiles.
-__global__ void __launch_bounds__(256) round_transpose_kernel(const float *acc, uint16_t *dst, int64_t M, int n, int64_t ld) {
+// dX[idx[m]][c] = the fp32 sums acc[split][c][m], added in order and rounded: 64 x 64 tiles.
+__global__ void __launch_bounds__(256) round_transpose_kernel(const float *acc, int splits, uint16_t *dst, int64_t M, int n,
+                                                              int64_t ld, const int *idx, const int *count) {
     __shared__ float t[64][65];
+    if (count) M = *count;
     const int64_t m0 = (int64_t)blockIdx.x * 64;
     const int c0 = blockIdx.y * 64, tid = threadIdx.x;
+    if (m0 >= M) return;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         const int c = (tid + 256 * q) / 16, m = (tid + 256 * q) % 16 * 4;
         f32x4_t v = {0.f, 0.f, 0.f, 0.f};
-        if (c0 + c < n) v = *reinterpret_cast<const f32x4_t *>(acc + (int64_t)(c0 + c) * ld + m0 + m);
+        if (c0 + c < n) {
+            const float *src = acc + (int64_t)(c0 + c) * ld + m0 + m;
+            v = *reinterpret_cast<const f32x4_t *>(src);
+            for (int s = 1; s < splits; ++s) {
+                const f32x4_t u = *reinterpret_cast<const f32x4_t *>(src + (int64_t)s * n * ld);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += u[e];
+            }
+        }
 #pragma unroll
         for (int e = 0; e < 4; ++e) t[m + e][c] = v[e];
     }
@@ -283,41 +360,65 @@ __global__ void __launch_bounds__(256) round_transpose_kernel(const float *acc, 
         float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = t[m][c + e];
-        store_cols<true>(dst + (m0 + m) * n, c0 + c, n, v);
+        store_cols<true>(dst + (idx ? idx[m0 + m] : m0 + m) * n, c0 + c, n, v);
     }
 }
 
-__global__ void __launch_bounds__(256) token_kernel(LossEpi e, Token t, int64_t M, int64_t padded) {
-    const int64_t m = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (m >= padded) return;
+__global__ void __launch_bounds__(256) token_kernel(LossEpi e, Token t, int64_t M, int64_t padded, const int *idx,
+                                                    const int *count) {
+    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (c >= padded) return;
+    if (count) M = *count;
     float scale = 0.f, lse = 0.f;
     int target = -1;
-    if (m < M) {
-        const int64_t v = e.targets[m];
+    if (c < M) {
+        const int64_t m = idx ? idx[c] : c, v = e.targets[m];
         if (loss_counts(e, v)) {
             scale = loss_scale(e, m, v);
             lse = e.lse[m];
             target = (int)v;
         }
     }
-    t.scale[m] = scale;
-    t.lse2[m] = lse * kLog2e;
-    t.target[m] = target;
+    t.scale[c] = scale;
+    t.lse2[c] = lse * kLog2e;
+    t.target[c] = target;
 }
 
-// Tiles: the widest that give the GPU's 256 CUs most of a round, else smaller ones, two to a CU.
-int tile_of(int64_t I, int64_t J) {
-    const auto count = [&](int64_t m, int64_t n) { return ((I + m - 1) / m) * ((J + n - 1) / n); };
-    if (count(256, 256) >= 128) return 0;
-    return count(128, 128) >= 128 ? 1 : 2;
+// Tiles: rows of side A and B, and the time of a round of them next to 256 x 256's, with one, two
+// or three workgroups on every CU (measured at 768, 1000 and 4096 wide; the wide ones fill a CU).
+struct Tile {
+    int bm, bn, per_cu;
+    double time[3];
+};
+constexpr Tile kTiles[] = {
+    {256, 256, 1, {1.0}}, {192, 256, 1, {0.85}}, {128, 128, 2, {0.36, 0.62}}, {64, 128, 3, {0.22, 0.38, 0.54}}};
+
+struct Choice {
+    int tile, splits;
+};
+// The tile of least time over 256 CUs, and with `most_splits` above 1 the reduction's splits,
+// where the tiles alone leave CUs idle.
+Choice choose(int64_t I, int64_t J, int64_t most_splits = 1) {
+    Choice best{0, 1};
+    double least = 0;
+    for (int t = 0; t < 4; ++t) {
+        const Tile &k = kTiles[t];
+        const int64_t tiles = ((I + k.bm - 1) / k.bm) * ((J + k.bn - 1) / k.bn);
+        int64_t splits = 256 / tiles;
+        splits = splits > most_splits ? most_splits : splits < 1 ? 1 : splits;
+        const int64_t count = tiles * splits, round = 256 * k.per_cu, rest = (count % round + 255) / 256;
+        const double time = ((double)(count / round) * k.time[k.per_cu - 1] + (rest ? k.time[rest - 1] : 0.0)) / (double)splits;
+        if (t == 0 || time < least) {
+            best = {t, (int)splits};
+            least = time;
+        }
+    }
+    return best;
 }
-int tile_bn(int t) { return t == 0 ? 256 : 128; }
 
 template <int BM, int BN, int WGM, int WGN, bool TB, Kind KIND>
 hipError_t launch_tile(Args &g, hipStream_t s) {
-    g.tiles_i = (int)((g.I + BM - 1) / BM);
-    g.tiles_j = (int)((g.J + BN - 1) / BN);
-    const int64_t tiles = (int64_t)g.tiles_i * g.tiles_j;
+    const int64_t tiles = ((g.I + BM - 1) / BM) * ((g.J + BN - 1) / BN) * g.splits;
     if (tiles >= (int64_t)1 << 31) return hipErrorNotSupported;
     g.group = 8;
     loss_pp_kernel<BM, BN, WGM, WGN, TB, KIND><<<(unsigned)tiles, kPPThreads, 0, s>>>(g);
@@ -325,108 +426,175 @@ hipError_t launch_tile(Args &g, hipStream_t s) {
 }
 
 template <bool TB, Kind KIND>
-hipError_t launch(Args g, hipStream_t s) {
-    switch (tile_of(g.I, g.J)) {
+hipError_t launch(Args g, const Choice &c, hipStream_t s) {
+    g.splits = c.splits;
+    switch (c.tile) {
     case 0: return launch_tile<256, 256, 2, 4, TB, KIND>(g, s);
-    case 1: return launch_tile<128, 128, 2, 4, TB, KIND>(g, s);
+    case 1: return launch_tile<192, 256, 2, 4, TB, KIND>(g, s);
+    case 2: return launch_tile<128, 128, 2, 4, TB, KIND>(g, s);
     default: return launch_tile<64, 128, 2, 4, TB, KIND>(g, s);
     }
 }
 
+// Below this the launches that gather would take longer than what they save.
+constexpr int64_t kCompactFrom = 257;
+
 int64_t up(int64_t v, int64_t q) { return (v + q - 1) / q * q; }
 size_t part(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
-hipError_t pad_cols(const void *src, uint16_t *dst, int64_t rows, int64_t n, int64_t np, hipStream_t s) {
+hipError_t gather(const void *src, uint16_t *dst, int64_t rows, int64_t n, int64_t np, const int *idx, const int *count,
+                  hipStream_t s) {
     const int64_t blocks = (rows * (np / 8) + 255) / 256;
-    pad_cols_kernel<<<(unsigned)(blocks < 16384 ? blocks : 16384), 256, 0, s>>>(static_cast<const uint16_t *>(src), dst, rows,
-                                                                                (int)n, (int)np);
+    gather_kernel<<<(unsigned)(blocks < 16384 ? blocks : 16384), 256, 0, s>>>(static_cast<const uint16_t *>(src), dst, rows,
+                                                                              (int)n, (int)np, idx, count);
     return hipGetLastError();
+}
+
+// Where things lie in the workspace; a size of 0 for what a call does not need.
+struct Space {
+    size_t total = 0;
+    size_t take(size_t bytes) {
+        const size_t at = total;
+        total += (bytes + 255) / 256 * 256;
+        return at;
+    }
+};
+
+// The tokens that count and the operands as the kernels read them.
+struct Operands {
+    int64_t np;                  // columns
+    bool compact;
+    size_t idx, targets, count, x, w;
+};
+Operands operands_of(Space &space, int64_t M, int64_t n, int64_t V) {
+    Operands o;
+    o.np = up(n, kPPK);
+    o.compact = M >= kCompactFrom;
+    o.idx = space.take(o.compact ? (size_t)M * 4 : 0);
+    o.targets = space.take(o.compact ? (size_t)M * 8 : 0);
+    o.count = space.take(o.compact ? 4 : 0);
+    o.x = space.take(o.compact || o.np != n ? (size_t)(M * o.np) * 2 : 0);
+    o.w = space.take(o.np != n ? (size_t)(V * o.np) * 2 : 0);
+    return o;
+}
+
+// What the launches take of them.
+struct Prepared {
+    const uint16_t *X, *W;
+    const int *idx, *count;
+    const int64_t *targets;
+};
+hipError_t prepare(const Operands &o, const LossPass &p, const LossEpi &e, char *ws, float *loss, float *lse, Prepared &r,
+                   hipStream_t s) {
+    r = {static_cast<const uint16_t *>(p.X), static_cast<const uint16_t *>(p.W), nullptr, nullptr, e.targets};
+    hipError_t err = hipSuccess;
+    if (o.compact) {
+        int *idx = reinterpret_cast<int *>(ws + o.idx), *count = reinterpret_cast<int *>(ws + o.count);
+        int64_t *targets = reinterpret_cast<int64_t *>(ws + o.targets);
+        compact_kernel<<<1, 1024, 0, s>>>(e, p.M, idx, targets, count, loss, lse);
+        err = hipGetLastError();
+        r.idx = idx;
+        r.count = count;
+        r.targets = targets;
+    }
+    if (err == hipSuccess && (o.compact || o.np != p.n)) {
+        uint16_t *x = reinterpret_cast<uint16_t *>(ws + o.x);
+        err = gather(p.X, x, p.M, p.n, o.np, r.idx, r.count, s);
+        r.X = x;
+    }
+    if (err == hipSuccess && o.np != p.n) {
+        uint16_t *w = reinterpret_cast<uint16_t *>(ws + o.w);
+        err = gather(p.W, w, p.V, p.n, o.np, nullptr, nullptr, s);
+        r.W = w;
+    }
+    return err;
 }
 
 // Vocabulary columns of a piece, and the workspace of a backward pass.
 struct Layout {
-    int64_t np, Mp, Mq, Vp, vp;
-    size_t tokens, xp, wp, wt, gt, acc, total;
+    Operands ops;
+    int64_t Mp, Mq, Vp, vp;
+    Choice dx;
+    size_t tokens, wt, gt, acc, total;
 };
 Layout layout_of(int64_t M, int64_t n, int64_t V) {
     Layout l;
-    l.np = up(n, kPPK);
+    Space space;
+    l.ops = operands_of(space, M, n, V);
     l.Mp = up(M, kPPK);
-    l.Mq = up(M, 256);
+    l.Mq = up(M, 256) + 256;     // the last tile's tokens, whatever its width
     l.Vp = up(V, kPPK);
     // G^T of a piece within 512 MB, but for very many tokens; pieces of one size, whole tiles
     int64_t most = ((int64_t)512 << 20) / (2 * l.Mp) / 256 * 256;
     if (most < 2048) most = 2048;
     const int64_t pieces = (V + most - 1) / most;
     l.vp = up((V + pieces - 1) / pieces, 256);
-    size_t at = 0;
-    const auto take = [&](size_t &where, size_t bytes) {
-        where = at;
-        at += part(bytes);
-    };
-    take(l.tokens, (size_t)l.Mq * 12);
-    take(l.xp, l.np != n ? (size_t)(M * l.np) * 2 : 0);
-    take(l.wp, l.np != n ? (size_t)(V * l.np) * 2 : 0);
-    take(l.wt, (size_t)(n * l.Vp) * 2);
-    take(l.gt, (size_t)(l.vp * l.Mp) * 2);
-    take(l.acc, (size_t)(n * l.Mp) * 4);
-    l.total = at;
+    // at least 16 units a split, and the splits' sums within the weights' gradient's size
+    int64_t splits = l.vp / kPPK / 16;
+    const int64_t room = l.vp / (2 * l.Mp);
+    splits = splits < room ? splits : room;
+    l.dx = choose(n, M, splits < 1 ? 1 : splits);
+    l.tokens = space.take((size_t)l.Mq * 12);
+    l.wt = space.take((size_t)(n * l.Vp) * 2);
+    l.gt = space.take((size_t)(l.vp * l.Mp) * 2);
+    l.acc = space.take((size_t)(l.dx.splits * n * l.Mp) * 4);
+    l.total = space.total;
     return l;
 }
 
 }  // namespace
 
 int loss_mfma_tiles(int64_t M, int64_t V) {
-    const int bn = tile_bn(tile_of(M, V));
+    const int bn = kTiles[choose(M, V).tile].bn;
     return (int)((V + bn - 1) / bn);
 }
 
 size_t loss_mfma_forward_bytes(int64_t M, int64_t n, int64_t V) {
-    return n % kPPK ? part((size_t)(M * up(n, kPPK)) * 2) + part((size_t)(V * up(n, kPPK)) * 2) : 0;
+    Space space;
+    operands_of(space, M, n, V);
+    return space.total;
 }
 
 size_t loss_mfma_backward_bytes(int64_t M, int64_t n, int64_t V) { return layout_of(M, n, V).total; }
 
-hipError_t launch_loss_mfma_stats(const LossPass &p, const LossEpi &e, void *ws, hipStream_t s) {
+hipError_t launch_loss_mfma_stats(const LossPass &p, const LossEpi &e, void *ws, float *each, LossTokens &tokens,
+                                  hipStream_t s) {
+    Space space;
+    const Operands o = operands_of(space, p.M, p.n, p.V);
+    Prepared r;
+    hipError_t err = prepare(o, p, e, static_cast<char *>(ws), each, p.lse, r, s);
+    if (err != hipSuccess) return err;
+    tokens = {r.idx, r.count};
     Args g{};
     g.e = e;
+    g.e.targets = r.targets;
+    g.count = r.count;
+    g.A = r.X;
+    g.B = r.W;
     g.I = p.M;
     g.J = p.V;
-    g.K = g.lda = g.ldb = up(p.n, kPPK);
-    g.A = static_cast<const uint16_t *>(p.X);
-    g.B = static_cast<const uint16_t *>(p.W);
-    if (g.K != p.n) {
-        uint16_t *xp = static_cast<uint16_t *>(ws);
-        uint16_t *wp = reinterpret_cast<uint16_t *>(static_cast<char *>(ws) + part((size_t)(p.M * g.K) * 2));
-        hipError_t err = pad_cols(p.X, xp, p.M, p.n, g.K, s);
-        if (err == hipSuccess) err = pad_cols(p.W, wp, p.V, p.n, g.K, s);
-        if (err != hipSuccess) return err;
-        g.A = xp;
-        g.B = wp;
-    }
-    return launch<false, kStats>(g, s);
+    g.K = g.lda = g.ldb = o.np;
+    return launch<false, kStats>(g, choose(p.M, p.V), s);
 }
 
 hipError_t launch_loss_mfma_grad(const LossPass &p, const LossEpi &e, hipStream_t s) {
     const Layout l = layout_of(p.M, p.n, p.V);
     char *ws = static_cast<char *>(p.ws);
     const auto at = [&](size_t o) { return reinterpret_cast<uint16_t *>(ws + o); };
+    Prepared r;
+    hipError_t err = prepare(l.ops, p, e, ws, nullptr, nullptr, r, s);
+    if (err != hipSuccess) return err;
     Token tok;
     tok.scale = reinterpret_cast<float *>(ws + l.tokens);
     tok.lse2 = tok.scale + l.Mq;
     tok.target = reinterpret_cast<int *>(tok.lse2 + l.Mq);
-    token_kernel<<<(unsigned)(l.Mq / 256), 256, 0, s>>>(e, tok, p.M, l.Mq);
-    const uint16_t *X = static_cast<const uint16_t *>(p.X), *W = static_cast<const uint16_t *>(p.W);
-    hipError_t err = hipGetLastError();
-    if (err == hipSuccess && l.np != p.n) {
-        err = pad_cols(p.X, at(l.xp), p.M, p.n, l.np, s);
-        if (err == hipSuccess) err = pad_cols(p.W, at(l.wp), p.V, p.n, l.np, s);
-        X = at(l.xp);
-        W = at(l.wp);
-    }
+    token_kernel<<<(unsigned)(l.Mq / 256), 256, 0, s>>>(e, tok, p.M, l.Mq, r.idx, r.count);
+    err = hipGetLastError();
     if (err == hipSuccess && p.dX) {
-        transpose_kernel<<<dim3((unsigned)(l.Vp / 64), (unsigned)(l.np / 64)), 256, 0, s>>>(
+        transpose_kernel<<<dim3((unsigned)(l.Vp / 64), (unsigned)(l.ops.np / 64)), 256, 0, s>>>(
             static_cast<const uint16_t *>(p.W), at(l.wt), p.V, (int)p.n, l.Vp);
+        if (r.count)
+            zero_rows_kernel<<<(unsigned)(p.M < 8192 ? p.M : 8192), 256, 0, s>>>(e, static_cast<uint16_t *>(p.dX), p.M, (int)p.n);
         err = hipGetLastError();
     }
     float *acc = reinterpret_cast<float *>(ws + l.acc);
@@ -434,23 +602,24 @@ hipError_t launch_loss_mfma_grad(const LossPass &p, const LossEpi &e, hipStream_
         const int64_t vn = p.V - v0 < l.vp ? p.V - v0 : l.vp;
         Args g{};
         g.e = e;
+        g.count = r.count;
         g.tok = tok;
         g.v0 = v0;
-        g.A = W + v0 * l.np;
-        g.B = X;
-        g.lda = g.ldb = g.K = l.np;
+        g.A = r.W + v0 * l.ops.np;
+        g.B = r.X;
+        g.lda = g.ldb = g.K = l.ops.np;
         g.I = vn;
         g.J = p.M;
         g.out = at(l.gt);
         g.ldo = l.Mp;
-        err = launch<false, kGrad>(g, s);
+        err = launch<false, kGrad>(g, choose(g.I, g.J), s);
         if (err == hipSuccess && p.dW) {
             g.A = at(l.gt);
             g.lda = g.K = l.Mp;
             g.rows_b = p.M;
             g.J = g.ldo = p.n;
             g.out = static_cast<uint16_t *>(p.dW) + v0 * p.n;
-            err = launch<true, kDw>(g, s);
+            err = launch<true, kDw>(g, choose(g.I, g.J), s);
         }
         if (err == hipSuccess && p.dX) {
             g.A = at(l.wt) + v0;
@@ -463,12 +632,12 @@ hipError_t launch_loss_mfma_grad(const LossPass &p, const LossEpi &e, hipStream_
             g.rows_b = vn;
             g.acc = acc;
             g.first = v0 == 0;
-            err = launch<true, kDx>(g, s);
+            err = launch<true, kDx>(g, l.dx, s);
         }
     }
     if (err == hipSuccess && p.dX) {
-        round_transpose_kernel<<<dim3((unsigned)(l.Mp / 64), (unsigned)(l.np / 64)), 256, 0, s>>>(
-            acc, static_cast<uint16_t *>(p.dX), p.M, (int)p.n, l.Mp);
+        round_transpose_kernel<<<dim3((unsigned)(l.Mp / 64), (unsigned)(l.ops.np / 64)), 256, 0, s>>>(
+            acc, l.dx.splits, static_cast<uint16_t *>(p.dX), p.M, (int)p.n, l.Mp, r.idx, r.count);
         err = hipGetLastError();
     }
     return err;

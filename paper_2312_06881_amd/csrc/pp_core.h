@@ -136,6 +136,7 @@ __device__ __forceinline__ void pp_barrier() {
 #define PP_IB(i) [pb##i] "v"(pb[i])
 #define PP_RA2 PP_RA(0, 0) PP_RA(1, 2048)
 #define PP_RA4 PP_RA(0, 0) PP_RA(1, 2048) PP_RA(2, 4096) PP_RA(3, 6144)
+#define PP_RA6 PP_RA4 PP_RA(4, 8192) PP_RA(5, 10240)
 #define PP_RA8 PP_RA4 PP_RA(4, 8192) PP_RA(5, 10240) PP_RA(6, 12288) PP_RA(7, 14336)
 #define PP_RB2 PP_RB(0, 0) PP_RB(1, 2048)
 #define PP_RB4 PP_RB2 PP_RB(2, 4096) PP_RB(3, 6144)
@@ -145,6 +146,7 @@ __device__ __forceinline__ void pp_barrier() {
 #define PP_TB6 PP_TB4 PP_TB(4) PP_TB(5)
 #define PP_OA2 PP_OA(0), PP_OA(1)
 #define PP_OA4 PP_OA(0), PP_OA(1), PP_OA(2), PP_OA(3)
+#define PP_OA6 PP_OA4, PP_OA(4), PP_OA(5)
 #define PP_OA8 PP_OA4, PP_OA(4), PP_OA(5), PP_OA(6), PP_OA(7)
 #define PP_OB2 PP_OB(0), PP_OB(1)
 #define PP_OB4 PP_OB2, PP_OB(2), PP_OB(3)
@@ -178,11 +180,12 @@ __device__ __forceinline__ void pp_read(uint32_t pa, const uint32_t (&pb)[TB ? S
                                         bf16x8_t (&b)[SN]) {
     bf16x4_t bl[SN], bh[SN];
     PP_CASE(8, 4)
+    PP_CASE(6, 4)
     PP_CASE(4, 6)
     PP_CASE(4, 4)
     PP_CASE(4, 2)
     PP_CASE(2, 2)
-    static_assert((SM == 8 && SN == 4) || (SM == 4 && (SN == 6 || SN == 4 || SN == 2)) || (SM == 2 && SN == 2),
+    static_assert(((SM == 8 || SM == 6) && SN == 4) || (SM == 4 && (SN == 6 || SN == 4 || SN == 2)) || (SM == 2 && SN == 2),
                   "a fragment read exists");
     if constexpr (TB) {
 #pragma unroll

@@ -45,4 +45,36 @@ __device__ __forceinline__ void store_cols(T *row, int c, int n, const float (&v
     }
 }
 
+// Eight values as they lie in memory, for operands that wait in registers until they are used.
+template <class T>
+struct Raw {
+    uint32_t w[sizeof(T) * 2];
+};
+template <bool RAG, class T>
+__device__ __forceinline__ Raw<T> load_raw(const T *row, int c, int n) {
+    Raw<T> r;
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) * 2; ++i) r.w[i] = 0u;
+    if (c + 8 <= n) {
+        __builtin_memcpy(r.w, row + c, sizeof(T) * 8);
+    } else if constexpr (RAG) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (c + e < n) {
+                if constexpr (sizeof(T) == 4) r.w[e] = __float_as_uint(row[c + e]);
+                else r.w[e >> 1] |= (uint32_t)row[c + e] << (16 * (e & 1));
+            }
+        }
+    }
+    return r;
+}
+__device__ __forceinline__ void unpack8(const Raw<float> &r, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(r.w[e]);
+}
+__device__ __forceinline__ void unpack8(const Raw<uint16_t> &r, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = unpack_bf16(r.w[e >> 1], e & 1);
+}
+
 }  // namespace dyad

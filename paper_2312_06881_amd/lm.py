@@ -15,6 +15,8 @@ and modules in ``nn`` are what it does.
 from __future__ import annotations
 
 import contextlib
+import ctypes
+import struct
 
 import torch
 
@@ -29,13 +31,15 @@ NORMS = {None: NORM_NONE, "layer": NORM_LAYER, "rms": NORM_RMS}
 REDUCTIONS = {"none": REDUCE_NONE, "sum": REDUCE_SUM, "mean": REDUCE_MEAN}
 
 
+_HERE = contextlib.nullcontext()
+
+
 def _on(x):
     """The launches go to x's device."""
     if not x.is_cuda:
         raise ValueError("libdyad takes device tensors")
-    if x.get_device() == torch.cuda.current_device():
-        return contextlib.nullcontext()
-    return torch.cuda.device(x.device)
+    # (x exists, so the device runtime is up)
+    return _HERE if x.get_device() == torch._C._cuda_getDevice() else torch.cuda.device(x.device)
 
 
 def _random(p, seed, offset, like):
@@ -78,39 +82,101 @@ def _norm_kind(kind, what):
     return NORMS[kind]
 
 
-def _arguments(M, n, x, y, norm, weight, bias, post_norm, post_weight, post_bias, gate, x_scale, y_scale, eps, p, seed,
-               offset, h, out, stats, post_stats, stream_dtype, dtype):
-    """The call's ``AddNormArgs``; x and out may be None (the backward pass)."""
-    like = x if x is not None else h
-    kinds = _norm_kind(norm, "norm"), _norm_kind(post_norm, "post_norm")
-    if y is None and (post_norm or gate is not None or p):
-        raise ValueError("post_norm, gate and dropout are of y")
-    if not norm and (weight is not None or bias is not None):
-        raise ValueError("weight and bias are of the norm")
-    if not post_norm and (post_weight is not None or post_bias is not None):
-        raise ValueError("post_weight and post_bias are of the post norm")
-    p, seed, offset, dev = _random(p, seed, offset, like)
-    params = [t for t in (weight, bias, post_weight, post_bias, gate) if t is not None]
-    for t in params[:len(params) - (gate is not None)]:
-        if t.shape != (n,):
-            raise ValueError(f"the norms' weights have shape {(n,)}, got {tuple(t.shape)}")
-    groups = 1
-    if gate is not None:
-        groups = gate.shape[0] if gate.dim() == 2 else 1
-        if gate.dim() not in (1, 2) or gate.shape[-1] != n or groups == 0 or M % groups:
-            raise ValueError(f"gate is {(n,)}, or {('groups', n)} with groups dividing the {M} tokens, got "
-                             f"{tuple(gate.shape)}")
-    _same_device(like, y, *params, h, out, stats, post_stats)
-    return AddNormArgs(M, n, groups, _dtype_of(stream_dtype), _dtype_of(dtype), _dtype(*params) if params else _dtype_of(dtype),
-                       *kinds, x_scale, y_scale, eps, p, seed, offset, _dev(dev), _ptr(x), _ptr(y), _ptr(weight),
-                       _ptr(bias), _ptr(post_weight), _ptr(post_bias), _ptr(gate), _ptr(h), _ptr(out), _ptr(stats),
-                       _ptr(post_stats))
-
-
 def _dtype_of(dtype):
     if dtype not in _dy._DT:
         raise TypeError(f"tensors are float32 or bfloat16, got {dtype}")
     return _dy._DT[dtype]
+
+
+_HEAD = struct.Struct("=3q5i3fd2Q")     # the values and the pointers of dyad_add_norm_args
+_POINTERS = struct.Struct("=12Q")
+_GRADS = struct.Struct("=9Q")
+assert _HEAD.size + _POINTERS.size == ctypes.sizeof(AddNormArgs) and _GRADS.size == ctypes.sizeof(AddNormGrads)
+
+
+def _p(t):
+    return 0 if t is None else t.data_ptr()
+
+
+class _AddNorm:
+    """A checked add_norm of x (or what stands for it), y and parameters, for its forward and backward calls."""
+
+    __slots__ = ("head", "M", "n", "norm", "post", "x_type", "dtype", "device", "has_y", "x_is_h", "dev")
+
+    def __init__(self, x, y, norm, weight, bias, post_norm, post_weight, post_bias, gate, x_scale, y_scale, eps, p, seed,
+                 offset, dtype):
+        M, n = x.shape
+        if y is not None and y.shape != x.shape:
+            raise ValueError(f"x and y have one shape, got {tuple(x.shape)} and {tuple(y.shape)}")
+        if dtype is not None and y is not None and dtype != y.dtype:
+            raise ValueError("out has y's dtype")
+        kinds = _norm_kind(norm, "norm"), _norm_kind(post_norm, "post_norm")
+        if y is None and (post_norm or gate is not None or p):
+            raise ValueError("post_norm, gate and dropout are of y")
+        if not norm and (weight is not None or bias is not None):
+            raise ValueError("weight and bias are of the norm")
+        if not post_norm and (post_weight is not None or post_bias is not None):
+            raise ValueError("post_weight and post_bias are of the post norm")
+        p, seed, offset, dev = _random(p, seed, offset, x)
+        dtype = dtype or (x if y is None else y).dtype
+        param, groups = None, 1
+        for t in (weight, bias, post_weight, post_bias, gate):
+            if t is None:
+                continue
+            if param is None:
+                param = t.dtype
+            elif t.dtype is not param:
+                raise TypeError(f"the parameters share one dtype, got {param} and {t.dtype}")
+            if t is not gate and t.shape != (n,):
+                raise ValueError(f"the norms' weights have shape {(n,)}, got {tuple(t.shape)}")
+            if t.device != x.device:
+                _same_device(x, t)
+            if not t.is_contiguous():
+                raise ValueError("libdyad takes contiguous tensors")
+        if gate is not None:
+            groups = gate.shape[0] if gate.dim() == 2 else 1
+            if gate.dim() not in (1, 2) or gate.shape[-1] != n or groups == 0 or M % groups:
+                raise ValueError(f"gate is {(n,)}, or {('groups', n)} with groups dividing the {M} tokens, got "
+                                 f"{tuple(gate.shape)}")
+        _ptr(x), _ptr(y), _same_device(x, y)
+        self.M, self.n, self.norm, self.post, self.dev = M, n, kinds[0], kinds[1], dev
+        self.x_type, self.dtype, self.device, self.has_y = x.dtype, dtype, x.device, y is not None
+        self.x_is_h = y is None and x_scale == 1.0
+        self.head = _HEAD.pack(M, n, groups, _dtype_of(x.dtype), _dtype_of(dtype), _dtype_of(param or dtype), *kinds, x_scale,
+                               y_scale, eps, p, seed, offset)
+
+    def forward(self, x, y, weight, bias, post_weight, post_bias, gate, keep):
+        """(h, out, stats, post_stats)."""
+        M, n, new = self.M, self.n, torch.empty
+        h = x if self.x_is_h else torch.empty_like(x)
+        out = new((M, n), dtype=self.dtype, device=self.device) if self.norm else None
+        stats = new((M, 2), dtype=torch.float32, device=self.device) if keep and self.norm else None
+        post_stats = new((M, 2), dtype=torch.float32, device=self.device) if keep and self.post else None
+        if self.norm or not self.x_is_h:
+            args = self.head + _POINTERS.pack(_p(self.dev), x.data_ptr(), _p(y), _p(weight), _p(bias), _p(post_weight),
+                                              _p(post_bias), _p(gate), 0 if self.x_is_h else h.data_ptr(), _p(out), _p(stats),
+                                              _p(post_stats))
+            with _on(x):
+                _check(_dy._load().dyad_add_norm_forward(args, _stream(x)))
+        return h, out, stats, post_stats
+
+    def backward(self, dh, dout, h, x, y, weight, bias, post_weight, post_bias, gate, stats, post_stats, dev, want):
+        """The gradients of x, y, weight, bias, post_weight, post_bias and gate, None where ``want`` is false.  x None: h is
+        read, else it is formed again from x and y.  A y whose values nothing reads may be any tensor."""
+        M, n, like = self.M, self.n, x if h is None else h
+        rows = [torch.empty((M, n), dtype=t, device=self.device) if w else None
+                for w, t in ((want[0], self.x_type), (want[1], self.dtype))]
+        grads = rows + [torch.empty_like(t) if w and t is not None else None
+                        for w, t in zip(want[2:], (weight, bias, post_weight, post_bias, gate))]
+        args = self.head + _POINTERS.pack(_p(dev), _p(x), _p(y), _p(weight), _p(bias), _p(post_weight), _p(post_bias),
+                                          _p(gate), _p(h), 0, _p(stats), _p(post_stats))
+        g = _GRADS.pack(_p(dh), _p(dout), *map(_p, grads))
+        lib = _dy._load()
+        need = lib.dyad_add_norm_workspace_bytes(args, g)
+        ws = torch.empty((need,), dtype=torch.uint8, device=self.device) if need else None
+        with _on(like):
+            _check(lib.dyad_add_norm_backward(args, g, _p(ws), need, _stream(like)))
+        return grads
 
 
 def add_norm(x, y=None, norm="layer", weight=None, bias=None, *, post_norm=None, post_weight=None, post_bias=None,
@@ -121,55 +187,42 @@ def add_norm(x, y=None, norm="layer", weight=None, bias=None, *, post_norm=None,
     row m taking gate row m // (M / groups); p, seed, offset as in ``dropout``.  h has x's type, out y's
     (without y: dtype, by default x's).  Without y and with x_scale 1, h is x itself.  keep: also the rows' statistics,
     (h, out, stats, post_stats), for ``add_norm_backward``."""
-    M, n = x.shape
-    if y is not None and y.shape != x.shape:
-        raise ValueError(f"x and y have one shape, got {tuple(x.shape)} and {tuple(y.shape)}")
-    if dtype is not None and y is not None and dtype != y.dtype:
-        raise ValueError("out has y's dtype")
-    dtype = dtype or (x if y is None else y).dtype
-    same = y is None and x_scale == 1.0
-    h = None if same else torch.empty_like(x)
-    out = torch.empty((M, n), dtype=dtype, device=x.device) if norm else None
-    stats = torch.empty((M, 2), dtype=torch.float32, device=x.device) if keep and norm else None
-    post_stats = torch.empty((M, 2), dtype=torch.float32, device=x.device) if keep and post_norm else None
-    a = _arguments(M, n, x, y, norm, weight, bias, post_norm, post_weight, post_bias, gate, x_scale, y_scale, eps, p,
-                   seed, offset, h, out, stats, post_stats, x.dtype, dtype)
-    if not same or norm:
-        with _on(x):
-            _check(_dy.dyad_add_norm_forward(a, _stream(x)))
-    h = x if same else h
-    return (h, out, stats, post_stats) if keep else (h, out)
+    call = _AddNorm(x, y, norm, weight, bias, post_norm, post_weight, post_bias, gate, x_scale, y_scale, eps, p, seed, offset,
+                    dtype)
+    res = call.forward(x, y, weight, bias, post_weight, post_bias, gate, keep)
+    return res if keep else res[:2]
 
 
-def add_norm_backward(dh, dout, h, stats, post_stats=None, y=None, norm="layer", weight=None, bias=None, *, post_norm=None,
-                      post_weight=None, post_bias=None, gate=None, x_scale=1.0, y_scale=1.0, eps=1e-5, p=0.0, seed=0,
-                      offset=0, dtype=None, want=("x", "y", "weight", "bias", "post_weight", "post_bias", "gate")):
-    """The gradients of ``add_norm`` as a dict, of what ``want`` names and the call has.  h, stats, post_stats: what
-    add_norm(..., keep=True) returned; dh, dout: the gradients that reach h and out, either may be None; y: the
-    block's output (its values are read with a post norm or a gate only); the others are the forward call's."""
-    M, n = h.shape
-    dtype = dtype or (h if y is None else y).dtype
-    for t, like in ((dh, h.dtype), (dout, dtype)):
-        if t is not None and (t.shape != h.shape or t.dtype != like):
-            raise ValueError(f"a gradient has shape {tuple(h.shape)} and {like}, got {tuple(t.shape)} and {t.dtype}")
+def add_norm_backward(dh, dout, stats, post_stats=None, x=None, y=None, norm="layer", weight=None, bias=None, *, h=None,
+                      post_norm=None, post_weight=None, post_bias=None, gate=None, x_scale=1.0, y_scale=1.0, eps=1e-5,
+                      p=0.0, seed=0, offset=0, dtype=None,
+                      want=("x", "y", "weight", "bias", "post_weight", "post_bias", "gate")):
+    """The gradients of ``add_norm`` as a dict, of what ``want`` names and the call has.  stats, post_stats: what
+    add_norm(..., keep=True) returned; dh, dout: the gradients that reach h and out, either may be None; the others are
+    the forward call's.  h in place of x: it is read, where with x it is formed again from x and y, which keeps a bf16
+    stream's rounding of it out of the gradients."""
+    like = x if x is not None else h
+    if like is None or (x is not None and h is not None):
+        raise ValueError("x or h")
+    call = _AddNorm(like, y, norm, weight, bias, post_norm, post_weight, post_bias, gate, x_scale, y_scale, eps, p, seed, offset,
+                    dtype)
+    for t, kind in ((dh, like.dtype), (dout, call.dtype)):
+        if t is not None and (t.shape != like.shape or t.dtype != kind):
+            raise ValueError(f"a gradient has shape {tuple(like.shape)} and {kind}, got {tuple(t.shape)} and {t.dtype}")
     for s in (stats, post_stats):
-        if s is not None and (s.shape != (M, 2) or s.dtype is not torch.float32):
-            raise ValueError(f"statistics are float32 {(M, 2)}")
+        if s is not None and (s.shape != (call.M, 2) or s.dtype is not torch.float32):
+            raise ValueError(f"statistics are float32 {(call.M, 2)}")
     if (norm and stats is None) or (post_norm and post_stats is None):
         raise ValueError("the statistics that add_norm(..., keep=True) returned are missing")
     if dout is not None and not norm:
         raise ValueError("there is no out without a norm")
-    a = _arguments(M, n, None, y, norm, weight, bias, post_norm, post_weight, post_bias, gate, x_scale, y_scale, eps, p,
-                   seed, offset, h, None, stats, post_stats, h.dtype, dtype)
-    _same_device(h, dh, dout)
-    got = {"x": h, "y": y, "weight": weight, "bias": bias, "post_weight": post_weight, "post_bias": post_bias, "gate": gate}
-    grads = {k: torch.empty_like(t) for k, t in got.items() if k in want and t is not None}
-    g = AddNormGrads(_ptr(dh), _ptr(dout), *(_ptr(grads.get(k)) for k in got))
-    with _on(h):
-        need = _dy.dyad_add_norm_workspace_bytes(a, g)
-        ws = _bytes(need, h.device) if need else None
-        _check(_dy.dyad_add_norm_backward(a, g, _ptr(ws), need, _stream(h)))
-    return grads
+    for t in (dh, dout, stats, post_stats):
+        _ptr(t), _same_device(like, t)
+    names = ("x", "y", "weight", "bias", "post_weight", "post_bias", "gate")
+    there = (like, y, weight, bias, post_weight, post_bias, gate)
+    got = call.backward(dh, dout, h, x, y, weight, bias, post_weight, post_bias, gate, stats, post_stats, call.dev,
+                        [k in want and t is not None for k, t in zip(names, there)])
+    return {k: g for k, g in zip(names, got) if g is not None}
 
 
 def _loss_arguments(x, weight, targets, reduction):

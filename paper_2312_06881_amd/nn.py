@@ -43,6 +43,8 @@ __all__ = ["DyadLinear", "DyadFF", "MX4DyadLinear", "MX4DyadFF", "dyad_linear", 
 
 
 def _tokens(x: torch.Tensor) -> torch.Tensor:
+    if x.dim() == 2 and x.is_contiguous():
+        return x
     return x.reshape(-1, x.shape[-1]).contiguous()
 
 
@@ -454,52 +456,58 @@ def dropout(x, p, seed, offset=0, training=True):
 
 class _AddNormFn(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, y, weight, bias, post_weight, post_bias, gate, offset, norm, post_norm, dtype, kw):
-        h, out, stats, post_stats = lm.add_norm(x, y, norm, weight, bias, post_norm=post_norm, post_weight=post_weight,
-                                                post_bias=post_bias, gate=gate, offset=offset, dtype=dtype, keep=True, **kw)
-        kept, ctx.offset = _saved_offset(offset)
-        # of y only its type counts where nothing reads it again
-        reads_y = post_norm is not None or gate is not None
-        ctx.y = None if y is None or reads_y else y.dtype
-        ctx.norm, ctx.post_norm, ctx.dtype, ctx.kw = norm, post_norm, dtype, kw
+    def forward(ctx, x, y, weight, bias, post_weight, post_bias, gate, call):
+        h, out, stats, post_stats = call.forward(x, y, weight, bias, post_weight, post_bias, gate, True)
+        ctx.call = call
+        # an fp32 stream's h is read again, a bf16 one's formed again from x and y; of y only
+        # its place counts where nothing reads it
+        again = x.dtype is not torch.float32 and not call.x_is_h and call.norm != 0
+        reads_y = again or call.post != 0 or gate is not None
+        ctx.again = again
         ctx.set_materialize_grads(False)
-        ctx.save_for_backward(h, y if reads_y else None, weight, bias, post_weight, post_bias, gate, stats, post_stats, kept)
+        ctx.save_for_backward(x if again else h, y if reads_y else None, weight, bias, post_weight, post_bias, gate, stats,
+                              post_stats, call.dev)
         if h is x:
             h = x.view_as(x)
-        return (h, out) if norm else (h,)
+        return (h, out) if call.norm else h
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dh, dout=None):
-        h, y, weight, bias, post_weight, post_bias, gate, stats, post_stats, kept = ctx.saved_tensors
         if dh is None and dout is None:
-            return (None,) * 12
-        names = ("x", "y", "weight", "bias", "post_weight", "post_bias", "gate")
-        want = [n for n, need in zip(names, ctx.needs_input_grad) if need]
-        if ctx.y is not None:
-            y = h if ctx.y == h.dtype else torch.empty(h.shape, dtype=ctx.y, device=h.device)
-        g = lm.add_norm_backward(None if dh is None else dh.contiguous(), None if dout is None else dout.contiguous(), h,
-                                 stats, post_stats, y, ctx.norm, weight, bias, post_norm=ctx.post_norm,
-                                 post_weight=post_weight, post_bias=post_bias, gate=gate,
-                                 offset=ctx.offset if kept is None else kept, dtype=ctx.dtype, want=want, **ctx.kw)
-        return (*(g.get(n) for n in names), None, None, None, None, None)
+            return (None,) * 8
+        kept, y, weight, bias, post_weight, post_bias, gate, stats, post_stats, dev = ctx.saved_tensors
+        call = ctx.call
+        if dh is not None and not dh.is_contiguous():
+            dh = dh.contiguous()
+        if dout is not None and not dout.is_contiguous():
+            dout = dout.contiguous()
+        x, h = (kept, None) if ctx.again else (None, kept)
+        if y is None and call.has_y:
+            y = kept
+        return (*call.backward(dh, dout, h, x, y, weight, bias, post_weight, post_bias, gate, stats, post_stats, dev,
+                               ctx.needs_input_grad), None)
 
 
 def add_norm(x, y=None, norm="layer", weight=None, bias=None, *, post_norm=None, post_weight=None, post_bias=None, gate=None,
              x_scale=1.0, y_scale=1.0, eps=1e-5, p=0.0, seed=0, offset=0, dtype=None):
     """(h, out): h = x_scale x + y_scale gate * dropout(post_norm(y)), the residual stream with a block's output,
-    and out = norm(h), the next block's input.  x and y [..., n]; see ``lm.add_norm``.  out is None without a norm."""
+    and out = norm(h), the next block's input.  x and y [..., n]; see ``lm.add_norm``.  out is None without a norm.
+    For the backward pass an fp32 stream keeps h, a bf16 one x and y (h is formed again, without its rounding)."""
     shape = x.shape
-    xt, yt = _tokens(x), None if y is None else _tokens(y)
     if y is not None and y.shape != shape:
         raise ValueError(f"x and y have one shape, got {tuple(shape)} and {tuple(y.shape)}")
-    kw = dict(x_scale=float(x_scale), y_scale=float(y_scale), eps=float(eps), p=float(p), seed=seed)
+    xt, yt = _tokens(x), None if y is None else _tokens(y)
+    call = lm._AddNorm(xt, yt, norm, weight, bias, post_norm, post_weight, post_bias, gate, x_scale, y_scale, eps, p, seed,
+                       offset, dtype)
     if _plain(x, y, weight, bias, post_weight, post_bias, gate):
-        h, out = lm.add_norm(xt, yt, norm, weight, bias, post_norm=post_norm, post_weight=post_weight,
-                             post_bias=post_bias, gate=gate, offset=offset, dtype=dtype, **kw)
+        h, out, _, _ = call.forward(xt, yt, weight, bias, post_weight, post_bias, gate, False)
+    elif call.norm:
+        h, out = _AddNormFn.apply(xt, yt, weight, bias, post_weight, post_bias, gate, call)
     else:
-        h, *out = _AddNormFn.apply(xt, yt, weight, bias, post_weight, post_bias, gate, offset, norm, post_norm, dtype, kw)
-        out = out[0] if out else None
+        h, out = _AddNormFn.apply(xt, yt, weight, bias, post_weight, post_bias, gate, call), None
+    if xt is x:
+        return h, out
     return h.reshape(shape), None if out is None else out.reshape(shape)
 
 

@@ -160,6 +160,23 @@ def test_nan_and_infinity_stay_in_their_tokens(dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("ignored", [0.0, 0.02, 0.5, 0.97, 1.1])
+def test_few_or_many_count(dtype, ignored):
+    # enough tokens that those that count are gathered; a batch that begins and ends with others
+    x, w, t = make(801, 72, 1100, dtype, ignored=ignored)
+    if ignored > 0.1:
+        t[:300] = -100
+        t[790:] = -100
+    check(x, w, t)
+    check(x, w, t, "none", no_grad=True)
+
+
+def test_many_splits_of_the_vocabulary():
+    check(*make(260, 64, 40000, BF))
+    check(*make(40, 192, 30000, BF))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_leading_dimensions_and_one_gradient_only(dtype):
     x, w, t = make(60, 64, 300, dtype)
     got, dx, dw = check(x, w, t)

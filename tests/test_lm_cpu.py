@@ -85,7 +85,7 @@ def test_add_norm_forward_refuses(kw, code):
 
 
 @pytest.mark.parametrize("kw,gkw,code", [(a, {}, c) for a, c in BAD_BOTH] + [
-    (dict(h=None), {}, -1), (dict(stats=None), {}, -1), (dict(post_stats=None), {}, -1), (dict(norm=0), {}, -1),
+    (dict(h=None, x=None), {}, -1), (dict(stats=None), {}, -1), (dict(post_stats=None), {}, -1), (dict(norm=0), {}, -1),
     (dict(norm=0), dict(dout=None, dbias=None), -1), (dict(post=0), {}, -1), (dict(y=None), {}, -1),
     (dict(gate=None), {}, -1), ({}, dict(dx=FAKE + 4), -3), ({}, {}, -5)])
 def test_add_norm_backward_refuses(kw, gkw, code):
