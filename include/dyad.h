@@ -366,8 +366,9 @@ int dyad_add_norm_backward(const dyad_add_norm_args *args, const dyad_add_norm_g
  *
  * Backward: dloss, of loss's length, is the gradient that reaches it; dX [M][n] and
  * dW [V][n], either of which may be NULL, are the gradients.  The logits are formed
- * again, a piece of the vocabulary at a time; their gradient is rounded to dtype
- * where it enters the products with W and X, whose sums are fp32.
+ * again, a piece of the vocabulary at a time.  With bf16 operands their gradient, and
+ * X times dloss, enter the products with W and X in fp16 (at powers of two that meet
+ * its range); the sums are fp32.
  *
  * M, V <= 2^22 and n <= 2^20, else DYAD_ERR_SHAPE.  The workspace holds
  * dyad_linear_ce_workspace_bytes() bytes for the pass (0 for invalid arguments).

@@ -1,12 +1,18 @@
 // The loss's matrix products in bf16, on the pipelined eight-wave tiles of pp_core.h:
 //   kStats  Z = X W^T, tokens by vocabulary: per token (largest, sum of exponentials) of the tile
-//   kGrad   Z^T = W X^T of a piece of the vocabulary, as G^T = dloss (exp(Z^T - lse) - onehot), in bf16
-//   kDw     dW = G^T X of the piece
-//   kDx     dX^T += W^T G of the piece, in fp32
+//   kGrad   Z^T = W X^T of a piece of the vocabulary, as G^T = exp(Z^T - lse) - onehot
+//   kDw     dW = G^T (dloss X) of the piece
+//   kDx     dX^T += W^T G of the piece, in fp32; times dloss at the end
 // Side A's rows run along the reduction, side B's do (W, X) or are its indices (X, G^T read
 // transposed out of LDS), so one copy of G serves both products.  What they need laid out
 // otherwise is laid out once a call: W^T, and X and W with rows of whole 64s where n is not.
 // Padded reduction indices are zero on one side and finite on the other.
+//
+// G, dloss X and W^T are fp16 there: G's values lie in [-1, 1], and in bf16 their rounding would
+// put as much error into the gradients as the gradients' own (2.4e-3 to 2.7e-3 off 64 bits in
+// place of 1.7e-3), where eleven bits put an eighth of that.  fp16's range is met by powers of two:
+// 2^15 for G (values from 2^-29 on keep all bits), and one a column for the other two, which
+// takes the column's largest magnitude to 2^14 .. 2^15 and goes out again with the sums.
 //
 // Tokens that do not count take no part: from kCompactFrom tokens the others are gathered, in
 // order, and the kernels take their number from device memory (prompts and padding are often half
@@ -27,6 +33,21 @@ struct Token {
     int *target;           // -1 where it does not
 };
 
+constexpr int kGExp = 15;                       // G is held as G 2^15
+
+// What a column is multiplied by, as an exponent, from the bits of its largest finite magnitude.
+__device__ __forceinline__ int column_exp(uint32_t top) {
+    if (top == 0u) return 0;
+    const int e = 14 + 127 - (int)(top >> 23);
+    return e < -100 ? -100 : e > 120 ? 120 : e;
+}
+
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+    typedef __attribute__((ext_vector_type(2))) _Float16 f16x2_t;
+    const f32x2_t v = {a, b};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2_t));
+}
+
 struct Args {
     const uint16_t *A, *B;
     int64_t lda, ldb, I, J, K;   // K: a multiple of 64
@@ -36,6 +57,7 @@ struct Args {
     const int *count;            // tokens, in place of the side that runs over them; null: as given
     LossEpi e;
     Token tok;
+    const uint32_t *col_top;     // kDw: of the columns of dloss X
     int64_t v0;
     uint16_t *out;
     float *acc;
@@ -64,8 +86,9 @@ __device__ __forceinline__ void swap_lane_rows(uint32_t &a, uint32_t &b) {
 
 // x: a lane's four sums of column block 2 jp and of the next.  After the swap it holds 8
 // consecutive columns, from lane_piece() of the pair on.
-__device__ __forceinline__ uint4 pack_pair(const float (&x)[8]) {
-    uint32_t d0 = pack_bf16(x[0], x[1]), d1 = pack_bf16(x[2], x[3]), s0 = pack_bf16(x[4], x[5]), s1 = pack_bf16(x[6], x[7]);
+template <class Pack>
+__device__ __forceinline__ uint4 pack_pair(const float (&x)[8], Pack pack) {
+    uint32_t d0 = pack(x[0], x[1]), d1 = pack(x[2], x[3]), s0 = pack(x[4], x[5]), s1 = pack(x[6], x[7]);
     swap_lane_rows(d0, s0);
     swap_lane_rows(d1, s1);
     return make_uint4(d0, d1, s0, s1);
@@ -167,8 +190,8 @@ __global__ void __launch_bounds__(kPPThreads, 1) loss_pp_kernel(Args g) {
 #pragma unroll
         for (int j = 0; j < SN; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     if (units > 0)
-        pp_loop<SM, SN, TB, 4 * SB::kPitch, SA::kPer, SB::kPer, C::kSlotA, C::kSlotB>(units, wave, acc, issue_a, issue_b,
-                                                                                    addr, [](int) { return true; });
+        pp_loop<SM, SN, TB, 4 * SB::kPitch, SA::kPer, SB::kPer, C::kSlotA, C::kSlotB, KIND == kDw || KIND == kDx>(
+            units, wave, acc, issue_a, issue_b, addr, [](int) { return true; });
     // acc[i][j][v]: side A's row wm0 + 16 i + lr, side B's wn0 + 16 j + 4 lg + v
     if constexpr (KIND == kStats) {
         loss_stats<SM, SN, BM, WGN>(g.e, acc, i0, g.I, j0, tile_j, wm0, wn0, wave % WGN, reinterpret_cast<float2 *>(smem));
@@ -194,23 +217,31 @@ __global__ void __launch_bounds__(kPPThreads, 1) loss_pp_kernel(Args g) {
                 for (int e = 0; e < 8; ++e) {
                     const float z = acc[i][2 * jp + (e >> 2)][e & 3];
                     const float p = __builtin_amdgcn_exp2f(fmaf(z, kLog2e, -lse2[e])) - (target[e] == v_lane + 16 * i ? 1.f : 0.f);
-                    x[e] = scale[e] != 0.f ? scale[e] * p : 0.f;          // zero whatever p is
+                    x[e] = scale[e] != 0.f ? p * (float)(1 << kGExp) : 0.f;   // zero whatever p is
                 }
-                const uint4 w = pack_pair(x);
+                const uint4 w = pack_pair(x, pack_f16);
                 if (col < g.ldo && i0 + wm0 + 16 * i + lr < g.I) *reinterpret_cast<uint4 *>(o + (int64_t)(16 * i) * g.ldo) = w;
             }
         }
     } else if constexpr (KIND == kDw) {
 #pragma unroll
-        for (int i = 0; i < SM; ++i) {
-            const int64_t row = i0 + wm0 + 16 * i + lr;
+        for (int jp = 0; jp < SN / 2; ++jp) {
+            int back[8];
 #pragma unroll
-            for (int jp = 0; jp < SN / 2; ++jp) {
+            for (int h = 0; h < 2; ++h) {
+                uint32_t top[4];                               // laid out for whole tiles
+                __builtin_memcpy(top, __builtin_assume_aligned(g.col_top + j0 + wn0 + 32 * jp + 16 * h + 4 * lg, 16), 16);
+#pragma unroll
+                for (int v = 0; v < 4; ++v) back[4 * h + v] = -(column_exp(top[v]) + kGExp);
+            }
+            const int64_t col = j0 + wn0 + 32 * jp + lane_piece(lg);
+#pragma unroll
+            for (int i = 0; i < SM; ++i) {
+                const int64_t row = i0 + wm0 + 16 * i + lr;
                 float x[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = acc[i][2 * jp + (e >> 2)][e & 3];
-                const uint4 w = pack_pair(x);
-                const int64_t col = j0 + wn0 + 32 * jp + lane_piece(lg);
+                for (int e = 0; e < 8; ++e) x[e] = ldexpf(acc[i][2 * jp + (e >> 2)][e & 3], back[e]);
+                const uint4 w = pack_pair(x, pack_bf16);
                 if (row >= g.I) continue;
                 uint16_t *o = g.out + row * g.ldo + col;
                 if (col + 8 <= g.J) {
@@ -298,8 +329,60 @@ __global__ void __launch_bounds__(256) zero_rows_kernel(LossEpi e, uint16_t *dx,
     }
 }
 
-// dst[c][r] = src[r][c] for r < rows, else 0, r < ld (a multiple of 64): 64 x 64 tiles.
-__global__ void __launch_bounds__(256) transpose_kernel(const uint16_t *src, uint16_t *dst, int64_t rows, int n, int64_t ld) {
+// The largest finite magnitude of each column of src (times each row's scale), as bits, into
+// top, which starts at zero.  256 columns by eight rows a workgroup, a stretch of rows.
+__global__ void __launch_bounds__(256) column_top_kernel(const uint16_t *src, const float *scale, int64_t rows, int n, int ld,
+                                                         const int *count, uint32_t *top) {
+    __shared__ uint32_t t[8][256 + 8];
+    if (count) rows = *count;
+    const int c = blockIdx.y * 256 + (threadIdx.x & 31) * 8, r = threadIdx.x >> 5;
+    uint32_t best[8] = {};
+    if (c < n) {
+        for (int64_t m = (int64_t)blockIdx.x * 8 + r; m < rows; m += (int64_t)gridDim.x * 8) {
+            float v[8];
+            load_cols<true>(src + m * ld, c, n, v);
+            const float s = scale ? scale[m] : 1.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t b = __float_as_uint(v[e] * s) & 0x7fffffffu;
+                best[e] = b < 0x7f800000u && b > best[e] ? b : best[e];
+            }
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) t[r][(threadIdx.x & 31) * 8 + e] = best[e];
+    __syncthreads();
+    uint32_t b = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) b = t[k][threadIdx.x] > b ? t[k][threadIdx.x] : b;
+    // the order of these does not matter
+    if (blockIdx.y * 256 + threadIdx.x < n && b) atomicMax(top + blockIdx.y * 256 + threadIdx.x, b);
+}
+
+// dst[m][c] = src[m][c] scale[m] in fp16 at the column's scale, rows of np columns.
+__global__ void __launch_bounds__(256) scale_kernel(const uint16_t *src, const float *scale, const uint32_t *top,
+                                                    uint16_t *dst, int64_t rows, int np, const int *count) {
+    if (count) rows = *count;
+    const int64_t total = rows * (np / 8);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t m = i / (np / 8);
+        const int c = (int)(i - m * (np / 8)) * 8;
+        float v[8];
+        load8(src + m * np + c, v);
+        const float s = scale[m];
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = s != 0.f ? ldexpf(v[e] * s, column_exp(top[c + e])) : 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = pack_f16(v[2 * e], v[2 * e + 1]);
+        __builtin_memcpy(__builtin_assume_aligned(dst + m * np + c, 16), w, 16);
+    }
+}
+
+// dst[c][r] = src[r][c] for r < rows, else 0, r < ld (a multiple of 64), in fp16 at the column's
+// scale: 64 x 64 tiles.
+__global__ void __launch_bounds__(256) transpose_kernel(const uint16_t *src, const uint32_t *top, uint16_t *dst, int64_t rows,
+                                                        int n, int64_t ld) {
     __shared__ uint16_t t[64][66];
     const int64_t r0 = (int64_t)blockIdx.x * 64;
     const int c0 = blockIdx.y * 64, tid = threadIdx.x;
@@ -321,15 +404,18 @@ __global__ void __launch_bounds__(256) transpose_kernel(const uint16_t *src, uin
     for (int q = 0; q < 2; ++q) {
         const int c = (tid + 256 * q) / 8, r = (tid + 256 * q) % 8 * 8;
         if (c0 + c >= n) continue;
-        uint16_t v[8];
+        const int up = column_exp(top[c0 + c]);
+        uint32_t w[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = t[c][r + e];
-        __builtin_memcpy(__builtin_assume_aligned(dst + (int64_t)(c0 + c) * ld + r0 + r, 16), v, 16);
+        for (int e = 0; e < 4; ++e)
+            w[e] = pack_f16(ldexpf(bf16_to_f32(t[c][r + 2 * e]), up), ldexpf(bf16_to_f32(t[c][r + 2 * e + 1]), up));
+        __builtin_memcpy(__builtin_assume_aligned(dst + (int64_t)(c0 + c) * ld + r0 + r, 16), w, 16);
     }
 }
 
-// dX[idx[m]][c] = the fp32 sums acc[split][c][m], added in order and rounded: 64 x 64 tiles.
-__global__ void __launch_bounds__(256) round_transpose_kernel(const float *acc, int splits, uint16_t *dst, int64_t M, int n,
+// dX[idx[m]][c] = scale[m] times the fp32 sums acc[split][c][m], added in order, rounded: 64 x 64 tiles.
+__global__ void __launch_bounds__(256) round_transpose_kernel(const float *acc, int splits, const float *scale,
+                                                              const uint32_t *top, uint16_t *dst, int64_t M, int n,
                                                               int64_t ld, const int *idx, const int *count) {
     __shared__ float t[64][65];
     if (count) M = *count;
@@ -349,24 +435,28 @@ __global__ void __launch_bounds__(256) round_transpose_kernel(const float *acc, 
                 for (int e = 0; e < 4; ++e) v[e] += u[e];
             }
         }
+        const int back = c0 + c < n ? -(column_exp(top[c0 + c]) + kGExp) : 0;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) t[m + e][c] = v[e];
+        for (int e = 0; e < 4; ++e) t[m + e][c] = ldexpf(v[e], back);
     }
     __syncthreads();
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
         const int m = (tid + 256 * q) / 8, c = (tid + 256 * q) % 8 * 8;
         if (m0 + m >= M) continue;
+        const float by = scale[m0 + m];
         float v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = t[m][c + e];
+        for (int e = 0; e < 8; ++e) v[e] = by != 0.f ? t[m][c + e] * by : 0.f;
         store_cols<true>(dst + (idx ? idx[m0 + m] : m0 + m) * n, c0 + c, n, v);
     }
 }
 
+// The tokens' part of the gradient, and zeros to start the columns' largest magnitudes from.
 __global__ void __launch_bounds__(256) token_kernel(LossEpi e, Token t, int64_t M, int64_t padded, const int *idx,
-                                                    const int *count) {
+                                                    const int *count, uint32_t *top, int64_t tops) {
     const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    for (int64_t k = c; k < tops; k += (int64_t)gridDim.x * 256) top[k] = 0u;
     if (c >= padded) return;
     if (count) M = *count;
     float scale = 0.f, lse = 0.f;
@@ -515,7 +605,8 @@ struct Layout {
     Operands ops;
     int64_t Mp, Mq, Vp, vp;
     Choice dx;
-    size_t tokens, wt, gt, acc, total;
+    size_t tokens, tops, xs, wt, gt, acc, total;
+    int64_t nq;
 };
 Layout layout_of(int64_t M, int64_t n, int64_t V) {
     Layout l;
@@ -535,6 +626,9 @@ Layout layout_of(int64_t M, int64_t n, int64_t V) {
     splits = splits < room ? splits : room;
     l.dx = choose(n, M, splits < 1 ? 1 : splits);
     l.tokens = space.take((size_t)l.Mq * 12);
+    l.nq = up(n, 256) + 256;
+    l.tops = space.take((size_t)l.nq * 8);
+    l.xs = space.take((size_t)(M * l.ops.np) * 2);
     l.wt = space.take((size_t)(n * l.Vp) * 2);
     l.gt = space.take((size_t)(l.vp * l.Mp) * 2);
     l.acc = space.take((size_t)(l.dx.splits * n * l.Mp) * 4);
@@ -588,13 +682,27 @@ hipError_t launch_loss_mfma_grad(const LossPass &p, const LossEpi &e, hipStream_
     tok.scale = reinterpret_cast<float *>(ws + l.tokens);
     tok.lse2 = tok.scale + l.Mq;
     tok.target = reinterpret_cast<int *>(tok.lse2 + l.Mq);
-    token_kernel<<<(unsigned)(l.Mq / 256), 256, 0, s>>>(e, tok, p.M, l.Mq, r.idx, r.count);
+    uint32_t *const x_top = reinterpret_cast<uint32_t *>(ws + l.tops), *const w_top = x_top + l.nq;
+    token_kernel<<<(unsigned)(l.Mq / 256), 256, 0, s>>>(e, tok, p.M, l.Mq, r.idx, r.count, x_top, 2 * l.nq);
     err = hipGetLastError();
+    const int np = (int)l.ops.np, n = (int)p.n;
+    const auto top_grid = [&](int64_t rows) {
+        const int64_t blocks = (rows + 63) / 64;
+        return dim3((unsigned)(blocks < 1024 ? blocks : 1024), (unsigned)((n + 255) / 256));
+    };
+    if (err == hipSuccess && p.dW) {
+        const int64_t blocks = (p.M * (np / 8) + 255) / 256;
+        column_top_kernel<<<top_grid(p.M), 256, 0, s>>>(r.X, tok.scale, p.M, n, np, r.count, x_top);
+        scale_kernel<<<(unsigned)(blocks < 16384 ? blocks : 16384), 256, 0, s>>>(r.X, tok.scale, x_top, at(l.xs), p.M, np,
+                                                                                 r.count);
+        err = hipGetLastError();
+    }
     if (err == hipSuccess && p.dX) {
-        transpose_kernel<<<dim3((unsigned)(l.Vp / 64), (unsigned)(l.ops.np / 64)), 256, 0, s>>>(
-            static_cast<const uint16_t *>(p.W), at(l.wt), p.V, (int)p.n, l.Vp);
+        const uint16_t *W = static_cast<const uint16_t *>(p.W);
+        column_top_kernel<<<top_grid(p.V), 256, 0, s>>>(W, nullptr, p.V, n, n, nullptr, w_top);
+        transpose_kernel<<<dim3((unsigned)(l.Vp / 64), (unsigned)(np / 64)), 256, 0, s>>>(W, w_top, at(l.wt), p.V, n, l.Vp);
         if (r.count)
-            zero_rows_kernel<<<(unsigned)(p.M < 8192 ? p.M : 8192), 256, 0, s>>>(e, static_cast<uint16_t *>(p.dX), p.M, (int)p.n);
+            zero_rows_kernel<<<(unsigned)(p.M < 8192 ? p.M : 8192), 256, 0, s>>>(e, static_cast<uint16_t *>(p.dX), p.M, n);
         err = hipGetLastError();
     }
     float *acc = reinterpret_cast<float *>(ws + l.acc);
@@ -616,8 +724,10 @@ hipError_t launch_loss_mfma_grad(const LossPass &p, const LossEpi &e, hipStream_
         if (err == hipSuccess && p.dW) {
             g.A = at(l.gt);
             g.lda = g.K = l.Mp;
+            g.B = at(l.xs);
             g.rows_b = p.M;
             g.J = g.ldo = p.n;
+            g.col_top = x_top;
             g.out = static_cast<uint16_t *>(p.dW) + v0 * p.n;
             err = launch<true, kDw>(g, choose(g.I, g.J), s);
         }
@@ -637,7 +747,7 @@ hipError_t launch_loss_mfma_grad(const LossPass &p, const LossEpi &e, hipStream_
     }
     if (err == hipSuccess && p.dX) {
         round_transpose_kernel<<<dim3((unsigned)(l.Mp / 64), (unsigned)(l.ops.np / 64)), 256, 0, s>>>(
-            acc, l.dx.splits, static_cast<uint16_t *>(p.dX), p.M, (int)p.n, l.Mp, r.idx, r.count);
+            acc, l.dx.splits, tok.scale, w_top, static_cast<uint16_t *>(p.dX), p.M, (int)p.n, l.Mp, r.idx, r.count);
         err = hipGetLastError();
     }
     return err;

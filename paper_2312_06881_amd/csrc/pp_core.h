@@ -201,8 +201,9 @@ __device__ __forceinline__ void pp_read(uint32_t pa, const uint32_t (&pb)[TB ? S
 // LDS is free, and no load is in flight, when it returns (after a barrier).
 // Side B's fragments are the first MFMA operand, so a lane's four sums lie
 // along side B (4 (l / 16) + v) at row l % 16 of side A.
-template <int SM, int SN, bool TB, int SB, int NVA, int NVB, int SLOTA, int SLOTB, class IssueA, class IssueB,
-          class Addr, class Both>
+// F16: the operands are fp16.
+template <int SM, int SN, bool TB, int SB, int NVA, int NVB, int SLOTA, int SLOTB, bool F16 = false, class IssueA,
+          class IssueB, class Addr, class Both>
 __device__ __forceinline__ void pp_loop(int units, int wave, f32x4_t (&acc)[SM][SN], IssueA issue_a, IssueB issue_b,
                                         Addr addr, Both both) {
     bf16x8_t a[SM], b[SN];
@@ -224,8 +225,14 @@ __device__ __forceinline__ void pp_loop(int units, int wave, f32x4_t (&acc)[SM][
 #pragma unroll
         for (int j = 0; j < SN; ++j)
 #pragma unroll
-            for (int i = 0; i < SM; ++i)
-                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], a[i], acc[i][j], 0, 0, 0);
+            for (int i = 0; i < SM; ++i) {
+                typedef __attribute__((ext_vector_type(8))) _Float16 f16x8_t;
+                if constexpr (F16)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+                        __builtin_bit_cast(f16x8_t, b[j]), __builtin_bit_cast(f16x8_t, a[i]), acc[i][j], 0, 0, 0);
+                else
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], a[i], acc[i][j], 0, 0, 0);
+            }
         __builtin_amdgcn_s_setprio(0);
     };
     for (int d = 0; d < units; ++d) {

@@ -2,8 +2,10 @@
 
 fp32 sums of n products are taken to be within 6 sqrt(n) 2^-24 of the sum of the products' magnitudes
 (rounding errors of either sign add up like a random walk; its own bound n 2^-24 is never nearly reached).
-In bf16 the logits' gradient is rounded before it is multiplied: each term of dX and dW is off by up to
-2^-8 of itself, of either sign, together 6 2^-8 times the root of the sum of their squares.
+With bf16 operands the logits' gradient and the token (times the loss's gradient) are rounded to fp16 before they
+are multiplied: each term of dX and dW is off by up to 2 2^-11 of itself, of either sign, together 6 2^-10 times
+the root of the sum of their squares.  fp16's smallest step is 2^-24, so a value held as itself times 2^15, as G is, is
+also off by up to 2^-40, and one of a column whose largest magnitude c was taken to 2^14 or more by up to c 2^-39.
 """
 import math
 
@@ -63,11 +65,18 @@ def check(x, w, t, reduction="mean", ignore=-100, dloss=None, no_grad=False):
     hot = torch.zeros_like(p).scatter_(1, at[:, None], 1.0)
     G = scale[:, None] * (p - hot)
     Gm = scale.abs()[:, None] * ((2 * dz[:, None] + 2.0 ** -22) * p + 2.0 ** -23 * (p + hot))  # how far G's values are off
-    half = 2.0 ** -8 if x.dtype is BF else 0.0
+    half = 2.0 ** -10 if x.dtype is BF else 0.0
     for name, out, A, B, E in (("dx", dx, G, wd, Gm), ("dw", dw, G.t().contiguous(), xd, Gm.t().contiguous())):
         want = A @ B
         assert out.dtype is x.dtype and out.shape == want.shape
         tol = (x.dtype is BF) * 2.0 ** -8 * want.abs() + 2.0 ** -24 * want.abs() + E @ B.abs()
+        if x.dtype is BF:
+            P = (p - hot).abs()
+            Sx, Sc = scale.abs()[:, None] * xd.abs(), (scale.abs()[:, None] * xd.abs()).amax(0)
+            if name == "dx":
+                tol += scale.abs()[:, None] * (2.0 ** -40 * wd.abs().sum(0) + 2.0 ** -39 * P.sum(1)[:, None] * wd.abs().amax(0))
+            else:
+                tol += 2.0 ** -40 * Sx.sum(0) + 2.0 ** -39 * P.sum(0)[:, None] * Sc
         tol += 6 * half * ((A * A) @ (B * B)).sqrt() + 6 * math.sqrt(A.shape[1]) * 2.0 ** -24 * (A.abs() @ B.abs()) + 1e-37
         err = (out.double() - want).abs()
         assert (err <= tol).all(), (name, float((err / tol).max()))
