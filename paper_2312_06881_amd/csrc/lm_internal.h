@@ -139,7 +139,10 @@ hipError_t launch_loss_forward(const LossPass &p, hipStream_t s);
 hipError_t launch_loss_backward(const LossPass &p, hipStream_t s);
 size_t loss_workspace(bool backward, int64_t M, int64_t n, int64_t V, int dtype);
 
-// fp32 (loss_f32.hip).  Forward: the statistics.  Backward: a piece of the vocabulary,
+// Splitting fp32 operands takes a pass over the weights, which fewer tokens do not pay for.
+constexpr int64_t kSplitFrom = 129;
+
+// fp32 up to there (loss_f32.hip).  Forward: the statistics.  Backward: a piece of the vocabulary,
 // columns v0 .. v0 + vp - 1: the logits' gradient G [M][vp], then dX (added to, but for the
 // first piece) and dW of the piece; either may be null.
 int loss_f32_tiles(int64_t M, int64_t V);
@@ -148,11 +151,11 @@ hipError_t launch_loss_f32_piece(const LossPass &p, const LossEpi &e, int64_t v0
                                  hipStream_t s);
 
 
-// bf16 (loss_mfma.hip).  The statistics (ws: forward_bytes), and the whole backward pass (the
+// bf16, and fp32 from kSplitFrom tokens (loss_mfma.hip).  The statistics (ws: forward_bytes), and the whole backward pass (the
 // call's workspace: backward_bytes).
 int loss_mfma_tiles(int64_t M, int64_t V);
-size_t loss_mfma_forward_bytes(int64_t M, int64_t n, int64_t V);
-size_t loss_mfma_backward_bytes(int64_t M, int64_t n, int64_t V);
+size_t loss_mfma_forward_bytes(int64_t M, int64_t n, int64_t V, bool f32);
+size_t loss_mfma_backward_bytes(int64_t M, int64_t n, int64_t V, bool f32);
 // Which token row c of the statistics is, and how many rows there are; null: c, and all.
 struct LossTokens {
     const int *idx, *count;

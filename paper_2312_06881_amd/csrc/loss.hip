@@ -68,6 +68,9 @@ __global__ void __launch_bounds__(256) zero_kernel(uint16_t *p, int64_t n) {
 
 int64_t up(int64_t v, int64_t q) { return (v + q - 1) / q * q; }
 
+// Which fp32 calls run on fp32 matrix instructions.
+bool plain_f32(int64_t M, int dtype) { return dtype == kF32 && M < kSplitFrom; }
+
 // Vocabulary columns of a piece in fp32: G within 256 MB, but for very many tokens.
 int64_t f32_piece(int64_t M, int64_t V) {
     int64_t vp = ((int64_t)256 << 20) / (4 * (M > 0 ? M : 1)) / 128 * 128;
@@ -94,9 +97,10 @@ LossEpi epi_of(const LossPass &p) {
 
 size_t loss_workspace(bool backward, int64_t M, int64_t n, int64_t V, int dtype) {
     if (M == 0) return 0;
-    const bool f32 = dtype == kF32;
-    if (backward) return f32 ? (size_t)(M * f32_piece(M, V)) * 4 : loss_mfma_backward_bytes(M, n, V);
-    return stats_bytes(M, f32 ? loss_f32_tiles(M, V) : loss_mfma_tiles(M, V)) + (f32 ? 0 : loss_mfma_forward_bytes(M, n, V));
+    const bool f32 = dtype == kF32, plain = plain_f32(M, dtype);
+    if (backward) return plain ? (size_t)(M * f32_piece(M, V)) * 4 : loss_mfma_backward_bytes(M, n, V, f32);
+    return plain ? stats_bytes(M, loss_f32_tiles(M, V))
+                 : stats_bytes(M, loss_mfma_tiles(M, V)) + loss_mfma_forward_bytes(M, n, V, f32);
 }
 
 hipError_t launch_loss_forward(const LossPass &p, hipStream_t s) {
@@ -106,12 +110,12 @@ hipError_t launch_loss_forward(const LossPass &p, hipStream_t s) {
         e.at_target = each + up(p.M, 4);
         e.part = reinterpret_cast<float2 *>(e.at_target + up(p.M, 4));
         if (p.reduction == kReduceNone) each = p.loss;
-        const bool f32 = p.dtype == kF32;
-        e.tiles = f32 ? loss_f32_tiles(p.M, p.V) : loss_mfma_tiles(p.M, p.V);
+        const bool plain = plain_f32(p.M, p.dtype);
+        e.tiles = plain ? loss_f32_tiles(p.M, p.V) : loss_mfma_tiles(p.M, p.V);
         LossTokens tokens{};
-        const hipError_t err = f32 ? launch_loss_f32_stats(p, e, s)
-                                   : launch_loss_mfma_stats(p, e, static_cast<char *>(p.ws) + stats_bytes(p.M, e.tiles), each,
-                                                            tokens, s);
+        const hipError_t err = plain ? launch_loss_f32_stats(p, e, s)
+                                     : launch_loss_mfma_stats(p, e, static_cast<char *>(p.ws) + stats_bytes(p.M, e.tiles),
+                                                              each, tokens, s);
         if (err != hipSuccess) return err;
         const int64_t blocks = (p.M + 3) / 4;
         loss_join_kernel<<<(unsigned)(blocks < 8192 ? blocks : 8192), 256, 0, s>>>(e, p.M, tokens, each, p.lse);
@@ -128,7 +132,7 @@ hipError_t launch_loss_backward(const LossPass &p, hipStream_t s) {
         return hipGetLastError();
     }
     const LossEpi e = epi_of(p);
-    if (p.dtype != kF32) return launch_loss_mfma_grad(p, e, s);
+    if (!plain_f32(p.M, p.dtype)) return launch_loss_mfma_grad(p, e, s);
     const int64_t piece = f32_piece(p.M, p.V);
     for (int64_t v0 = 0; v0 < p.V; v0 += piece) {
         const hipError_t err = launch_loss_f32_piece(p, e, v0, p.V - v0 < piece ? p.V - v0 : piece,

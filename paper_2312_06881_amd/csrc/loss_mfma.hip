@@ -1,4 +1,4 @@
-// The loss's matrix products in bf16, on the pipelined eight-wave tiles of pp_core.h:
+// The loss's matrix products on the pipelined eight-wave bf16 tiles of pp_core.h:
 //   kStats  Z = X W^T, tokens by vocabulary: per token (largest, sum of exponentials) of the tile
 //   kGrad   Z^T = W X^T of a piece of the vocabulary, as G^T = exp(Z^T - lse) - onehot
 //   kDw     dW = G^T (dloss X) of the piece
@@ -13,6 +13,12 @@
 // place of 1.7e-3), where eleven bits put an eighth of that.  fp16's range is met by powers of two:
 // 2^15 for G (values from 2^-29 on keep all bits), and one a column for the other two, which
 // takes the column's largest magnitude to 2^14 .. 2^15 and goes out again with the sums.
+//
+// fp32 operands (from kSplitFrom tokens) are split in three bf16 values, x = h + m + l with 8 bits
+// each, exact to 2^-27, and six of the nine products h h, h m, m h, h l, l h, m m are summed in
+// fp32; the others are below 2^-26 of the whole.  The reduction is six times as long at eight
+// times the rate of the fp32 matrix instructions (157 TFLOP/s, of which plain tiles get half).
+// G is split as it is formed, and holds dloss.
 //
 // Tokens that do not count take no part: from kCompactFrom tokens the others are gathered, in
 // order, and the kernels take their number from device memory (prompts and padding are often half
@@ -29,7 +35,7 @@ enum Kind { kStats, kGrad, kDw, kDx };
 
 // What the gradient's epilogue needs of a token, tokens past the last too.
 struct Token {
-    float *scale, *lse2;   // 0 where the token does not count; lse log2(e)
+    float *scale, *lse;    // dloss, 0 where the token does not count; lse, in bf16 times log2(e)
     int *target;           // -1 where it does not
 };
 
@@ -48,8 +54,31 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2_t));
 }
 
+// The planes (h 0, m 1, l 2) of the product that unit d of a split reduction multiplies.
+constexpr int kProducts = 6;
+__device__ __forceinline__ int plane_a(int d) { return 0x120100 >> (4 * (d % kProducts)) & 15; }
+__device__ __forceinline__ int plane_b(int d) { return 0x102010 >> (4 * (d % kProducts)) & 15; }
+
+// Eight values as three planes of eight bf16; an infinity or NaN stays in the first alone.
+__device__ __forceinline__ void split8(const float (&v)[8], uint4 (&p)[3]) {
+    float r[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = v[e];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        const uint32_t w[4] = {pack_bf16(r[0], r[1]), pack_bf16(r[2], r[3]), pack_bf16(r[4], r[5]), pack_bf16(r[6], r[7])};
+        p[k] = make_uint4(w[0], w[1], w[2], w[3]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float h = unpack_bf16(w[e >> 1], e & 1);
+            r[e] = (__float_as_uint(h) & 0x7f800000u) != 0x7f800000u ? r[e] - h : 0.f;
+        }
+    }
+}
+
 struct Args {
     const uint16_t *A, *B;
+    int64_t plane_a, plane_b, plane_out;   // values from one plane to the next (fp32)
     int64_t lda, ldb, I, J, K;   // K: a multiple of 64
     int64_t rows_b;              // side B's rows where they are the reduction's indices
     int group;
@@ -59,7 +88,7 @@ struct Args {
     Token tok;
     const uint32_t *col_top;     // kDw: of the columns of dloss X
     int64_t v0;
-    uint16_t *out;
+    void *out;
     float *acc;
     int64_t ldo;
     bool first;
@@ -95,7 +124,7 @@ __device__ __forceinline__ uint4 pack_pair(const float (&x)[8], Pack pack) {
 }
 __device__ __forceinline__ int lane_piece(int lg) { return (lg & 1) * 16 + (lg >> 1) * 8; }
 
-template <int BM, int BN, int WGM, int WGN, bool TB, Kind KIND>
+template <int BM, int BN, int WGM, int WGN, bool TB, Kind KIND, bool F32>
 __global__ void __launch_bounds__(kPPThreads, 1) loss_pp_kernel(Args g) {
     using C = Cfg<BM, BN, WGM, WGN, TB>;
     using SA = typename C::A;
@@ -127,7 +156,7 @@ __global__ void __launch_bounds__(kPPThreads, 1) loss_pp_kernel(Args g) {
     const int tile_j = item % run / gm;
     const int64_t j0 = (int64_t)tile_j * BN;
     const int64_t left_i = g.I - i0 < BM ? g.I - i0 : BM, left_j = g.J - j0 < BN ? g.J - j0 : BN;
-    const int all = (int)(g.K / kPPK);
+    const int all = (int)(g.K / kPPK) * (F32 ? kProducts : 1);
     const int u0 = KIND == kDx ? (int)((int64_t)all * split / g.splits) : 0;
     const int units = (KIND == kDx ? (int)((int64_t)all * (split + 1) / g.splits) : all) - u0;
 
@@ -153,22 +182,29 @@ __global__ void __launch_bounds__(kPPThreads, 1) loss_pp_kernel(Args g) {
     const auto clamp = [&](int d) { return u0 + (d < units ? d : units - 1); };
     auto issue_a = [&](int d) {
         lds_u8 *slot = lds + d % C::kSlotA * SA::kBytes;
-        const uint32_t so = (uint32_t)clamp(d) * (uint32_t)(2 * kPPK);
+        const int u = clamp(d), k = F32 ? u / kProducts : u;
+        const uint32_t so = (uint32_t)k * (uint32_t)(2 * kPPK);
+        __amdgpu_buffer_rsrc_t r = rA;
+        if constexpr (F32) r = buffer_rsrc(g.A + plane_a(u) * g.plane_a + i0 * g.lda, (uint32_t)(left_i * g.lda * 2));
 #pragma unroll
-        for (int q = 0; q < SA::kPer; ++q) dma16(rA, slot + loA[q], voA[q], so);
+        for (int q = 0; q < SA::kPer; ++q) dma16(r, slot + loA[q], voA[q], so);
     };
     auto issue_b = [&](int d) {
         lds_u8 *slot = lds + d % C::kSlotB * SB::kBytes;
+        const int u = clamp(d), k = F32 ? u / kProducts : u;
+        const uint16_t *plane = g.B;
+        if constexpr (F32) plane += plane_b(u) * g.plane_b;
         __amdgpu_buffer_rsrc_t r = rB0;
         uint32_t so = 0;
         if constexpr (TB) {
             // the rows of this unit: their offsets pass 32 bits over the reduction, and those
             // past the last read zero
-            const int64_t k0 = (int64_t)clamp(d) * kPPK;
+            const int64_t k0 = (int64_t)k * kPPK;
             const int64_t rows = g.rows_b - k0 < kPPK ? g.rows_b - k0 : kPPK;
-            r = buffer_rsrc(g.B + k0 * g.ldb + j0, rows > 0 ? (uint32_t)((rows * g.ldb - j0) * 2) : 0u);
+            r = buffer_rsrc(plane + k0 * g.ldb + j0, rows > 0 ? (uint32_t)((rows * g.ldb - j0) * 2) : 0u);
         } else {
-            so = (uint32_t)clamp(d) * (uint32_t)(2 * kPPK);
+            so = (uint32_t)k * (uint32_t)(2 * kPPK);
+            if constexpr (F32) r = buffer_rsrc(plane + j0 * g.ldb, (uint32_t)(left_j * g.ldb * 2));
         }
 #pragma unroll
         for (int q = 0; q < SB::kPer; ++q) dma16(r, slot + loB[q], voB[q], so);
@@ -190,7 +226,7 @@ __global__ void __launch_bounds__(kPPThreads, 1) loss_pp_kernel(Args g) {
 #pragma unroll
         for (int j = 0; j < SN; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     if (units > 0)
-        pp_loop<SM, SN, TB, 4 * SB::kPitch, SA::kPer, SB::kPer, C::kSlotA, C::kSlotB, KIND == kDw || KIND == kDx>(
+        pp_loop<SM, SN, TB, 4 * SB::kPitch, SA::kPer, SB::kPer, C::kSlotA, C::kSlotB, !F32 && (KIND == kDw || KIND == kDx)>(
             units, wave, acc, issue_a, issue_b, addr, [](int) { return true; });
     // acc[i][j][v]: side A's row wm0 + 16 i + lr, side B's wn0 + 16 j + 4 lg + v
     if constexpr (KIND == kStats) {
@@ -199,28 +235,58 @@ __global__ void __launch_bounds__(kPPThreads, 1) loss_pp_kernel(Args g) {
         const int v_lane = (int)(g.v0 + i0) + wm0 + lr;
 #pragma unroll
         for (int jp = 0; jp < SN / 2; ++jp) {
-            float scale[8], lse2[8];
+            float scale[8], lse[8];
             int target[8];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int64_t t = j0 + wn0 + 32 * jp + 16 * h + 4 * lg;   // tokens are laid out for whole tiles
                 __builtin_memcpy(scale + 4 * h, __builtin_assume_aligned(g.tok.scale + t, 16), 16);
-                __builtin_memcpy(lse2 + 4 * h, __builtin_assume_aligned(g.tok.lse2 + t, 16), 16);
+                __builtin_memcpy(lse + 4 * h, __builtin_assume_aligned(g.tok.lse + t, 16), 16);
                 __builtin_memcpy(target + 4 * h, __builtin_assume_aligned(g.tok.target + t, 16), 16);
             }
             const int64_t col = j0 + wn0 + 32 * jp + lane_piece(lg);
-            uint16_t *o = g.out + (i0 + wm0 + lr) * g.ldo + col;
+            uint16_t *o = static_cast<uint16_t *>(g.out) + (i0 + wm0 + lr) * g.ldo + col;
 #pragma unroll
             for (int i = 0; i < SM; ++i) {
                 float x[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float z = acc[i][2 * jp + (e >> 2)][e & 3];
-                    const float p = __builtin_amdgcn_exp2f(fmaf(z, kLog2e, -lse2[e])) - (target[e] == v_lane + 16 * i ? 1.f : 0.f);
-                    x[e] = scale[e] != 0.f ? p * (float)(1 << kGExp) : 0.f;   // zero whatever p is
+                    const float p = __builtin_amdgcn_exp2f(F32 ? (z - lse[e]) * kLog2e : fmaf(z, kLog2e, -lse[e])) - (target[e] == v_lane + 16 * i ? 1.f : 0.f);
+                    x[e] = scale[e] != 0.f ? p * (F32 ? scale[e] : (float)(1 << kGExp)) : 0.f;   // zero whatever p is
                 }
-                const uint4 w = pack_pair(x, pack_f16);
-                if (col < g.ldo && i0 + wm0 + 16 * i + lr < g.I) *reinterpret_cast<uint4 *>(o + (int64_t)(16 * i) * g.ldo) = w;
+                const bool in = col < g.ldo && i0 + wm0 + 16 * i + lr < g.I;
+                if constexpr (F32) {
+                    uint4 p[3];
+                    split8(x, p);
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) {
+                        swap_lane_rows(p[k].x, p[k].z);
+                        swap_lane_rows(p[k].y, p[k].w);
+                        if (in) *reinterpret_cast<uint4 *>(o + k * g.plane_out + (int64_t)(16 * i) * g.ldo) = p[k];
+                    }
+                } else {
+                    const uint4 w = pack_pair(x, pack_f16);
+                    if (in) *reinterpret_cast<uint4 *>(o + (int64_t)(16 * i) * g.ldo) = w;
+                }
+            }
+        }
+    } else if constexpr (KIND == kDw && F32) {
+#pragma unroll
+        for (int i = 0; i < SM; ++i) {
+            const int64_t row = i0 + wm0 + 16 * i + lr;
+#pragma unroll
+            for (int j = 0; j < SN; ++j) {
+                const int64_t col = j0 + wn0 + 16 * j + 4 * lg;
+                if (row >= g.I) continue;
+                float *o = static_cast<float *>(g.out) + row * g.ldo + col;
+                if (col + 4 <= g.J) {
+                    __builtin_memcpy(o, &acc[i][j], 16);
+                } else {
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+                        if (col + v < g.J) o[v] = acc[i][j][v];
+                }
             }
         }
     } else if constexpr (KIND == kDw) {
@@ -243,7 +309,7 @@ __global__ void __launch_bounds__(kPPThreads, 1) loss_pp_kernel(Args g) {
                 for (int e = 0; e < 8; ++e) x[e] = ldexpf(acc[i][2 * jp + (e >> 2)][e & 3], back[e]);
                 const uint4 w = pack_pair(x, pack_bf16);
                 if (row >= g.I) continue;
-                uint16_t *o = g.out + row * g.ldo + col;
+                uint16_t *o = static_cast<uint16_t *>(g.out) + row * g.ldo + col;
                 if (col + 8 <= g.J) {
                     __builtin_memcpy(o, &w, 16);
                 } else {
@@ -275,35 +341,56 @@ __global__ void __launch_bounds__(kPPThreads, 1) loss_pp_kernel(Args g) {
 }
 
 // The tokens that count, in order: their places idx, their targets and how many; the others'
-// loss and lse are zero (forward).  One workgroup, a run of tokens a thread.
+// loss and lse are zero (forward).  One workgroup, eight tokens a thread at a time (16384 tokens
+// 20 us; a run of tokens a thread, read twice, took 39).
 __global__ void __launch_bounds__(1024) compact_kernel(LossEpi e, int64_t M, int *idx, int64_t *targets, int *count,
                                                        float *loss, float *lse) {
-    __shared__ int sums[16];
+    __shared__ int sums[2][16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t per = (M + 1023) / 1024, m0 = tid * per, m1 = m0 + per < M ? m0 + per : M;
-    int n = 0;
-    for (int64_t m = m0; m < m1; ++m) n += loss_counts(e, e.targets[m]) ? 1 : 0;
-    int before = n;
+    int total = 0, parity = 0;
+    for (int64_t base = 0; base < M; base += 8192, parity ^= 1) {
+        const int64_t m0 = base + 8 * tid;
+        int64_t t[8];
+        uint32_t in = 0;
 #pragma unroll
-    for (int w = 1; w < 64; w <<= 1) {
-        const int t = __shfl_up(before, w);
-        if (lane >= w) before += t;
-    }
-    if (lane == 63) sums[wave] = before;
-    __syncthreads();
-    before -= n;
-    for (int w = 0; w < wave; ++w) before += sums[w];
-    if (tid == 1023) *count = before + n;
-    for (int64_t m = m0; m < m1; ++m) {
-        const int64_t t = e.targets[m];
-        if (loss_counts(e, t)) {
-            idx[before] = (int)m;
-            targets[before++] = t;
-        } else if (loss) {
-            loss[m] = 0.f;
-            lse[m] = 0.f;
+        for (int k = 0; k < 8; ++k) t[k] = m0 + k < M ? e.targets[m0 + k] : -1;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) in |= loss_counts(e, t[k]) ? 1u << k : 0u;
+        const int n = __popc(in);
+        int before = n;
+#pragma unroll
+        for (int w = 1; w < 64; w <<= 1) {
+            const int up = __shfl_up(before, w);
+            if (lane >= w) before += up;
+        }
+        if (lane == 63) sums[parity][wave] = before;
+        __syncthreads();
+        before += total - n;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) {
+            const int c = sums[parity][w];
+            before += w < wave ? c : 0;
+            total += c;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (in >> k & 1u) {
+                idx[before] = (int)(m0 + k);
+                targets[before++] = t[k];
+            } else if (loss && m0 + k < M) {
+                loss[m0 + k] = 0.f;
+                lse[m0 + k] = 0.f;
+            }
         }
     }
+    if (tid == 0) *count = total;
+}
+
+// Row and first column of octet i of rows of np columns.
+__device__ __forceinline__ void octet_at(int64_t i, int64_t total, int np, int64_t &r, int &c) {
+    const uint32_t per = (uint32_t)np / 8;
+    r = total >> 32 ? i / per : (int64_t)((uint32_t)i / per);   // the 64-bit division takes longer than the copy
+    c = (int)(i - r * per) * 8;
 }
 
 // dst[r][c] = src[idx[r]][c] for c < n, else 0, c < np (a multiple of 64).  idx null: row r;
@@ -313,19 +400,68 @@ __global__ void __launch_bounds__(256) gather_kernel(const uint16_t *src, uint16
     if (count) rows = *count;
     const int64_t total = rows * (np / 8);
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        const int64_t r = i / (np / 8);
-        const int c = (int)(i - r * (np / 8)) * 8;
+        int64_t r;
+        int c;
+        octet_at(i, total, np, r, c);
         float v[8];
         load_cols<true>(src + (idx ? idx[r] : r) * n, c, n, v);
         store8(dst + r * np + c, v);
     }
 }
 
+// The same of fp32 rows, as three planes.
+__global__ void __launch_bounds__(256) gather_split_kernel(const float *src, uint16_t *dst, int64_t plane, int64_t rows, int n,
+                                                           int np, const int *idx, const int *count) {
+    if (count) rows = *count;
+    const int64_t total = rows * (np / 8);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        int64_t r;
+        int c;
+        octet_at(i, total, np, r, c);
+        float v[8];
+        load_cols<true>(src + (idx ? idx[r] : r) * n, c, n, v);
+        uint4 p[3];
+        split8(v, p);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4 *>(dst + k * plane + r * np + c) = p[k];
+    }
+}
+
+// dst[c][r] = src[r][c] of fp32 rows for r < rows, else 0, r < ld, as three planes: 64 x 64 tiles.
+__global__ void __launch_bounds__(256) transpose_split_kernel(const float *src, uint16_t *dst, int64_t plane, int64_t rows,
+                                                              int n, int64_t ld) {
+    __shared__ float t[64][65];
+    const int64_t r0 = (int64_t)blockIdx.x * 64;
+    const int c0 = blockIdx.y * 64, tid = threadIdx.x;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const int r = (tid + 256 * q) / 8, c = (tid + 256 * q) % 8 * 8;
+        float v[8] = {};
+        if (r0 + r < rows) load_cols<true>(src + (r0 + r) * n, c0 + c, n, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t[c + e][r] = v[e];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const int c = (tid + 256 * q) / 8, r = (tid + 256 * q) % 8 * 8;
+        if (c0 + c >= n) continue;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = t[c][r + e];
+        uint4 p[3];
+        split8(v, p);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4 *>(dst + k * plane + (int64_t)(c0 + c) * ld + r0 + r) = p[k];
+    }
+}
+
 // Rows of tokens that do not count: their gradient is zero.
-__global__ void __launch_bounds__(256) zero_rows_kernel(LossEpi e, uint16_t *dx, int64_t M, int n) {
+template <class T>
+__global__ void __launch_bounds__(256) zero_rows_kernel(LossEpi e, T *dx, int64_t M, int n) {
     for (int64_t m = blockIdx.x; m < M; m += gridDim.x) {
         if (loss_counts(e, e.targets[m])) continue;
-        for (int c = threadIdx.x; c < n; c += 256) dx[m * n + c] = 0;
+        for (int c = threadIdx.x; c < n; c += 256) dx[m * n + c] = T(0);
     }
 }
 
@@ -365,14 +501,16 @@ __global__ void __launch_bounds__(256) scale_kernel(const uint16_t *src, const f
     if (count) rows = *count;
     const int64_t total = rows * (np / 8);
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        const int64_t m = i / (np / 8);
-        const int c = (int)(i - m * (np / 8)) * 8;
+        int64_t m;
+        int c;
+        octet_at(i, total, np, m, c);
         float v[8];
         load8(src + m * np + c, v);
         const float s = scale[m];
-        uint32_t w[4];
+        uint32_t w[4], b[8];
+        __builtin_memcpy(b, __builtin_assume_aligned(top + c, 16), 32);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = s != 0.f ? ldexpf(v[e] * s, column_exp(top[c + e])) : 0.f;
+        for (int e = 0; e < 8; ++e) v[e] = s != 0.f ? ldexpf(v[e] * s, column_exp(b[e])) : 0.f;
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[e] = pack_f16(v[2 * e], v[2 * e + 1]);
         __builtin_memcpy(__builtin_assume_aligned(dst + m * np + c, 16), w, 16);
@@ -413,10 +551,13 @@ __global__ void __launch_bounds__(256) transpose_kernel(const uint16_t *src, con
     }
 }
 
-// dX[idx[m]][c] = scale[m] times the fp32 sums acc[split][c][m], added in order, rounded: 64 x 64 tiles.
+// dX[idx[m]][c] = the fp32 sums acc[split][c][m] added in order, in bf16 times scale[m] at the
+// column's scale: 64 x 64 tiles.
+template <class T>
 __global__ void __launch_bounds__(256) round_transpose_kernel(const float *acc, int splits, const float *scale,
-                                                              const uint32_t *top, uint16_t *dst, int64_t M, int n,
+                                                              const uint32_t *top, T *dst, int64_t M, int n,
                                                               int64_t ld, const int *idx, const int *count) {
+    constexpr bool kBf16 = sizeof(T) == 2;
     __shared__ float t[64][65];
     if (count) M = *count;
     const int64_t m0 = (int64_t)blockIdx.x * 64;
@@ -435,7 +576,7 @@ __global__ void __launch_bounds__(256) round_transpose_kernel(const float *acc, 
                 for (int e = 0; e < 4; ++e) v[e] += u[e];
             }
         }
-        const int back = c0 + c < n ? -(column_exp(top[c0 + c]) + kGExp) : 0;
+        const int back = kBf16 && c0 + c < n ? -(column_exp(top[c0 + c]) + kGExp) : 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) t[m + e][c] = ldexpf(v[e], back);
     }
@@ -444,7 +585,7 @@ __global__ void __launch_bounds__(256) round_transpose_kernel(const float *acc, 
     for (int q = 0; q < 2; ++q) {
         const int m = (tid + 256 * q) / 8, c = (tid + 256 * q) % 8 * 8;
         if (m0 + m >= M) continue;
-        const float by = scale[m0 + m];
+        const float by = kBf16 ? scale[m0 + m] : 1.f;
         float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = by != 0.f ? t[m][c + e] * by : 0.f;
@@ -454,7 +595,7 @@ __global__ void __launch_bounds__(256) round_transpose_kernel(const float *acc, 
 
 // The tokens' part of the gradient, and zeros to start the columns' largest magnitudes from.
 __global__ void __launch_bounds__(256) token_kernel(LossEpi e, Token t, int64_t M, int64_t padded, const int *idx,
-                                                    const int *count, uint32_t *top, int64_t tops) {
+                                                    const int *count, float lse_by, uint32_t *top, int64_t tops) {
     const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
     for (int64_t k = c; k < tops; k += (int64_t)gridDim.x * 256) top[k] = 0u;
     if (c >= padded) return;
@@ -470,18 +611,18 @@ __global__ void __launch_bounds__(256) token_kernel(LossEpi e, Token t, int64_t 
         }
     }
     t.scale[c] = scale;
-    t.lse2[c] = lse * kLog2e;
+    t.lse[c] = lse * lse_by;
     t.target[c] = target;
 }
 
-// Tiles: rows of side A and B, and the time of a round of them next to 256 x 256's, with one, two
-// or three workgroups on every CU (measured at 768, 1000 and 4096 wide; the wide ones fill a CU).
+// Tiles: rows of side A and B, workgroups to a CU, the time of a round of them on all 256 CUs next
+// to 256 x 256's (measured at 4096 wide: 800, 903, 1129 and 1386 us for the same logits), and
+// that of a tile where they are few, when clocks are higher and less is shared.
 struct Tile {
     int bm, bn, per_cu;
-    double time[3];
+    double round, alone;
 };
-constexpr Tile kTiles[] = {
-    {256, 256, 1, {1.0}}, {192, 256, 1, {0.85}}, {128, 128, 2, {0.36, 0.62}}, {64, 128, 3, {0.22, 0.38, 0.54}}};
+constexpr Tile kTiles[] = {{256, 256, 1, 1.0, 0.77}, {192, 256, 1, 0.79, 0.74}, {128, 128, 2, 0.694, 0.33}, {64, 128, 3, 0.66, 0.2}};
 
 struct Choice {
     int tile, splits;
@@ -494,36 +635,45 @@ Choice choose(int64_t I, int64_t J, int64_t most_splits = 1) {
     for (int t = 0; t < 4; ++t) {
         const Tile &k = kTiles[t];
         const int64_t tiles = ((I + k.bm - 1) / k.bm) * ((J + k.bn - 1) / k.bn);
-        int64_t splits = 256 / tiles;
-        splits = splits > most_splits ? most_splits : splits < 1 ? 1 : splits;
-        const int64_t count = tiles * splits, round = 256 * k.per_cu, rest = (count % round + 255) / 256;
-        const double time = ((double)(count / round) * k.time[k.per_cu - 1] + (rest ? k.time[rest - 1] : 0.0)) / (double)splits;
-        if (t == 0 || time < least) {
-            best = {t, (int)splits};
-            least = time;
+        for (int w = 1; w <= k.per_cu; ++w) {
+            int64_t splits = 256 * w / tiles;
+            splits = splits > most_splits ? most_splits : splits < 1 ? 1 : splits;
+            const int64_t count = tiles * splits, round = 256 * k.per_cu;
+            const double rest = k.round * (double)(count % round) / (double)round;
+            const double last = count % round == 0 ? 0.0 : rest > k.alone ? rest : k.alone;
+            const double time = (k.round * (double)(count / round) + last) / (double)splits;
+            if (least == 0 || time < least) {
+                best = {t, (int)splits};
+                least = time;
+            }
         }
     }
     return best;
 }
 
-template <int BM, int BN, int WGM, int WGN, bool TB, Kind KIND>
+template <int BM, int BN, int WGM, int WGN, bool TB, Kind KIND, bool F32>
 hipError_t launch_tile(Args &g, hipStream_t s) {
     const int64_t tiles = ((g.I + BM - 1) / BM) * ((g.J + BN - 1) / BN) * g.splits;
     if (tiles >= (int64_t)1 << 31) return hipErrorNotSupported;
     g.group = 8;
-    loss_pp_kernel<BM, BN, WGM, WGN, TB, KIND><<<(unsigned)tiles, kPPThreads, 0, s>>>(g);
+    loss_pp_kernel<BM, BN, WGM, WGN, TB, KIND, F32><<<(unsigned)tiles, kPPThreads, 0, s>>>(g);
     return hipGetLastError();
 }
 
-template <bool TB, Kind KIND>
-hipError_t launch(Args g, const Choice &c, hipStream_t s) {
-    g.splits = c.splits;
+template <bool TB, Kind KIND, bool F32>
+hipError_t launch_as(Args &g, const Choice &c, hipStream_t s) {
     switch (c.tile) {
-    case 0: return launch_tile<256, 256, 2, 4, TB, KIND>(g, s);
-    case 1: return launch_tile<192, 256, 2, 4, TB, KIND>(g, s);
-    case 2: return launch_tile<128, 128, 2, 4, TB, KIND>(g, s);
-    default: return launch_tile<64, 128, 2, 4, TB, KIND>(g, s);
+    case 0: return launch_tile<256, 256, 2, 4, TB, KIND, F32>(g, s);
+    case 1: return launch_tile<192, 256, 2, 4, TB, KIND, F32>(g, s);
+    case 2: return launch_tile<128, 128, 2, 4, TB, KIND, F32>(g, s);
+    default: return launch_tile<64, 128, 2, 4, TB, KIND, F32>(g, s);
     }
+}
+
+template <bool TB, Kind KIND>
+hipError_t launch(Args g, const Choice &c, bool f32, hipStream_t s) {
+    g.splits = c.splits;
+    return f32 ? launch_as<TB, KIND, true>(g, c, s) : launch_as<TB, KIND, false>(g, c, s);
 }
 
 // Below this the launches that gather would take longer than what they save.
@@ -531,14 +681,6 @@ constexpr int64_t kCompactFrom = 257;
 
 int64_t up(int64_t v, int64_t q) { return (v + q - 1) / q * q; }
 size_t part(size_t bytes) { return (bytes + 255) / 256 * 256; }
-
-hipError_t gather(const void *src, uint16_t *dst, int64_t rows, int64_t n, int64_t np, const int *idx, const int *count,
-                  hipStream_t s) {
-    const int64_t blocks = (rows * (np / 8) + 255) / 256;
-    gather_kernel<<<(unsigned)(blocks < 16384 ? blocks : 16384), 256, 0, s>>>(static_cast<const uint16_t *>(src), dst, rows,
-                                                                              (int)n, (int)np, idx, count);
-    return hipGetLastError();
-}
 
 // Where things lie in the workspace; a size of 0 for what a call does not need.
 struct Space {
@@ -550,21 +692,22 @@ struct Space {
     }
 };
 
-// The tokens that count and the operands as the kernels read them.
+// The tokens that count and the operands as the kernels read them; in fp32 three planes each.
 struct Operands {
     int64_t np;                  // columns
-    bool compact;
+    bool compact, f32;
     size_t idx, targets, count, x, w;
 };
-Operands operands_of(Space &space, int64_t M, int64_t n, int64_t V) {
+Operands operands_of(Space &space, int64_t M, int64_t n, int64_t V, bool f32) {
     Operands o;
     o.np = up(n, kPPK);
     o.compact = M >= kCompactFrom;
+    o.f32 = f32;
     o.idx = space.take(o.compact ? (size_t)M * 4 : 0);
     o.targets = space.take(o.compact ? (size_t)M * 8 : 0);
     o.count = space.take(o.compact ? 4 : 0);
-    o.x = space.take(o.compact || o.np != n ? (size_t)(M * o.np) * 2 : 0);
-    o.w = space.take(o.np != n ? (size_t)(V * o.np) * 2 : 0);
+    o.x = space.take(f32 ? (size_t)(M * o.np) * 6 : o.compact || o.np != n ? (size_t)(M * o.np) * 2 : 0);
+    o.w = space.take(f32 ? (size_t)(V * o.np) * 6 : o.np != n ? (size_t)(V * o.np) * 2 : 0);
     return o;
 }
 
@@ -574,6 +717,16 @@ struct Prepared {
     const int *idx, *count;
     const int64_t *targets;
 };
+hipError_t gather(const void *src, uint16_t *dst, int64_t rows, int64_t n, int64_t np, bool f32, const int *idx,
+                  const int *count, hipStream_t s) {
+    const int64_t blocks = (rows * (np / 8) + 255) / 256;
+    const unsigned grid = (unsigned)(blocks < 16384 ? blocks : 16384);
+    if (f32)
+        gather_split_kernel<<<grid, 256, 0, s>>>(static_cast<const float *>(src), dst, rows * np, rows, (int)n, (int)np, idx, count);
+    else
+        gather_kernel<<<grid, 256, 0, s>>>(static_cast<const uint16_t *>(src), dst, rows, (int)n, (int)np, idx, count);
+    return hipGetLastError();
+}
 hipError_t prepare(const Operands &o, const LossPass &p, const LossEpi &e, char *ws, float *loss, float *lse, Prepared &r,
                    hipStream_t s) {
     r = {static_cast<const uint16_t *>(p.X), static_cast<const uint16_t *>(p.W), nullptr, nullptr, e.targets};
@@ -587,14 +740,14 @@ hipError_t prepare(const Operands &o, const LossPass &p, const LossEpi &e, char 
         r.count = count;
         r.targets = targets;
     }
-    if (err == hipSuccess && (o.compact || o.np != p.n)) {
+    if (err == hipSuccess && (o.compact || o.np != p.n || o.f32)) {
         uint16_t *x = reinterpret_cast<uint16_t *>(ws + o.x);
-        err = gather(p.X, x, p.M, p.n, o.np, r.idx, r.count, s);
+        err = gather(p.X, x, p.M, p.n, o.np, o.f32, r.idx, r.count, s);
         r.X = x;
     }
-    if (err == hipSuccess && o.np != p.n) {
+    if (err == hipSuccess && (o.np != p.n || o.f32)) {
         uint16_t *w = reinterpret_cast<uint16_t *>(ws + o.w);
-        err = gather(p.W, w, p.V, p.n, o.np, nullptr, nullptr, s);
+        err = gather(p.W, w, p.V, p.n, o.np, o.f32, nullptr, nullptr, s);
         r.W = w;
     }
     return err;
@@ -603,34 +756,34 @@ hipError_t prepare(const Operands &o, const LossPass &p, const LossEpi &e, char 
 // Vocabulary columns of a piece, and the workspace of a backward pass.
 struct Layout {
     Operands ops;
-    int64_t Mp, Mq, Vp, vp;
+    int64_t Mp, Mq, nq, Vp, vp;
     Choice dx;
     size_t tokens, tops, xs, wt, gt, acc, total;
-    int64_t nq;
 };
-Layout layout_of(int64_t M, int64_t n, int64_t V) {
+Layout layout_of(int64_t M, int64_t n, int64_t V, bool f32) {
     Layout l;
     Space space;
-    l.ops = operands_of(space, M, n, V);
+    const size_t value = f32 ? 6 : 2;    // bytes
+    l.ops = operands_of(space, M, n, V, f32);
     l.Mp = up(M, kPPK);
     l.Mq = up(M, 256) + 256;     // the last tile's tokens, whatever its width
+    l.nq = up(n, 256) + 256;
     l.Vp = up(V, kPPK);
     // G^T of a piece within 512 MB, but for very many tokens; pieces of one size, whole tiles
-    int64_t most = ((int64_t)512 << 20) / (2 * l.Mp) / 256 * 256;
+    int64_t most = ((int64_t)512 << 20) / ((int64_t)value * l.Mp) / 256 * 256;
     if (most < 2048) most = 2048;
     const int64_t pieces = (V + most - 1) / most;
     l.vp = up((V + pieces - 1) / pieces, 256);
-    // at least 16 units a split, and the splits' sums within the weights' gradient's size
-    int64_t splits = l.vp / kPPK / 16;
-    const int64_t room = l.vp / (2 * l.Mp);
+    // at least 16 units a split, and the splits' sums within 256 MB
+    int64_t splits = l.vp / kPPK * (f32 ? kProducts : 1) / 16;
+    const int64_t room = ((int64_t)64 << 20) / (n * l.Mp);
     splits = splits < room ? splits : room;
     l.dx = choose(n, M, splits < 1 ? 1 : splits);
     l.tokens = space.take((size_t)l.Mq * 12);
-    l.nq = up(n, 256) + 256;
-    l.tops = space.take((size_t)l.nq * 8);
-    l.xs = space.take((size_t)(M * l.ops.np) * 2);
-    l.wt = space.take((size_t)(n * l.Vp) * 2);
-    l.gt = space.take((size_t)(l.vp * l.Mp) * 2);
+    l.tops = space.take(f32 ? 0 : (size_t)l.nq * 8);
+    l.xs = space.take(f32 ? 0 : (size_t)(M * l.ops.np) * 2);
+    l.wt = space.take((size_t)(n * l.Vp) * value);
+    l.gt = space.take((size_t)(l.vp * l.Mp) * value);
     l.acc = space.take((size_t)(l.dx.splits * n * l.Mp) * 4);
     l.total = space.total;
     return l;
@@ -643,18 +796,19 @@ int loss_mfma_tiles(int64_t M, int64_t V) {
     return (int)((V + bn - 1) / bn);
 }
 
-size_t loss_mfma_forward_bytes(int64_t M, int64_t n, int64_t V) {
+size_t loss_mfma_forward_bytes(int64_t M, int64_t n, int64_t V, bool f32) {
     Space space;
-    operands_of(space, M, n, V);
+    operands_of(space, M, n, V, f32);
     return space.total;
 }
 
-size_t loss_mfma_backward_bytes(int64_t M, int64_t n, int64_t V) { return layout_of(M, n, V).total; }
+size_t loss_mfma_backward_bytes(int64_t M, int64_t n, int64_t V, bool f32) { return layout_of(M, n, V, f32).total; }
 
 hipError_t launch_loss_mfma_stats(const LossPass &p, const LossEpi &e, void *ws, float *each, LossTokens &tokens,
                                   hipStream_t s) {
     Space space;
-    const Operands o = operands_of(space, p.M, p.n, p.V);
+    const bool f32 = p.dtype == kF32;
+    const Operands o = operands_of(space, p.M, p.n, p.V, f32);
     Prepared r;
     hipError_t err = prepare(o, p, e, static_cast<char *>(ws), each, p.lse, r, s);
     if (err != hipSuccess) return err;
@@ -665,14 +819,17 @@ hipError_t launch_loss_mfma_stats(const LossPass &p, const LossEpi &e, void *ws,
     g.count = r.count;
     g.A = r.X;
     g.B = r.W;
+    g.plane_a = p.M * o.np;
+    g.plane_b = p.V * o.np;
     g.I = p.M;
     g.J = p.V;
     g.K = g.lda = g.ldb = o.np;
-    return launch<false, kStats>(g, choose(p.M, p.V), s);
+    return launch<false, kStats>(g, choose(p.M, p.V), f32, s);
 }
 
 hipError_t launch_loss_mfma_grad(const LossPass &p, const LossEpi &e, hipStream_t s) {
-    const Layout l = layout_of(p.M, p.n, p.V);
+    const bool f32 = p.dtype == kF32;
+    const Layout l = layout_of(p.M, p.n, p.V, f32);
     char *ws = static_cast<char *>(p.ws);
     const auto at = [&](size_t o) { return reinterpret_cast<uint16_t *>(ws + o); };
     Prepared r;
@@ -680,17 +837,19 @@ hipError_t launch_loss_mfma_grad(const LossPass &p, const LossEpi &e, hipStream_
     if (err != hipSuccess) return err;
     Token tok;
     tok.scale = reinterpret_cast<float *>(ws + l.tokens);
-    tok.lse2 = tok.scale + l.Mq;
-    tok.target = reinterpret_cast<int *>(tok.lse2 + l.Mq);
+    tok.lse = tok.scale + l.Mq;
+    tok.target = reinterpret_cast<int *>(tok.lse + l.Mq);
     uint32_t *const x_top = reinterpret_cast<uint32_t *>(ws + l.tops), *const w_top = x_top + l.nq;
-    token_kernel<<<(unsigned)(l.Mq / 256), 256, 0, s>>>(e, tok, p.M, l.Mq, r.idx, r.count, x_top, 2 * l.nq);
+    token_kernel<<<(unsigned)(l.Mq / 256), 256, 0, s>>>(e, tok, p.M, l.Mq, r.idx, r.count, f32 ? 1.f : kLog2e, x_top,
+                                                        f32 ? 0 : 2 * l.nq);
     err = hipGetLastError();
     const int np = (int)l.ops.np, n = (int)p.n;
     const auto top_grid = [&](int64_t rows) {
         const int64_t blocks = (rows + 63) / 64;
         return dim3((unsigned)(blocks < 1024 ? blocks : 1024), (unsigned)((n + 255) / 256));
     };
-    if (err == hipSuccess && p.dW) {
+    const int64_t plane_x = p.M * l.ops.np, plane_w = p.V * l.ops.np, plane_wt = p.n * l.Vp, plane_gt = l.vp * l.Mp;
+    if (err == hipSuccess && p.dW && !f32) {
         const int64_t blocks = (p.M * (np / 8) + 255) / 256;
         column_top_kernel<<<top_grid(p.M), 256, 0, s>>>(r.X, tok.scale, p.M, n, np, r.count, x_top);
         scale_kernel<<<(unsigned)(blocks < 16384 ? blocks : 16384), 256, 0, s>>>(r.X, tok.scale, x_top, at(l.xs), p.M, np,
@@ -698,11 +857,17 @@ hipError_t launch_loss_mfma_grad(const LossPass &p, const LossEpi &e, hipStream_
         err = hipGetLastError();
     }
     if (err == hipSuccess && p.dX) {
-        const uint16_t *W = static_cast<const uint16_t *>(p.W);
-        column_top_kernel<<<top_grid(p.V), 256, 0, s>>>(W, nullptr, p.V, n, n, nullptr, w_top);
-        transpose_kernel<<<dim3((unsigned)(l.Vp / 64), (unsigned)(np / 64)), 256, 0, s>>>(W, w_top, at(l.wt), p.V, n, l.Vp);
-        if (r.count)
-            zero_rows_kernel<<<(unsigned)(p.M < 8192 ? p.M : 8192), 256, 0, s>>>(e, static_cast<uint16_t *>(p.dX), p.M, n);
+        const dim3 grid((unsigned)(l.Vp / 64), (unsigned)(np / 64));
+        const unsigned rows = (unsigned)(p.M < 8192 ? p.M : 8192);
+        if (f32) {
+            transpose_split_kernel<<<grid, 256, 0, s>>>(static_cast<const float *>(p.W), at(l.wt), plane_wt, p.V, n, l.Vp);
+            if (r.count) zero_rows_kernel<<<rows, 256, 0, s>>>(e, static_cast<float *>(p.dX), p.M, n);
+        } else {
+            const uint16_t *W = static_cast<const uint16_t *>(p.W);
+            column_top_kernel<<<top_grid(p.V), 256, 0, s>>>(W, nullptr, p.V, n, n, nullptr, w_top);
+            transpose_kernel<<<grid, 256, 0, s>>>(W, w_top, at(l.wt), p.V, n, l.Vp);
+            if (r.count) zero_rows_kernel<<<rows, 256, 0, s>>>(e, static_cast<uint16_t *>(p.dX), p.M, n);
+        }
         err = hipGetLastError();
     }
     float *acc = reinterpret_cast<float *>(ws + l.acc);
@@ -715,26 +880,32 @@ hipError_t launch_loss_mfma_grad(const LossPass &p, const LossEpi &e, hipStream_
         g.v0 = v0;
         g.A = r.W + v0 * l.ops.np;
         g.B = r.X;
+        g.plane_a = plane_w;
+        g.plane_b = plane_x;
         g.lda = g.ldb = g.K = l.ops.np;
         g.I = vn;
         g.J = p.M;
         g.out = at(l.gt);
+        g.plane_out = plane_gt;
         g.ldo = l.Mp;
-        err = launch<false, kGrad>(g, choose(g.I, g.J), s);
+        err = launch<false, kGrad>(g, choose(g.I, g.J), f32, s);
         if (err == hipSuccess && p.dW) {
             g.A = at(l.gt);
+            g.plane_a = plane_gt;
             g.lda = g.K = l.Mp;
-            g.B = at(l.xs);
+            if (!f32) g.B = at(l.xs);
             g.rows_b = p.M;
             g.J = g.ldo = p.n;
             g.col_top = x_top;
-            g.out = static_cast<uint16_t *>(p.dW) + v0 * p.n;
-            err = launch<true, kDw>(g, choose(g.I, g.J), s);
+            g.out = static_cast<char *>(p.dW) + v0 * p.n * (f32 ? 4 : 2);
+            err = launch<true, kDw>(g, choose(g.I, g.J), f32, s);
         }
         if (err == hipSuccess && p.dX) {
             g.A = at(l.wt) + v0;
+            g.plane_a = plane_wt;
             g.lda = l.Vp;
             g.B = at(l.gt);
+            g.plane_b = plane_gt;
             g.ldb = g.ldo = l.Mp;
             g.I = p.n;
             g.J = p.M;
@@ -742,12 +913,17 @@ hipError_t launch_loss_mfma_grad(const LossPass &p, const LossEpi &e, hipStream_
             g.rows_b = vn;
             g.acc = acc;
             g.first = v0 == 0;
-            err = launch<true, kDx>(g, l.dx, s);
+            err = launch<true, kDx>(g, l.dx, f32, s);
         }
     }
     if (err == hipSuccess && p.dX) {
-        round_transpose_kernel<<<dim3((unsigned)(l.Mp / 64), (unsigned)(l.ops.np / 64)), 256, 0, s>>>(
-            acc, l.dx.splits, tok.scale, w_top, static_cast<uint16_t *>(p.dX), p.M, (int)p.n, l.Mp, r.idx, r.count);
+        const dim3 grid((unsigned)(l.Mp / 64), (unsigned)(np / 64));
+        if (f32)
+            round_transpose_kernel<<<grid, 256, 0, s>>>(acc, l.dx.splits, tok.scale, w_top, static_cast<float *>(p.dX), p.M, n,
+                                                        l.Mp, r.idx, r.count);
+        else
+            round_transpose_kernel<<<grid, 256, 0, s>>>(acc, l.dx.splits, tok.scale, w_top, static_cast<uint16_t *>(p.dX), p.M,
+                                                        n, l.Mp, r.idx, r.count);
         err = hipGetLastError();
     }
     return err;

@@ -101,6 +101,7 @@ def test_shapes(M, n, V, dtype):
 def test_many_tiles(dtype):
     check(*make(1500, 192, 5003, dtype))
     check(*make(700, 320, 9000, dtype, spread=8.0))
+    check(*make(4096, 64, 300, dtype))
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -152,8 +153,9 @@ def test_large_logits(dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-def test_nan_and_infinity_stay_in_their_tokens(dtype):
-    x, w, t = make(70, 64, 400, dtype, ignored=0.0)
+@pytest.mark.parametrize("M", [70, 200, 600])
+def test_nan_and_infinity_stay_in_their_tokens(dtype, M):
+    x, w, t = make(M, 64, 400, dtype, ignored=0.0)
     t[11] = -100
     clean, dx0, _ = check(x, w, t, "none")
     x[3, 5] = float("nan")
@@ -162,7 +164,7 @@ def test_nan_and_infinity_stay_in_their_tokens(dtype):
     a, b = x.cuda().requires_grad_(True), w.cuda()
     each = nn.linear_cross_entropy(a, b, t.cuda(), reduction="none")
     dx, = torch.autograd.grad(each, a, torch.ones_like(each))
-    ok = torch.ones(70, dtype=torch.bool, device="cuda")
+    ok = torch.ones(M, dtype=torch.bool, device="cuda")
     ok[[3, 4]] = False
     assert torch.equal(each[ok], clean[ok]) and torch.isnan(each[~ok]).all()
     assert torch.equal(dx[ok], dx0[ok]) and torch.isnan(dx[3]).all()
