@@ -45,7 +45,8 @@ def parse():
                     help="run just this call (e.g. IT:fc1.fwd) --steps times, for counter collection")
     ap.add_argument("--block", default="",
                     help="instead of the layer step: time an OPT-125m-shaped decoder block fwd+bwd "
-                         "(dense, Dyad FF only, Dyad everywhere) with this variant (IT/OT/DT)")
+                         "(dense, Dyad FF only, Dyad everywhere, the residual stream in AddNorm) with this "
+                         "variant (IT/OT/DT), and the loss over a vocabulary")
     ap.add_argument("--fused", action="store_true",
                     help="feed-forward block with GELU inside fc2's kernels (fc1 writes only its "
                          "pre-activation; dyad_forward_ex / dyad_backward_dw_ex)")
@@ -159,16 +160,18 @@ def build_calls(dy, lib, wl, fc1, fc2, variants, ws, ws_bytes, sp, fused=False):
 
 def block_bench(args):
     """OPT-125m-shaped pre-LN decoder block (d 768, 12 heads, ffn 3072, causal self-attention;
-    batch 8 x 2048 tokens) forward + backward on synthetic bf16 tokens, three ways: dense
+    batch 8 x 2048 tokens) forward + backward on synthetic bf16 tokens, four ways: dense
     nn.Linear everywhere, Dyad in the two FF layers only, Dyad in every linear layer (FF and
-    the q / k / v / out projections); plus the FF sub-block alone, dense vs Dyad.  Attention
+    the q / k / v / out projections), and that with the residual stream in nn.AddNorm; plus the FF
+    sub-block alone, dense vs Dyad, the residual stream alone (two joins and norms) and the
+    loss over a vocabulary of 50000, each through torch's operators and this library's.  Attention
     scores and softmax run in fp32 through plain matmuls (contiguous operands)."""
     import math
     import torch
     import torch.nn.functional as F
-    from paper_2312_06881_amd.nn import DyadFF, DyadLinear
+    from paper_2312_06881_amd.nn import AddNorm, DyadFF, DyadLinear, LinearCrossEntropy
 
-    d, ffn, heads, D, B, T = 768, 3072, 12, 4, 8, 2048
+    d, ffn, heads, D, B, T, V = 768, 3072, 12, 4, 8, 2048, 50000
     hd = d // heads
     v = args.block
     dev = torch.device("cuda:0")
@@ -196,18 +199,63 @@ def block_bench(args):
             self.q, self.k, self.v, self.o = (lin(d, d, attn_dyad) for _ in range(4))
             self.ff = DyadFF(d, ffn, D, v, device=dev) if ff_dyad else DenseFF()
 
-        def forward(self, x):
-            h = self.ln1(x)
+        def attention(self, h):
             q, k, w = (t.reshape(B, T, heads, hd).transpose(1, 2).float() for t in (self.q(h), self.k(h), self.v(h)))
             s = torch.matmul(q.contiguous(), k.transpose(-1, -2).contiguous()) / math.sqrt(hd) + mask
             a = torch.matmul(torch.softmax(s, dim=-1), w.contiguous())
-            x = x + self.o(a.transpose(1, 2).reshape(B, T, d).to(bf).contiguous())
+            return self.o(a.transpose(1, 2).reshape(B, T, d).to(bf).contiguous())
+
+        def forward(self, x):
+            x = x + self.attention(self.ln1(x))
             return x + self.ff(self.ln2(x))
+
+    class FusedBlock(Block):
+        """The same with the stream in AddNorm: each join also norms for what comes next."""
+
+        def __init__(self):
+            super().__init__(True, True)
+            self.ln1, self.ln2 = AddNorm(d, device=dev), AddNorm(d, device=dev)
+            self.last = AddNorm(d, norm=None, device=dev)
+
+        def forward(self, x):
+            x, h = self.ln1(x)
+            x, h = self.ln2(x, self.attention(h))
+            return self.last(x, self.ff(h))[0]
+
+    class Stream(torch.nn.Module):
+        """What stands between the layers: two joins with the stream, each normed."""
+
+        def __init__(self, fused):
+            super().__init__()
+            self.fused = fused
+            self.norms = torch.nn.ModuleList(AddNorm(d, device=dev) if fused else torch.nn.LayerNorm(d, device=dev, dtype=bf)
+                                             for _ in range(2))
+
+        def forward(self, x):
+            a = x
+            for norm in self.norms:
+                if self.fused:
+                    x, a = norm(x, a)
+                else:
+                    x = x + a
+                    a = norm(x)
+            return x + a
+
+    class Loss(torch.nn.Module):
+        def __init__(self, fused):
+            super().__init__()
+            self.head = LinearCrossEntropy(d, V, device=dev)
+            self.fused, self.t = fused, torch.randint(0, V, (B, T), device=dev)
+
+        def forward(self, x):
+            if self.fused:
+                return self.head(x, self.t)
+            return F.cross_entropy((x.reshape(-1, d) @ self.head.weight.t()).float(), self.t.view(-1))
 
     x = torch.randn((B, T, d), device=dev, dtype=bf)
     g = torch.randn((B, T, d), device=dev, dtype=bf)
 
-    def timed(mod, inp):
+    def timed(mod, inp, g=g):
         xi = inp.detach().requires_grad_(True)
         for _ in range(args.warmup):
             mod(xi).backward(g)
@@ -221,17 +269,20 @@ def block_bench(args):
         return round(e0.elapsed_time(e1) / args.steps, 4)
 
     res = {"dense": timed(Block(False, False), x), "dyad_ff": timed(Block(False, True), x),
-           "dyad_all": timed(Block(True, True), x),
-           "ff_dense": timed(DenseFF(), x), "ff_dyad": timed(DyadFF(d, ffn, D, v, device=dev), x)}
+           "dyad_all": timed(Block(True, True), x), "dyad_all_add_norm": timed(FusedBlock(), x),
+           "ff_dense": timed(DenseFF(), x), "ff_dyad": timed(DyadFF(d, ffn, D, v, device=dev), x),
+           "stream_torch": timed(Stream(False), x), "stream_add_norm": timed(Stream(True), x),
+           "loss_torch": timed(Loss(False), x, None), "loss_linear_cross_entropy": timed(Loss(True), x, None)}
     print(json.dumps({
         "metric": "decoder block forward+backward ms (OPT-125m shape)", "unit": "ms",
         "higher_is_better": False, "n_gpus": 1, "steps": args.steps, "warmup": args.warmup,
         "dtype": "bf16", "data": "synthetic",
         "config": {"workload": "opt125m_decoder_block", "d": d, "ffn": ffn, "heads": heads, "n_dyad": D,
-                   "variant": v, "batch": B, "seq_len": T},
+                   "variant": v, "batch": B, "seq_len": T, "vocab": V},
         "ms": res,
         "speedup_vs_dense": {"block_dyad_ff": round(res["dense"] / res["dyad_ff"], 3),
                              "block_dyad_all": round(res["dense"] / res["dyad_all"], 3),
+                             "block_dyad_all_add_norm": round(res["dense"] / res["dyad_all_add_norm"], 3),
                              "ff_only": round(res["ff_dense"] / res["ff_dyad"], 3)},
     }))
 

@@ -298,7 +298,7 @@ int dyad_backward_dw_mx8(dyad_variant variant, int64_t n_in, int64_t n_out, int6
  * draws another mask at every replay if the program changes it in between.
  */
 
-/* Y = X dropped and scaled; the gradient is the same call on dY.  Y may be X. */
+/* Y = X dropped and scaled; the gradient is the same call on dY.  Y may be X.  cols <= 2^31 - 16. */
 int dyad_dropout(int64_t rows, int64_t cols, dyad_dtype dtype, const void *X, double p, uint64_t seed, uint64_t offset,
                  const uint64_t *offset_dev, void *Y, hipStream_t stream);
 
@@ -362,7 +362,8 @@ int dyad_add_norm_backward(const dyad_add_norm_args *args, const dyad_add_norm_g
  * Z[m][target]; a target that is ignore_index, or lies outside 0 .. V - 1, counts for
  * nothing: loss 0, no gradient.  reduction NONE: loss [M]; SUM, MEAN over the tokens
  * that count (0 where none does): loss [1].  lse [M] and, for MEAN, count [1] (the
- * tokens that count) are what the backward pass needs of the forward one.
+ * tokens that count) are what the backward pass needs of the forward one; lse of a
+ * token that does not count has no meaning.
  *
  * Backward: dloss, of loss's length, is the gradient that reaches it; dX [M][n] and
  * dW [V][n], either of which may be NULL, are the gradients.  The logits are formed

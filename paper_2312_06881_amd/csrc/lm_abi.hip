@@ -72,7 +72,8 @@ int dyad_dropout(int64_t rows, int64_t cols, dyad_dtype dtype_arg, const void *X
                  uint64_t offset, const uint64_t *offset_dev, void *Y, hipStream_t stream) {
     const int dtype = enum_value(dtype_arg);
     if (!known_dtype(dtype)) return DYAD_ERR_DTYPE;
-    if (!small(rows, cols) || !probability(p) || (rows > 0 && (!X || !Y))) return DYAD_ERR_INVALID_ARG;
+    // a row's columns are counted in 32 bits, eight at a time
+    if (!small(rows, cols) || cols > kMaxDim - 16 || !probability(p) || (rows > 0 && (!X || !Y))) return DYAD_ERR_INVALID_ARG;
     if (!aligned16(X) || !aligned16(Y) || !aligned8(offset_dev)) return DYAD_ERR_ALIGN;
     if (rows == 0) return DYAD_OK;
     return launch_status(dyad::launch_dropout(rows, cols, dtype, X, dyad::drop_args(p, seed, offset, offset_dev), Y, stream));

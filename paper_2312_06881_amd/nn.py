@@ -426,6 +426,14 @@ def _saved_offset(offset):
     return (offset, None) if isinstance(offset, torch.Tensor) else (None, offset)
 
 
+def _ready(t):
+    """t contiguous and where the library takes it: gradients of slices and stacked scalars need not be."""
+    if t is None:
+        return None
+    t = t if t.is_contiguous() else t.contiguous()
+    return t.clone() if t.data_ptr() % 16 else t
+
+
 class _DropoutFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, p, seed, offset):
@@ -438,7 +446,7 @@ class _DropoutFn(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dy):
         kept, = ctx.saved_tensors
-        return lm.dropout(dy.contiguous(), ctx.p, ctx.seed, ctx.offset if kept is None else kept), None, None, None
+        return lm.dropout(_ready(dy), ctx.p, ctx.seed, ctx.offset if kept is None else kept), None, None, None
 
 
 def dropout(x, p, seed, offset=0, training=True):
@@ -448,7 +456,7 @@ def dropout(x, p, seed, offset=0, training=True):
     passes it must not change."""
     if not training:
         return x
-    x = x.contiguous()
+    x = _ready(x)
     if _plain(x):
         return lm.dropout(x, p, seed, offset)
     return _DropoutFn.apply(x, p, seed, offset)
@@ -478,10 +486,7 @@ class _AddNormFn(torch.autograd.Function):
             return (None,) * 8
         kept, y, weight, bias, post_weight, post_bias, gate, stats, post_stats, dev = ctx.saved_tensors
         call = ctx.call
-        if dh is not None and not dh.is_contiguous():
-            dh = dh.contiguous()
-        if dout is not None and not dout.is_contiguous():
-            dout = dout.contiguous()
+        dh, dout = _ready(dh), _ready(dout)
         x, h = (kept, None) if ctx.again else (None, kept)
         if y is None and call.has_y:
             y = kept
@@ -497,7 +502,7 @@ def add_norm(x, y=None, norm="layer", weight=None, bias=None, *, post_norm=None,
     shape = x.shape
     if y is not None and y.shape != shape:
         raise ValueError(f"x and y have one shape, got {tuple(shape)} and {tuple(y.shape)}")
-    xt, yt = _tokens(x), None if y is None else _tokens(y)
+    xt, yt = _ready(_tokens(x)), None if y is None else _ready(_tokens(y))
     call = lm._AddNorm(xt, yt, norm, weight, bias, post_norm, post_weight, post_bias, gate, x_scale, y_scale, eps, p, seed,
                        offset, dtype)
     if _plain(x, y, weight, bias, post_weight, post_bias, gate):
@@ -523,7 +528,7 @@ class _LinearCrossEntropyFn(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dloss):
         x, weight, targets, lse, count = ctx.saved_tensors
-        dx, dw = lm.linear_cross_entropy_backward(dloss.contiguous(), x, weight, targets, lse, count, ctx.ignore_index,
+        dx, dw = lm.linear_cross_entropy_backward(_ready(dloss), x, weight, targets, lse, count, ctx.ignore_index,
                                                   ctx.reduction, *ctx.needs_input_grad[:2])
         return dx, dw, None, None, None
 
@@ -534,7 +539,7 @@ def linear_cross_entropy(x, weight, targets, ignore_index=-100, reduction="mean"
     passes, and never kept.  See ``lm.linear_cross_entropy``."""
     if targets.shape != x.shape[:-1]:
         raise ValueError(f"targets have shape {tuple(x.shape[:-1])}, got {tuple(targets.shape)}")
-    xt, t = _tokens(x), targets.reshape(-1).contiguous()
+    xt, t = _ready(_tokens(x)), _ready(targets.reshape(-1))
     if _plain(x, weight):
         loss = lm.linear_cross_entropy(xt, weight, t, ignore_index, reduction)
     else:

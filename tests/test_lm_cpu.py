@@ -120,7 +120,7 @@ def test_add_norm_workspace():
 @pytest.mark.parametrize("kw,code", [
     (dict(dtype=5), -4), (dict(rows=-1), -1), (dict(cols=0), -1), (dict(p=-0.5), -1), (dict(p=float("nan")), -1),
     (dict(p=1.01), -1), (dict(x=None), -1), (dict(y=None), -1), (dict(x=FAKE + 2), -3), (dict(off=FAKE + 4), -3),
-    (dict(rows=2 ** 31), -1), (dict(rows=2 ** 30, cols=2 ** 12), -1), (dict(rows=0, x=None, y=None), 0)])
+    (dict(rows=2 ** 31), -1), (dict(cols=2 ** 31 - 8, rows=1), -1), (dict(rows=2 ** 30, cols=2 ** 12), -1), (dict(rows=0, x=None, y=None), 0)])
 def test_dropout_refuses(kw, code):
     v = dict(rows=4, cols=8, dtype=dy.BF16, x=FAKE, p=0.5, off=None, y=FAKE)
     v.update(kw)
