@@ -45,8 +45,8 @@ constexpr int teams_of(int tpr) { return threads_of(tpr) / tpr; }
 
 template <bool RAG>
 __device__ __forceinline__ void load_param(const void *base, bool f32, int64_t row, int c, int n, float (&v)[8]) {
-    if (f32) load_cols<RAG>(static_cast<const float *>(base) + row * n, c, n, v);
-    else load_cols<RAG>(static_cast<const uint16_t *>(base) + row * n, c, n, v);
+    if (f32) load_row<RAG>(static_cast<const float *>(base) + row * n, c, n, v);
+    else load_row<RAG>(static_cast<const uint16_t *>(base) + row * n, c, n, v);
 }
 
 // Sums of a and b over a team, the same bits in each of its threads.
@@ -114,11 +114,11 @@ __global__ void __launch_bounds__(threads_of(TPR)) add_norm_kernel(Norm a) {
         const TS *xr = static_cast<const TS *>(a.p.x) + row * n;
         float x[NV][8];
 #pragma unroll
-        for (int q = 0; q < NV; ++q) load_cols<RAG>(xr, c0 + q * 8 * TPR, n, x[q]);
+        for (int q = 0; q < NV; ++q) load_row<RAG>(xr, c0 + q * 8 * TPR, n, x[q]);
         if (a.p.y) {
             const TB *yr = static_cast<const TB *>(a.p.y) + row * n;
 #pragma unroll
-            for (int q = 0; q < NV; ++q) load_cols<RAG>(yr, c0 + q * 8 * TPR, n, h[q]);
+            for (int q = 0; q < NV; ++q) load_row<RAG>(yr, c0 + q * 8 * TPR, n, h[q]);
             if (a.p.post != kNormNone) {
                 const float2 st = row_stats<TPR, NV>(h, a.p.post, a, c0, sum);
                 if (a.p.post_stats && lane == 0) reinterpret_cast<float2 *>(a.p.post_stats)[row] = st;
@@ -286,6 +286,27 @@ __global__ void __launch_bounds__(threads_of(TPR)) add_norm_grad_kernel(Norm a) 
         if (FULL && a.p.post != kNormNone) r.ps = reinterpret_cast<const float2 *>(a.p.post_stats)[row];
         return r;
     };
+    // the parameters stay in registers: loads return in order, so one in the loop would wait for
+    // the next row's (8192 rows of 4096, post norm and gate: 163 us with such loads, 143 without)
+    float w[NV][8], gate[NV][8], pw[FULL ? NV : 1][8], pb[FULL ? NV : 1][8];
+    const auto param = [&](const void *base, int64_t row, float missing, int q, float (&v)[8]) __attribute__((always_inline)) {
+        if (base) {
+            load_param<RAG>(base, pf32, row, c0 + q * 8 * TPR, n, v);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = missing;
+        }
+    };
+#pragma unroll
+    for (int q = 0; q < NV; ++q) {
+        param(a.p.w, 0, 1.f, q, w[q]);
+        if constexpr (FULL) {
+            param(a.p.pw, 0, 1.f, q, pw[q]);
+            param(a.p.pb, 0, 0.f, q, pb[q]);
+        }
+        param(a.p.gate, 0, 1.f, q, gate[q]);
+    }
+    int64_t gate_row = 0;
     float dw[NV][8] = {}, db[NV][8] = {};
     float dpw[FULL ? NV : 1][8] = {}, dpb[FULL ? NV : 1][8] = {}, dgate[FULL ? NV : 1][8] = {};
     const int64_t u1 = (int64_t)(blockIdx.x + 1) * a.units / gridDim.x;
@@ -301,7 +322,11 @@ __global__ void __launch_bounds__(threads_of(TPR)) add_norm_grad_kernel(Norm a) 
             next = fetch(row + teams_of(TPR) < last ? row + teams_of(TPR) : row);
             float g[NV][8], u[NV][8];
             uint32_t keep[NV];
-            const int64_t grow = a.p.gate && a.p.groups > 1 ? row / a.rows_per_gate : 0;
+            if (a.p.groups > 1 && row / a.rows_per_gate != gate_row) {
+                gate_row = row / a.rows_per_gate;
+#pragma unroll
+                for (int q = 0; q < NV; ++q) param(a.p.gate, gate_row, 1.f, q, gate[q]);
+            }
             if (a.drop) {
 #pragma unroll
                 for (int q = 0; q < NV; ++q) {
@@ -320,20 +345,10 @@ __global__ void __launch_bounds__(threads_of(TPR)) add_norm_grad_kernel(Norm a) 
                 }
             };
             const auto post_y = [&](int q, float (&z)[8]) __attribute__((always_inline)) {
-                const int c = c0 + q * 8 * TPR;
                 unit_y(q, z);
                 if constexpr (FULL) {
-                    float t[8];
-                    if (a.p.pw) {
-                        load_param<RAG>(a.p.pw, pf32, 0, c, n, t);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) z[e] *= t[e];
-                    }
-                    if (a.p.pb) {
-                        load_param<RAG>(a.p.pb, pf32, 0, c, n, t);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) z[e] += t[e];
-                    }
+                    for (int e = 0; e < 8; ++e) z[e] = fmaf(z[e], pw[q][e], pb[q][e]);
                 }
             };
             if (a.p.dout) {
@@ -347,21 +362,15 @@ __global__ void __launch_bounds__(threads_of(TPR)) add_norm_grad_kernel(Norm a) 
                 const float2 st = cur.st;
 #pragma unroll
                 for (int q = 0; q < NV; ++q) {
-                    const int c = c0 + q * 8 * TPR;
                     if (again) {
 #pragma unroll
                         for (int e = 0; e < 8; ++e) u[q][e] *= a.p.x_scale;
                         if (a.p.y) {
-                            float z[8], t[8];
+                            float z[8];
                             post_y(q, z);
                             if (a.drop) apply_drop(z, keep[q], a.d.scale);
-                            if (a.p.gate) {
-                                load_param<RAG>(a.p.gate, pf32, grow, c, n, t);
 #pragma unroll
-                                for (int e = 0; e < 8; ++e) z[e] *= t[e];
-                            }
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) u[q][e] = fmaf(z[e], a.p.y_scale, u[q][e]);
+                            for (int e = 0; e < 8; ++e) u[q][e] = fmaf(z[e] * gate[q][e], a.p.y_scale, u[q][e]);
                         }
                     }
 #pragma unroll
@@ -370,12 +379,8 @@ __global__ void __launch_bounds__(threads_of(TPR)) add_norm_grad_kernel(Norm a) 
                         db[q][e] += g[q][e];
                         dw[q][e] = fmaf(g[q][e], u[q][e], dw[q][e]);
                     }
-                    if (a.p.w) {
-                        float w[8];
-                        load_param<RAG>(a.p.w, pf32, 0, c, n, w);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) g[q][e] *= w[e];
-                    }
+                    for (int e = 0; e < 8; ++e) g[q][e] *= w[q][e];
                 }
                 norm_grad<TPR, NV>(g, u, st.y, a.p.norm, n, sum);
                 if (a.p.dh) {
@@ -417,12 +422,8 @@ __global__ void __launch_bounds__(threads_of(TPR)) add_norm_grad_kernel(Norm a) 
                         for (int e = 0; e < 8; ++e) dgate[q][e] += g[q][e] != 0.f ? g[q][e] * z[e] : 0.f;
                     }
                 }
-                if (a.p.gate) {
-                    float t[8];
-                    load_param<RAG>(a.p.gate, pf32, grow, c, n, t);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) g[q][e] *= t[e];
-                }
+                for (int e = 0; e < 8; ++e) g[q][e] *= gate[q][e];
                 if constexpr (FULL) {
                     if (a.p.post != kNormNone) {
                         unit_y(q, u[q]);           // the stream's u has had its turn
@@ -431,12 +432,8 @@ __global__ void __launch_bounds__(threads_of(TPR)) add_norm_grad_kernel(Norm a) 
                             dpb[q][e] += g[q][e];
                             dpw[q][e] = fmaf(g[q][e], u[q][e], dpw[q][e]);
                         }
-                        if (a.p.pw) {
-                            float t[8];
-                            load_param<RAG>(a.p.pw, pf32, 0, c, n, t);
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) g[q][e] *= t[e];
-                        }
+                        for (int e = 0; e < 8; ++e) g[q][e] *= pw[q][e];
                     }
                 }
             }
@@ -515,7 +512,8 @@ Plan plan_of(const AddNormPass &p) {
     const Shape sh = shape_of(p.n, true);
     const int64_t teams = teams_of(sh.tpr);
     // two rows a team at least, and no more workgroups than the GPU holds at once: 3 waves a
-    // SIMD, or 2 with the sums of a post norm (rows loaded ahead, so more would not help)
+    // SIMD, or 2 with the sums of a post norm (rows loaded ahead, so more would not help; with
+    // eight rows a team 3997 rows of 1001 took 93 us in place of 60)
     const int64_t most = 1024 * (l.full ? 2 : 3) / (threads_of(sh.tpr) / 64);
     int64_t want = (p.M + 2 * teams - 1) / (2 * teams);
     if (want > most) want = most;
