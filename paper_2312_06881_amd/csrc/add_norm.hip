@@ -287,8 +287,12 @@ __global__ void __launch_bounds__(threads_of(TPR)) add_norm_grad_kernel(Norm a) 
         return r;
     };
     // the parameters stay in registers: loads return in order, so one in the loop would wait for
-    // the next row's (8192 rows of 4096, post norm and gate: 163 us with such loads, 143 without)
-    float w[NV][8], gate[NV][8], pw[FULL ? NV : 1][8], pb[FULL ? NV : 1][8];
+    // the next row's (8192 rows of 4096, post norm and gate: 163 us with such loads, 143 without).
+    // Sixteen waves have 128 registers each and cannot: with a post norm they load rows and
+    // parameters as they come to them and keep four of the sums in LDS, where each thread adds to
+    // words of its own (4096 rows of 8192, fp32 stream, post norm and gate: 165 us, 3.7 TB/s).
+    constexpr bool kKeep = TPR < 1024, kAhead = TPR < 1024 || !FULL, kLdsSums = TPR == 1024 && FULL && NV == 1;
+    __shared__ f32x4_t lsum[kLdsSums ? 8 * TPR : 1];
     const auto param = [&](const void *base, int64_t row, float missing, int q, float (&v)[8]) __attribute__((always_inline)) {
         if (base) {
             load_param<RAG>(base, pf32, row, c0 + q * 8 * TPR, n, v);
@@ -297,15 +301,49 @@ __global__ void __launch_bounds__(threads_of(TPR)) add_norm_grad_kernel(Norm a) 
             for (int e = 0; e < 8; ++e) v[e] = missing;
         }
     };
+    float w[kKeep ? NV : 1][8], gate[kKeep ? NV : 1][8], pw[kKeep && FULL ? NV : 1][8], pb[kKeep && FULL ? NV : 1][8];
+    if constexpr (kKeep) {
 #pragma unroll
-    for (int q = 0; q < NV; ++q) {
-        param(a.p.w, 0, 1.f, q, w[q]);
-        if constexpr (FULL) {
-            param(a.p.pw, 0, 1.f, q, pw[q]);
-            param(a.p.pb, 0, 0.f, q, pb[q]);
+        for (int q = 0; q < NV; ++q) {
+            param(a.p.w, 0, 1.f, q, w[q]);
+            if constexpr (FULL) {
+                param(a.p.pw, 0, 1.f, q, pw[q]);
+                param(a.p.pb, 0, 0.f, q, pb[q]);
+            }
+            param(a.p.gate, 0, 1.f, q, gate[q]);
         }
-        param(a.p.gate, 0, 1.f, q, gate[q]);
     }
+    // v times a parameter's eight columns (kept ones in t)
+    const auto times = [&](float (&v)[8], const void *base, int64_t row, int q, const auto &kept) __attribute__((always_inline)) {
+        float t[8];
+        if constexpr (kKeep) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) t[e] = kept[q][e];
+        } else {
+            param(base, row, 1.f, q, t);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= t[e];
+    };
+    if constexpr (kLdsSums) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) lsum[k * TPR + lane] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    // sum k (0 dw, 1 db, 2 dpw, 3 dpb) of eight columns
+    const auto add = [&](int k, float (&acc)[8], const float (&v)[8]) __attribute__((always_inline)) {
+        if constexpr (kLdsSums) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                f32x4_t t = lsum[(2 * k + h) * TPR + lane];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) t[e] += v[4 * h + e];
+                lsum[(2 * k + h) * TPR + lane] = t;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[e] += v[e];
+        }
+    };
     int64_t gate_row = 0;
     float dw[NV][8] = {}, db[NV][8] = {};
     float dpw[FULL ? NV : 1][8] = {}, dpb[FULL ? NV : 1][8] = {}, dgate[FULL ? NV : 1][8] = {};
@@ -319,13 +357,14 @@ __global__ void __launch_bounds__(threads_of(TPR)) add_norm_grad_kernel(Norm a) 
         if (first + team < last) next = fetch(first + team);
         for (int64_t row = first + team; row < last; row += teams_of(TPR)) {
             const Row<TS, TB, NV> cur = next;
-            next = fetch(row + teams_of(TPR) < last ? row + teams_of(TPR) : row);
+            if constexpr (kAhead) next = fetch(row + teams_of(TPR) < last ? row + teams_of(TPR) : row);
             float g[NV][8], u[NV][8];
             uint32_t keep[NV];
             if (a.p.groups > 1 && row / a.rows_per_gate != gate_row) {
                 gate_row = row / a.rows_per_gate;
+                if constexpr (kKeep)
 #pragma unroll
-                for (int q = 0; q < NV; ++q) param(a.p.gate, gate_row, 1.f, q, gate[q]);
+                    for (int q = 0; q < NV; ++q) param(a.p.gate, gate_row, 1.f, q, gate[q]);
             }
             if (a.drop) {
 #pragma unroll
@@ -348,7 +387,16 @@ __global__ void __launch_bounds__(threads_of(TPR)) add_norm_grad_kernel(Norm a) 
                 unit_y(q, z);
                 if constexpr (FULL) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) z[e] = fmaf(z[e], pw[q][e], pb[q][e]);
+                    for (int e = 0; e < 8; ++e) {
+                        if constexpr (kKeep) z[e] = fmaf(z[e], pw[q][e], pb[q][e]);
+                    }
+                    if constexpr (!kKeep) {
+                        float s[8], t[8];
+                        param(a.p.pw, 0, 1.f, q, s);
+                        param(a.p.pb, 0, 0.f, q, t);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) z[e] = fmaf(z[e], s[e], t[e]);
+                    }
                 }
             };
             if (a.p.dout) {
@@ -369,18 +417,19 @@ __global__ void __launch_bounds__(threads_of(TPR)) add_norm_grad_kernel(Norm a) 
                             float z[8];
                             post_y(q, z);
                             if (a.drop) apply_drop(z, keep[q], a.d.scale);
+                            times(z, a.p.gate, gate_row, q, gate);
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) u[q][e] = fmaf(z[e] * gate[q][e], a.p.y_scale, u[q][e]);
+                            for (int e = 0; e < 8; ++e) u[q][e] = fmaf(z[e], a.p.y_scale, u[q][e]);
                         }
                     }
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        u[q][e] = (u[q][e] - st.x) * st.y;
-                        db[q][e] += g[q][e];
-                        dw[q][e] = fmaf(g[q][e], u[q][e], dw[q][e]);
-                    }
+                    for (int e = 0; e < 8; ++e) u[q][e] = (u[q][e] - st.x) * st.y;
+                    float t[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) g[q][e] *= w[q][e];
+                    for (int e = 0; e < 8; ++e) t[e] = g[q][e] * u[q][e];
+                    add(0, dw[kLdsSums ? 0 : q], t);
+                    add(1, db[kLdsSums ? 0 : q], g[q]);
+                    times(g[q], a.p.w, 0, q, w);
                 }
                 norm_grad<TPR, NV>(g, u, st.y, a.p.norm, n, sum);
                 if (a.p.dh) {
@@ -406,7 +455,7 @@ __global__ void __launch_bounds__(threads_of(TPR)) add_norm_grad_kernel(Norm a) 
                     store_cols<RAG>(dx, c0 + q * 8 * TPR, n, t);
                 }
             }
-            if (!FULL && !a.p.dy) continue;
+            if (!FULL && !a.p.dy) continue;   // (only rows loaded ahead)
 #pragma unroll
             for (int q = 0; q < NV; ++q) {
                 const int c = c0 + q * 8 * TPR;
@@ -422,18 +471,16 @@ __global__ void __launch_bounds__(threads_of(TPR)) add_norm_grad_kernel(Norm a) 
                         for (int e = 0; e < 8; ++e) dgate[q][e] += g[q][e] != 0.f ? g[q][e] * z[e] : 0.f;
                     }
                 }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) g[q][e] *= gate[q][e];
+                times(g[q], a.p.gate, gate_row, q, gate);
                 if constexpr (FULL) {
                     if (a.p.post != kNormNone) {
                         unit_y(q, u[q]);           // the stream's u has had its turn
+                        float t[8];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            dpb[q][e] += g[q][e];
-                            dpw[q][e] = fmaf(g[q][e], u[q][e], dpw[q][e]);
-                        }
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) g[q][e] *= pw[q][e];
+                        for (int e = 0; e < 8; ++e) t[e] = g[q][e] * u[q][e];
+                        add(2, dpw[kLdsSums ? 0 : q], t);
+                        add(3, dpb[kLdsSums ? 0 : q], g[q]);
+                        times(g[q], a.p.pw, 0, q, pw);
                     }
                 }
             }
@@ -443,9 +490,21 @@ __global__ void __launch_bounds__(threads_of(TPR)) add_norm_grad_kernel(Norm a) 
 #pragma unroll
                 for (int q = 0; q < NV; ++q) store_cols<RAG>(dy, c0 + q * 8 * TPR, n, g[q]);
             }
+            if constexpr (!kAhead)
+                if (row + teams_of(TPR) < last) next = fetch(row + teams_of(TPR));
         }
         if constexpr (FULL)
             if (a.gpart) flush<TPR, NV>(dgate, a.gpart + unit * a.npad, a.npad, buf);
+    }
+    if constexpr (kLdsSums) {
+        const auto back = [&](int k, float (&acc)[8]) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[e] = lsum[(2 * k + e / 4) * TPR + lane][e % 4];
+        };
+        back(0, dw[0]);
+        back(1, db[0]);
+        back(2, dpw[0]);
+        back(3, dpb[0]);
     }
     if (a.part[0]) flush<TPR, NV>(dw, a.part[0] + (int64_t)blockIdx.x * a.npad, a.npad, buf);
     if (a.part[1]) flush<TPR, NV>(db, a.part[1] + (int64_t)blockIdx.x * a.npad, a.npad, buf);
@@ -514,7 +573,8 @@ Plan plan_of(const AddNormPass &p) {
     // two rows a team at least, and no more workgroups than the GPU holds at once: 3 waves a
     // SIMD, or 2 with the sums of a post norm (rows loaded ahead, so more would not help; with
     // eight rows a team 3997 rows of 1001 took 93 us in place of 60)
-    const int64_t most = 1024 * (l.full ? 2 : 3) / (threads_of(sh.tpr) / 64);
+    int64_t most = 1024 * (l.full ? 2 : 3) / (threads_of(sh.tpr) / 64);
+    if (most < 256) most = 256;
     int64_t want = (p.M + 2 * teams - 1) / (2 * teams);
     if (want > most) want = most;
     if (want < 1) want = 1;
