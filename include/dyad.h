@@ -371,7 +371,7 @@ int dyad_add_norm_backward(const dyad_add_norm_args *args, const dyad_add_norm_g
  * X times dloss, enter the products with W and X in fp16 (at powers of two that meet
  * its range); the sums are fp32.
  *
- * M, V <= 2^22 and n <= 2^20, else DYAD_ERR_SHAPE.  The workspace holds
+ * M, V <= 2^22, M V <= 2^38 and n <= 2^20, else DYAD_ERR_SHAPE.  The workspace holds
  * dyad_linear_ce_workspace_bytes() bytes for the pass (0 for invalid arguments).
  */
 typedef enum { DYAD_REDUCE_NONE = 0, DYAD_REDUCE_SUM = 1, DYAD_REDUCE_MEAN = 2 } dyad_reduction;

@@ -60,7 +60,8 @@ int norm_pass(const dyad_add_norm_args *a, const dyad_add_norm_grads *g, dyad::A
 int loss_sizes(int64_t M, int64_t n, int64_t V, int dtype) {
     if (!known_dtype(dtype)) return DYAD_ERR_DTYPE;
     if (!small(M, n) || !small(V, n) || V <= 0) return DYAD_ERR_INVALID_ARG;
-    if (M > dyad::kLossMaxRows || V > dyad::kLossMaxRows || n > dyad::kLossMaxWidth) return DYAD_ERR_SHAPE;
+    if (M > dyad::kLossMaxRows || V > dyad::kLossMaxRows || n > dyad::kLossMaxWidth || M * V > dyad::kLossMaxLogits)
+        return DYAD_ERR_SHAPE;
     return DYAD_OK;
 }
 

@@ -40,6 +40,7 @@ constexpr int kReduceNone = 0, kReduceSum = 1, kReduceMean = 2;
 // Tokens and vocabulary of a call: offsets within a tile's operand rows are 32-bit.
 constexpr int64_t kLossMaxRows = (int64_t)1 << 22;
 constexpr int64_t kLossMaxWidth = (int64_t)1 << 20;
+constexpr int64_t kLossMaxLogits = (int64_t)1 << 38;   // a launch has fewer than 2^32 threads, 512 to 2^16 logits
 
 struct LossPass {
     int64_t M, n, V;

@@ -133,7 +133,7 @@ CE = dict(M=4, n=8, V=100, dtype=dy.F32, X=FAKE, W=FAKE, t=FAKE, red=dy.REDUCE_M
 
 @pytest.mark.parametrize("kw,code", [
     (dict(dtype=3), -4), (dict(M=-1), -1), (dict(n=0), -1), (dict(V=0), -1), (dict(M=2 ** 22 + 1), -2),
-    (dict(V=2 ** 22 + 1), -2), (dict(n=2 ** 20 + 1), -2), (dict(red=3), -1), (dict(X=None), -1), (dict(W=None), -1),
+    (dict(V=2 ** 22 + 1), -2), (dict(M=2 ** 20, V=2 ** 18 + 1), -2), (dict(n=2 ** 20 + 1), -2), (dict(red=3), -1), (dict(X=None), -1), (dict(W=None), -1),
     (dict(t=None), -1), (dict(lse=None), -1), (dict(loss=None), -1), (dict(count=None), -1), (dict(X=FAKE + 8), -3),
     (dict(t=FAKE + 8), -3), (dict(ws=None), -5), (dict(size=8), -5), (dict(ws=FAKE + 4), -3)])
 def test_linear_ce_refuses(kw, code):
