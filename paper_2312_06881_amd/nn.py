@@ -548,30 +548,30 @@ def linear_cross_entropy(x, weight, targets, ignore_index=-100, reduction="mean"
 
 
 class Dropout(torch.nn.Module):
-    """Dropout whose mask is drawn from a counter and never stored.  Every call in training takes the next
-    offset.  seed: by default one drawn from torch's CPU generator; layers that share one drop the same places.
-    capturable: the counter lives on the device (with the module), so that every replay of a captured call
-    draws another mask."""
+    """Dropout whose mask is drawn from a counter and never stored.  Every call in training draws its offset (kept in
+    ``offset``) from torch's CPU generator, so torch.manual_seed makes runs repeat, and activation checkpointing, which
+    restores that generator, draws the same mask when it runs the layer again.  seed: by default drawn there too; layers
+    that share one still differ by their offsets.  capturable: the offset counts calls on the device (``calls``, with the
+    module), so that every replay of a captured call draws another mask; not for layers that checkpointing runs
+    again."""
 
     def __init__(self, p=0.1, seed=None, capturable=False, device=None):
         super().__init__()
         if not 0.0 <= p <= 1.0:
             raise ValueError(f"p is a probability, got {p}")
-        self.p, self.capturable = p, capturable
+        self.p, self.capturable, self.offset = p, capturable, None
         self.seed = int(torch.randint(2 ** 62, ()).item()) if seed is None else seed
-        self.calls = 0
         if capturable:
-            del self.calls
             self.register_buffer("calls", torch.zeros((1,), dtype=torch.int64, device=device))
 
     def next_offset(self):
-        """The offset of the call that asks, and one more from here on."""
-        if not self.capturable:
+        """The offset of the call that asks."""
+        if self.capturable:
+            now = self.calls.clone()     # the backward pass draws this call's mask again
             self.calls += 1
-            return self.calls - 1
-        now = self.calls.clone()     # the backward pass draws this call's mask again
-        self.calls += 1
-        return now
+            return now
+        self.offset = int(torch.randint(2 ** 62, ()).item())
+        return self.offset
 
     def forward(self, x):
         if not self.training or self.p == 0.0:

@@ -4,6 +4,7 @@ import math
 
 import pytest
 import torch
+import torch.utils.checkpoint
 
 from paper_2312_06881_amd import lm, nn
 from tests import lm_reference as ref
@@ -55,8 +56,8 @@ def exact(model, tokens, targets, variant):
     p = {n: v.detach().cpu().double().requires_grad_(True) for n, v in model.named_parameters()}
     M = tokens.numel()
 
-    def drop(x, seed, offset=0):
-        kept, scale = ref.keep_mask(M, D, P, seed, offset)
+    def drop(x, layer):
+        kept, scale = ref.keep_mask(M, D, P, layer.seed, layer.offset)
         return torch.where(kept, x * scale, 0.0)
 
     def norm(x, kind, w, b=None):
@@ -65,13 +66,13 @@ def exact(model, tokens, targets, variant):
         x = x * (x.square().mean(1, keepdim=True) + 1e-5).rsqrt() * w
         return x if b is None else x + b
 
-    x = drop(p["embed.weight"][tokens.cpu().view(-1)], 100)
+    x = drop(p["embed.weight"][tokens.cpu().view(-1)], model.drop)
     a = norm(x, "layer", p["first.weight"], p["first.bias"])
     for i in range(LAYERS):
         fc = [(dense(p[f"ffs.{i}.{n}.w1"], p[f"ffs.{i}.{n}.w2"], variant), p[f"ffs.{i}.{n}.bias"]) for n in ("fc1", "fc2")]
         h = a @ fc[0][0].t() + fc[0][1]
         y = (h * 0.5 * torch.erfc(-h / math.sqrt(2.0))) @ fc[1][0].t() + fc[1][1]
-        z = drop(norm(y, "rms", p[f"joins.{i}.post_weight"]), 200 + i)
+        z = drop(norm(y, "rms", p[f"joins.{i}.post_weight"]), model.joins[i].dropout)
         x = x + p[f"joins.{i}.gate"] * z
         a = norm(x, "layer", p[f"joins.{i}.weight"], p[f"joins.{i}.bias"])
     t = targets.cpu().view(-1)
@@ -91,6 +92,7 @@ def test_language_model(variant, dtype, tol):
     targets = tokens.roll(-1, 1)
     targets[:, -1] = -100
     m = Model(dtype, variant)
+    torch.manual_seed(5)
     loss = m(tokens, targets)
     loss.backward()
     want, grads = exact(m, tokens, targets, variant)
@@ -98,12 +100,33 @@ def test_language_model(variant, dtype, tol):
     for n, v in m.named_parameters():
         g = v.grad.cpu().double()
         assert (g - grads[n]).norm() <= tol * grads[n].norm(), n
-    # another pass draws other masks, evaluation none
+    # the same seed draws the same masks, another pass others, evaluation none
+    torch.manual_seed(5)
+    assert float(m(tokens, targets)) == float(loss)
     again = m(tokens, targets)
     assert float(again) != float(loss)
     m.eval()
     with torch.no_grad():
         assert float(m(tokens, targets)) == float(m(tokens, targets))
+
+
+def test_checkpointed_layers_draw_the_same_masks():
+    torch.manual_seed(3)
+    join, drop = nn.AddNorm(48, p=0.4, device="cuda", dtype=F), nn.Dropout(0.3)
+    x = torch.randn(30, 48, device="cuda", requires_grad=True)
+    y = torch.randn(30, 48, device="cuda", requires_grad=True)
+
+    def layer(x, y):
+        h, out = join(x, drop(y))
+        return h * out
+
+    results = []
+    for again in (False, True):
+        torch.manual_seed(4)
+        z = torch.utils.checkpoint.checkpoint(layer, x, y, use_reentrant=False) if again else layer(x, y)
+        results.append([z.detach(), *torch.autograd.grad(z, (x, y, join.weight, join.bias), torch.ones_like(z))])
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
 
 
 def step_tensors(seed, dtype=BF, M=600, n=128, V=700):
