@@ -71,12 +71,10 @@ int64_t up(int64_t v, int64_t q) { return (v + q - 1) / q * q; }
 // Which fp32 calls run on fp32 matrix instructions.
 bool plain_f32(int64_t M, int dtype) { return dtype == kF32 && M < kSplitFrom; }
 
-// Vocabulary columns of a piece in fp32: G within 256 MB, but for very many tokens.
-int64_t f32_piece(int64_t M, int64_t V) {
-    int64_t vp = ((int64_t)256 << 20) / (4 * (M > 0 ? M : 1)) / 128 * 128;
-    if (vp < 1024) vp = 1024;
-    return vp < V ? vp : V;
-}
+// Vocabulary columns of a piece on fp32 matrix instructions: dX's sums in one accumulator are no
+// longer than that.  (Over 524288 columns, beside a target's term of the whole gradient's size, the
+// terms below half of the sum's last bit were lost, 1e-3 of dX.)
+int64_t f32_piece(int64_t V) { return V < 16384 ? V : 16384; }
 
 // Every token's loss, its target's logit and the tiles' statistics.
 size_t stats_bytes(int64_t M, int64_t tiles) { return (size_t)up(2 * up(M, 4) * 4 + M * tiles * 8, 256); }
@@ -98,7 +96,7 @@ LossEpi epi_of(const LossPass &p) {
 size_t loss_workspace(bool backward, int64_t M, int64_t n, int64_t V, int dtype) {
     if (M == 0) return 0;
     const bool f32 = dtype == kF32, plain = plain_f32(M, dtype);
-    if (backward) return plain ? (size_t)(M * f32_piece(M, V)) * 4 : loss_mfma_backward_bytes(M, n, V, f32);
+    if (backward) return plain ? (size_t)(M * f32_piece(V)) * 4 : loss_mfma_backward_bytes(M, n, V, f32);
     return plain ? stats_bytes(M, loss_f32_tiles(M, V))
                  : stats_bytes(M, loss_mfma_tiles(M, V)) + loss_mfma_forward_bytes(M, n, V, f32);
 }
@@ -133,7 +131,7 @@ hipError_t launch_loss_backward(const LossPass &p, hipStream_t s) {
     }
     const LossEpi e = epi_of(p);
     if (!plain_f32(p.M, p.dtype)) return launch_loss_mfma_grad(p, e, s);
-    const int64_t piece = f32_piece(p.M, p.V);
+    const int64_t piece = f32_piece(p.V);
     for (int64_t v0 = 0; v0 < p.V; v0 += piece) {
         const hipError_t err = launch_loss_f32_piece(p, e, v0, p.V - v0 < piece ? p.V - v0 : piece,
                                                      static_cast<float *>(p.ws), v0 == 0, s);

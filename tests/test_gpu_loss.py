@@ -182,6 +182,11 @@ def test_few_or_many_count(dtype, ignored):
     check(x, w, t, "none", no_grad=True)
 
 
+@pytest.mark.parametrize("M,n,V,dtype", [(4096, 64, 70001, BF), (1500, 72, 66000, F), (128, 8, 530000, F)])
+def test_several_pieces_of_the_vocabulary(M, n, V, dtype):
+    check(*make(M, n, V, dtype, ignored=0.1))
+
+
 def test_many_splits_of_the_vocabulary():
     check(*make(260, 64, 40000, BF))
     check(*make(40, 192, 30000, BF))
