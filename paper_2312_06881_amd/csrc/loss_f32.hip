@@ -42,6 +42,8 @@ __device__ __forceinline__ f32x4_t load4(const float *p, int64_t ld, int64_t row
 template <int BT, bool AK, bool BK, Kind KIND>
 __global__ void __launch_bounds__(kThreads) loss_f32_kernel(Gemm g) {
     constexpr int S = BT / 32, kLoads = BT * kStage / 4 / kThreads;   // 2 x 2 waves of BT / 2
+    // a token without a gradient leaves none, whatever it (side B of dW) and the weights (dX) hold: 0 times NaN is NaN
+    constexpr bool kDw = !AK && !BK, kDx = AK && !BK;
     __shared__ float lds[2][2][BT * kPitch];
     __shared__ float2 red[KIND == kStats ? BT * 2 : 1];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lr = lane & 15, lg = lane >> 4;
@@ -61,6 +63,10 @@ __global__ void __launch_bounds__(kThreads) loss_f32_kernel(Gemm g) {
             const int v = tid + q * kThreads;
             ra[q] = load4<AK>(g.A, g.lda, i0 + row_of(AK, v), k0 + k_of(AK, v), g.I, g.K);
             rb[q] = load4<BK>(g.B, g.ldb, j0 + row_of(BK, v), k0 + k_of(BK, v), g.J, g.K);
+            if constexpr (kDw) {
+                const int64_t m = k0 + k_of(BK, v);
+                if (m < g.K && loss_scale(g.e, m, g.e.targets[m]) == 0.f) rb[q] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            }
         }
     };
     const auto put = [&](bool kc, float *dst, int v, const f32x4_t &r) {
@@ -110,9 +116,11 @@ __global__ void __launch_bounds__(kThreads) loss_f32_kernel(Gemm g) {
         if (row >= g.I) continue;
         float dl = 0.f, lse = 0.f;
         int64_t t = -1;
-        if constexpr (KIND == kGrad) {
+        if constexpr (KIND == kGrad || kDx) {
             t = g.e.targets[row];
             dl = loss_scale(g.e, row, t);
+        }
+        if constexpr (KIND == kGrad) {
             lse = g.e.lse[row];
             t -= g.v0;
         }
@@ -127,6 +135,7 @@ __global__ void __launch_bounds__(kThreads) loss_f32_kernel(Gemm g) {
                 if constexpr (KIND == kGrad)
                     x = dl != 0.f ? dl * (__builtin_amdgcn_exp2f((x - lse) * kLog2e) - (col == t ? 1.f : 0.f)) : 0.f;
                 if constexpr (KIND == kAdd) x += *o;
+                if constexpr (kDx) x = dl != 0.f ? x : 0.f;
                 *o = x;
             }
     }

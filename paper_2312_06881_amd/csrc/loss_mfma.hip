@@ -410,9 +410,10 @@ __global__ void __launch_bounds__(256) gather_kernel(const uint16_t *src, uint16
     }
 }
 
-// The same of fp32 rows, as three planes.
+// The same of fp32 rows, as three planes.  e's targets, where given, are the rows': those that do not count become
+// zero, as dW multiplies them as they are, by a G of zero, which leaves a NaN (with bf16 operands scale_kernel does it).
 __global__ void __launch_bounds__(256) gather_split_kernel(const float *src, uint16_t *dst, int64_t plane, int64_t rows, int n,
-                                                           int np, const int *idx, const int *count) {
+                                                           int np, const int *idx, const int *count, LossEpi e) {
     if (count) rows = *count;
     const int64_t total = rows * (np / 8);
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
@@ -421,6 +422,9 @@ __global__ void __launch_bounds__(256) gather_split_kernel(const float *src, uin
         octet_at(i, total, np, r, c);
         float v[8];
         load_cols<true>(src + (idx ? idx[r] : r) * n, c, n, v);
+        if (e.targets && !loss_counts(e, e.targets[r]))
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = 0.f;
         uint4 p[3];
         split8(v, p);
 #pragma unroll
@@ -586,7 +590,7 @@ __global__ void __launch_bounds__(256) round_transpose_kernel(const float *acc, 
     for (int q = 0; q < 2; ++q) {
         const int m = (tid + 256 * q) / 8, c = (tid + 256 * q) % 8 * 8;
         if (m0 + m >= M) continue;
-        const float by = kBf16 ? scale[m0 + m] : 1.f;
+        const float own = scale[m0 + m], by = kBf16 || own == 0.f ? own : 1.f;   // fp32 sums hold it already
         float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = by != 0.f ? t[m][c + e] * by : 0.f;
@@ -719,11 +723,11 @@ struct Prepared {
     const int64_t *targets;
 };
 hipError_t gather(const void *src, uint16_t *dst, int64_t rows, int64_t n, int64_t np, bool f32, const int *idx,
-                  const int *count, hipStream_t s) {
+                  const int *count, const LossEpi &e, hipStream_t s) {
     const int64_t blocks = (rows * (np / 8) + 255) / 256;
     const unsigned grid = (unsigned)(blocks < 16384 ? blocks : 16384);
     if (f32)
-        gather_split_kernel<<<grid, 256, 0, s>>>(static_cast<const float *>(src), dst, rows * np, rows, (int)n, (int)np, idx, count);
+        gather_split_kernel<<<grid, 256, 0, s>>>(static_cast<const float *>(src), dst, rows * np, rows, (int)n, (int)np, idx, count, e);
     else
         gather_kernel<<<grid, 256, 0, s>>>(static_cast<const uint16_t *>(src), dst, rows, (int)n, (int)np, idx, count);
     return hipGetLastError();
@@ -743,12 +747,12 @@ hipError_t prepare(const Operands &o, const LossPass &p, const LossEpi &e, char 
     }
     if (err == hipSuccess && (o.compact || o.np != p.n || o.f32)) {
         uint16_t *x = reinterpret_cast<uint16_t *>(ws + o.x);
-        err = gather(p.X, x, p.M, p.n, o.np, o.f32, r.idx, r.count, s);
+        err = gather(p.X, x, p.M, p.n, o.np, o.f32, r.idx, r.count, o.compact ? LossEpi{} : e, s);
         r.X = x;
     }
     if (err == hipSuccess && (o.np != p.n || o.f32)) {
         uint16_t *w = reinterpret_cast<uint16_t *>(ws + o.w);
-        err = gather(p.W, w, p.V, p.n, o.np, o.f32, nullptr, nullptr, s);
+        err = gather(p.W, w, p.V, p.n, o.np, o.f32, nullptr, nullptr, LossEpi{}, s);
         r.W = w;
     }
     return err;
