@@ -42,11 +42,12 @@ struct Token {
 
 constexpr int kGExp = 15;                       // G is held as G 2^15
 
-// What a column is multiplied by, as an exponent, from the bits of its largest finite magnitude.
+// What a column is multiplied by, as an exponent, from the bits of its largest finite magnitude:
+// -113 for magnitudes of 2^127 and more, and at most 120 (2^-106 and less are held below 2^14).
 __device__ __forceinline__ int column_exp(uint32_t top) {
     if (top == 0u) return 0;
     const int e = 14 + 127 - (int)(top >> 23);
-    return e < -100 ? -100 : e > 120 ? 120 : e;
+    return e > 120 ? 120 : e;
 }
 
 __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
