@@ -759,6 +759,11 @@ hipError_t prepare(const Operands &o, const LossPass &p, const LossEpi &e, char 
     return err;
 }
 
+// dX's reduction units in one accumulator at most (split fp32: 16384 vocabulary columns; bf16: 98304).  Each unit is two
+// additions, and each may lose half of the last bit of a sum that a target's term has made as large as the whole
+// gradient: 1e-4 of it at worst, where 43520 columns of small terms of one sign had lost 3.6e-5 in place of 1.2e-5.
+constexpr int64_t kMostUnits = 1536;
+
 // Vocabulary columns of a piece, and the workspace of a backward pass.
 struct Layout {
     Operands ops;
@@ -785,6 +790,11 @@ Layout layout_of(int64_t M, int64_t n, int64_t V, bool f32) {
     const int64_t room = ((int64_t)64 << 20) / (n * l.Mp);
     splits = splits < room ? splits : room;
     l.dx = choose(n, M, splits < 1 ? 1 : splits);
+    const int64_t longest = l.dx.splits * kMostUnits / (f32 ? kProducts : 1) * kPPK;
+    if (l.vp > longest) {
+        const int64_t shorter = (V + longest - 1) / longest;
+        l.vp = up((V + shorter - 1) / shorter, 256);
+    }
     l.tokens = space.take((size_t)l.Mq * 12);
     l.tops = space.take(f32 ? 0 : (size_t)l.nq * 8);
     l.xs = space.take(f32 ? 0 : (size_t)(M * l.ops.np) * 2);
