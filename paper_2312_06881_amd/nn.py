@@ -547,11 +547,16 @@ def linear_cross_entropy(x, weight, targets, ignore_index=-100, reduction="mean"
     return loss.reshape(targets.shape) if reduction == "none" else loss
 
 
+def _draw():
+    """A whole number from torch's CPU generator, whatever the default device is."""
+    return int(torch.randint(2 ** 62, (), device="cpu").item())
+
+
 class Dropout(torch.nn.Module):
     """Dropout whose mask is drawn from a counter and never stored.  Every call in training draws its offset (kept in
     ``offset``) from torch's CPU generator, so torch.manual_seed makes runs repeat, and activation checkpointing, which
-    restores that generator, draws the same mask when it runs the layer again.  seed: by default drawn there too; layers
-    that share one still differ by their offsets.  capturable: the offset counts calls on the device (``calls``, with the
+    restores that generator, draws the same mask when it runs the layer again.  seed: by default drawn there too (0 for a
+    layer made with p = 0, which draws nothing); layers that share one still differ by their offsets.  capturable: the offset counts calls on the device (``calls``, with the
     module), so that every replay of a captured call draws another mask; not for layers that checkpointing runs
     again."""
 
@@ -560,7 +565,7 @@ class Dropout(torch.nn.Module):
         if not 0.0 <= p <= 1.0:
             raise ValueError(f"p is a probability, got {p}")
         self.p, self.capturable, self.offset = p, capturable, None
-        self.seed = int(torch.randint(2 ** 62, ()).item()) if seed is None else seed
+        self.seed = seed if seed is not None else _draw() if p or capturable else 0
         if capturable:
             self.register_buffer("calls", torch.zeros((1,), dtype=torch.int64, device=device))
 
@@ -570,7 +575,7 @@ class Dropout(torch.nn.Module):
             now = self.calls.clone()     # the backward pass draws this call's mask again
             self.calls += 1
             return now
-        self.offset = int(torch.randint(2 ** 62, ()).item())
+        self.offset = _draw()
         return self.offset
 
     def forward(self, x):
