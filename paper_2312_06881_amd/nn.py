@@ -556,9 +556,10 @@ class Dropout(torch.nn.Module):
     """Dropout whose mask is drawn from a counter and never stored.  Every call in training draws its offset (kept in
     ``offset``) from torch's CPU generator, so torch.manual_seed makes runs repeat, and activation checkpointing, which
     restores that generator, draws the same mask when it runs the layer again.  seed: by default drawn there too (0 for a
-    layer made with p = 0, which draws nothing); layers that share one still differ by their offsets.  capturable: the offset counts calls on the device (``calls``, with the
-    module), so that every replay of a captured call draws another mask; not for layers that checkpointing runs
-    again."""
+    layer made with p = 0, which draws nothing); layers that share one still differ by their offsets.  capturable: the
+    offset counts calls on the device (``calls``, with the module), so that every replay of a captured call draws
+    another mask.  Such a layer needs a seed of its own (copies of it count alike), and is refused where checkpointing
+    runs it again, with another count."""
 
     def __init__(self, p=0.1, seed=None, capturable=False, device=None):
         super().__init__()
@@ -572,6 +573,9 @@ class Dropout(torch.nn.Module):
     def next_offset(self):
         """The offset of the call that asks."""
         if self.capturable:
+            if torch._C._current_graph_task_id() != -1:      # inside a backward pass
+                raise RuntimeError("a capturable Dropout cannot be run again by activation checkpointing: its count has "
+                                   "gone on, and with it the mask; capturable=False draws the same mask again")
             now = self.calls.clone()     # the backward pass draws this call's mask again
             self.calls += 1
             return now
