@@ -89,7 +89,7 @@ struct Args {
     LossEpi e;
     Token tok;
     const uint32_t *col_top;     // kDw: of the columns of dloss X
-    int64_t v0;
+    int64_t v0;                  // the piece's first vocabulary column
     void *out;
     float *acc;
     int64_t ldo;
@@ -232,7 +232,7 @@ __global__ void __launch_bounds__(kPPThreads, 1) loss_pp_kernel(Args g) {
             units, wave, acc, issue_a, issue_b, addr, [](int) { return true; });
     // acc[i][j][v]: side A's row wm0 + 16 i + lr, side B's wn0 + 16 j + 4 lg + v
     if constexpr (KIND == kStats) {
-        loss_stats<SM, SN, BM, WGN>(g.e, acc, i0, g.I, j0, tile_j, wm0, wn0, wave % WGN, reinterpret_cast<float2 *>(smem));
+        loss_stats<SM, SN, BM, WGN>(g.e, acc, i0, g.I, g.v0 + j0, (int)(g.v0 / BN) + tile_j, wm0, wn0, wave % WGN, reinterpret_cast<float2 *>(smem));
     } else if constexpr (KIND == kGrad) {
         const int v_lane = (int)(g.v0 + i0) + wm0 + lr;
 #pragma unroll
@@ -698,13 +698,15 @@ struct Space {
     }
 };
 
-// The tokens that count and the operands as the kernels read them; in fp32 three planes each.
+// The tokens that count and the operands as the kernels read them, W a piece at a time; in fp32
+// three planes each.
 struct Operands {
     int64_t np;                  // columns
     bool compact, f32;
     size_t idx, targets, count, x, w;
 };
-Operands operands_of(Space &space, int64_t M, int64_t n, int64_t V, bool f32) {
+bool lays_out_w(int64_t n, bool f32) { return f32 || n % kPPK != 0; }
+Operands operands_of(Space &space, int64_t M, int64_t n, int64_t piece, bool f32) {
     Operands o;
     o.np = up(n, kPPK);
     o.compact = M >= kCompactFrom;
@@ -713,13 +715,13 @@ Operands operands_of(Space &space, int64_t M, int64_t n, int64_t V, bool f32) {
     o.targets = space.take(o.compact ? (size_t)M * 8 : 0);
     o.count = space.take(o.compact ? 4 : 0);
     o.x = space.take(f32 ? (size_t)(M * o.np) * 6 : o.compact || o.np != n ? (size_t)(M * o.np) * 2 : 0);
-    o.w = space.take(f32 ? (size_t)(V * o.np) * 6 : o.np != n ? (size_t)(V * o.np) * 2 : 0);
+    o.w = space.take(lays_out_w(n, f32) ? (size_t)(piece * o.np) * (f32 ? 6 : 2) : 0);
     return o;
 }
 
 // What the launches take of them.
 struct Prepared {
-    const uint16_t *X, *W;
+    const uint16_t *X;
     const int *idx, *count;
     const int64_t *targets;
 };
@@ -735,7 +737,7 @@ hipError_t gather(const void *src, uint16_t *dst, int64_t rows, int64_t n, int64
 }
 hipError_t prepare(const Operands &o, const LossPass &p, const LossEpi &e, char *ws, float *loss, float *lse, Prepared &r,
                    hipStream_t s) {
-    r = {static_cast<const uint16_t *>(p.X), static_cast<const uint16_t *>(p.W), nullptr, nullptr, e.targets};
+    r = {static_cast<const uint16_t *>(p.X), nullptr, nullptr, e.targets};
     hipError_t err = hipSuccess;
     if (o.compact) {
         int *idx = reinterpret_cast<int *>(ws + o.idx), *count = reinterpret_cast<int *>(ws + o.count);
@@ -751,12 +753,31 @@ hipError_t prepare(const Operands &o, const LossPass &p, const LossEpi &e, char 
         err = gather(p.X, x, p.M, p.n, o.np, o.f32, r.idx, r.count, o.compact ? LossEpi{} : e, s);
         r.X = x;
     }
-    if (err == hipSuccess && (o.np != p.n || o.f32)) {
-        uint16_t *w = reinterpret_cast<uint16_t *>(ws + o.w);
-        err = gather(p.W, w, p.V, p.n, o.np, o.f32, nullptr, nullptr, LossEpi{}, s);
-        r.W = w;
-    }
     return err;
+}
+// Rows v0 .. v0 + vn - 1 of W.
+hipError_t prepare_w(const Operands &o, const LossPass &p, int64_t v0, int64_t vn, char *ws, const uint16_t *&W, hipStream_t s) {
+    const char *rows = static_cast<const char *>(p.W) + v0 * p.n * (o.f32 ? 4 : 2);
+    W = reinterpret_cast<const uint16_t *>(rows);
+    if (!lays_out_w(p.n, o.f32)) return hipSuccess;
+    uint16_t *w = reinterpret_cast<uint16_t *>(ws + o.w);
+    W = w;
+    return gather(rows, w, vn, p.n, o.np, o.f32, nullptr, nullptr, LossEpi{}, s);
+}
+
+// The vocabulary in pieces of one size, whole tiles, of at most `most` columns or 2048 (which of
+// very long rows are more than the bytes that `most` is from).
+int64_t piece_of(int64_t V, int64_t most) {
+    most = most / 256 * 256;
+    if (most < 2048) most = 2048;
+    const int64_t pieces = (V + most - 1) / most;
+    return up((V + pieces - 1) / pieces, 256);
+}
+// What a piece of W laid out otherwise, and of G, may take.
+constexpr int64_t kPieceBytes = (int64_t)512 << 20;
+
+int64_t forward_piece(int64_t n, int64_t V, bool f32) {
+    return lays_out_w(n, f32) ? piece_of(V, kPieceBytes / ((f32 ? 6 : 2) * up(n, kPPK))) : V;
 }
 
 // dX's reduction units in one accumulator at most (split fp32: 16384 vocabulary columns; bf16: 98304).  Each unit is two
@@ -767,7 +788,7 @@ constexpr int64_t kMostUnits = 1536;
 // Vocabulary columns of a piece, and the workspace of a backward pass.
 struct Layout {
     Operands ops;
-    int64_t Mp, Mq, nq, Vp, vp;
+    int64_t Mp, Mq, nq, vp;
     Choice dx;
     size_t tokens, tops, xs, wt, gt, acc, total;
 };
@@ -775,30 +796,24 @@ Layout layout_of(int64_t M, int64_t n, int64_t V, bool f32) {
     Layout l;
     Space space;
     const size_t value = f32 ? 6 : 2;    // bytes
-    l.ops = operands_of(space, M, n, V, f32);
     l.Mp = up(M, kPPK);
     l.Mq = up(M, 256) + 256;     // the last tile's tokens, whatever its width
     l.nq = up(n, 256) + 256;
-    l.Vp = up(V, kPPK);
-    // G^T of a piece within 512 MB, but for very many tokens; pieces of one size, whole tiles
-    int64_t most = ((int64_t)512 << 20) / ((int64_t)value * l.Mp) / 256 * 256;
-    if (most < 2048) most = 2048;
-    const int64_t pieces = (V + most - 1) / most;
-    l.vp = up((V + pieces - 1) / pieces, 256);
+    // G^T of a piece within kPieceBytes, and W^T with W where it is laid out
+    const int64_t longer = n + (lays_out_w(n, f32) ? up(n, kPPK) : 0);
+    l.vp = piece_of(V, kPieceBytes / ((int64_t)value * (l.Mp > longer ? l.Mp : longer)));
     // at least 16 units a split, and the splits' sums within 256 MB
     int64_t splits = l.vp / kPPK * (f32 ? kProducts : 1) / 16;
     const int64_t room = ((int64_t)64 << 20) / (n * l.Mp);
     splits = splits < room ? splits : room;
     l.dx = choose(n, M, splits < 1 ? 1 : splits);
     const int64_t longest = l.dx.splits * kMostUnits / (f32 ? kProducts : 1) * kPPK;
-    if (l.vp > longest) {
-        const int64_t shorter = (V + longest - 1) / longest;
-        l.vp = up((V + shorter - 1) / shorter, 256);
-    }
+    if (l.vp > longest) l.vp = piece_of(V, longest);
+    l.ops = operands_of(space, M, n, l.vp, f32);
     l.tokens = space.take((size_t)l.Mq * 12);
     l.tops = space.take(f32 ? 0 : (size_t)l.nq * 8);
     l.xs = space.take(f32 ? 0 : (size_t)(M * l.ops.np) * 2);
-    l.wt = space.take((size_t)(n * l.Vp) * value);
+    l.wt = space.take((size_t)(n * l.vp) * value);
     l.gt = space.take((size_t)(l.vp * l.Mp) * value);
     l.acc = space.take((size_t)(l.dx.splits * n * l.Mp) * 4);
     l.total = space.total;
@@ -814,7 +829,7 @@ int loss_mfma_tiles(int64_t M, int64_t V) {
 
 size_t loss_mfma_forward_bytes(int64_t M, int64_t n, int64_t V, bool f32) {
     Space space;
-    operands_of(space, M, n, V, f32);
+    operands_of(space, M, n, forward_piece(n, V, f32), f32);
     return space.total;
 }
 
@@ -824,7 +839,9 @@ hipError_t launch_loss_mfma_stats(const LossPass &p, const LossEpi &e, void *ws,
                                   hipStream_t s) {
     Space space;
     const bool f32 = p.dtype == kF32;
-    const Operands o = operands_of(space, p.M, p.n, p.V, f32);
+    const int64_t piece = forward_piece(p.n, p.V, f32);
+    const Operands o = operands_of(space, p.M, p.n, piece, f32);
+    const Choice tile = choose(p.M, p.V);
     Prepared r;
     hipError_t err = prepare(o, p, e, static_cast<char *>(ws), each, p.lse, r, s);
     if (err != hipSuccess) return err;
@@ -834,13 +851,17 @@ hipError_t launch_loss_mfma_stats(const LossPass &p, const LossEpi &e, void *ws,
     g.e.targets = r.targets;
     g.count = r.count;
     g.A = r.X;
-    g.B = r.W;
     g.plane_a = p.M * o.np;
-    g.plane_b = p.V * o.np;
     g.I = p.M;
-    g.J = p.V;
     g.K = g.lda = g.ldb = o.np;
-    return launch<false, kStats>(g, choose(p.M, p.V), f32, s);
+    for (int64_t v0 = 0; v0 < p.V && err == hipSuccess; v0 += piece) {
+        g.v0 = v0;
+        g.J = p.V - v0 < piece ? p.V - v0 : piece;
+        g.plane_b = g.J * o.np;
+        err = prepare_w(o, p, v0, g.J, static_cast<char *>(ws), g.B, s);
+        if (err == hipSuccess) err = launch<false, kStats>(g, tile, f32, s);
+    }
+    return err;
 }
 
 hipError_t launch_loss_mfma_grad(const LossPass &p, const LossEpi &e, hipStream_t s) {
@@ -864,7 +885,7 @@ hipError_t launch_loss_mfma_grad(const LossPass &p, const LossEpi &e, hipStream_
         const int64_t blocks = (rows + 63) / 64;
         return dim3((unsigned)(blocks < 1024 ? blocks : 1024), (unsigned)((n + 255) / 256));
     };
-    const int64_t plane_x = p.M * l.ops.np, plane_w = p.V * l.ops.np, plane_wt = p.n * l.Vp, plane_gt = l.vp * l.Mp;
+    const int64_t plane_x = p.M * l.ops.np, plane_wt = p.n * l.vp, plane_gt = l.vp * l.Mp;
     if (err == hipSuccess && p.dW && !f32) {
         const int64_t blocks = (p.M * (np / 8) + 255) / 256;
         column_top_kernel<<<top_grid(p.M), 256, 0, s>>>(r.X, tok.scale, p.M, n, np, r.count, x_top);
@@ -873,17 +894,11 @@ hipError_t launch_loss_mfma_grad(const LossPass &p, const LossEpi &e, hipStream_
         err = hipGetLastError();
     }
     if (err == hipSuccess && p.dX) {
-        const dim3 grid((unsigned)(l.Vp / 64), (unsigned)(np / 64));
         const unsigned rows = (unsigned)(p.M < 8192 ? p.M : 8192);
-        if (f32) {
-            transpose_split_kernel<<<grid, 256, 0, s>>>(static_cast<const float *>(p.W), at(l.wt), plane_wt, p.V, n, l.Vp);
-            if (r.count) zero_rows_kernel<<<rows, 256, 0, s>>>(e, static_cast<float *>(p.dX), p.M, n);
-        } else {
-            const uint16_t *W = static_cast<const uint16_t *>(p.W);
-            column_top_kernel<<<top_grid(p.V), 256, 0, s>>>(W, nullptr, p.V, n, n, nullptr, w_top);
-            transpose_kernel<<<grid, 256, 0, s>>>(W, w_top, at(l.wt), p.V, n, l.Vp);
-            if (r.count) zero_rows_kernel<<<rows, 256, 0, s>>>(e, static_cast<uint16_t *>(p.dX), p.M, n);
-        }
+        if (!f32)
+            column_top_kernel<<<top_grid(p.V), 256, 0, s>>>(static_cast<const uint16_t *>(p.W), nullptr, p.V, n, n, nullptr, w_top);
+        if (r.count && f32) zero_rows_kernel<<<rows, 256, 0, s>>>(e, static_cast<float *>(p.dX), p.M, n);
+        if (r.count && !f32) zero_rows_kernel<<<rows, 256, 0, s>>>(e, static_cast<uint16_t *>(p.dX), p.M, n);
         err = hipGetLastError();
     }
     float *acc = reinterpret_cast<float *>(ws + l.acc);
@@ -894,9 +909,10 @@ hipError_t launch_loss_mfma_grad(const LossPass &p, const LossEpi &e, hipStream_
         g.count = r.count;
         g.tok = tok;
         g.v0 = v0;
-        g.A = r.W + v0 * l.ops.np;
+        err = prepare_w(l.ops, p, v0, vn, ws, g.A, s);
+        if (err != hipSuccess) break;
         g.B = r.X;
-        g.plane_a = plane_w;
+        g.plane_a = vn * l.ops.np;
         g.plane_b = plane_x;
         g.lda = g.ldb = g.K = l.ops.np;
         g.I = vn;
@@ -917,9 +933,17 @@ hipError_t launch_loss_mfma_grad(const LossPass &p, const LossEpi &e, hipStream_
             err = launch<true, kDw>(g, choose(g.I, g.J), f32, s);
         }
         if (err == hipSuccess && p.dX) {
-            g.A = at(l.wt) + v0;
+            const dim3 grid((unsigned)((vn + 63) / 64), (unsigned)(np / 64));
+            if (f32)
+                transpose_split_kernel<<<grid, 256, 0, s>>>(static_cast<const float *>(p.W) + v0 * n, at(l.wt), plane_wt, vn, n, l.vp);
+            else
+                transpose_kernel<<<grid, 256, 0, s>>>(static_cast<const uint16_t *>(p.W) + v0 * n, w_top, at(l.wt), vn, n, l.vp);
+            err = hipGetLastError();
+        }
+        if (err == hipSuccess && p.dX) {
+            g.A = at(l.wt);
             g.plane_a = plane_wt;
-            g.lda = l.Vp;
+            g.lda = l.vp;
             g.B = at(l.gt);
             g.plane_b = plane_gt;
             g.ldb = g.ldo = l.Mp;

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_2312_06881_amd import nn
-from tests.test_gpu_loss import DTYPES, F, check, make
+from tests.test_gpu_loss import BF, DTYPES, F, check, make
 
 pytestmark = pytest.mark.gpu
 
@@ -37,3 +37,9 @@ def test_long_vocabularies_keep_their_small_terms():
     dx, = torch.autograd.grad(loss, x)
     want = c * (V - 1) / V + (1 / V - 1)
     assert float((dx.double() - want).abs().max()) <= (512 + 16) * 2.0 ** -25
+
+
+@pytest.mark.parametrize("M,n,V,dtype", [(130, 16384, 5600, F), (130, 16392, 17000, BF), (600, 5000, 20011, F)])
+def test_weights_laid_out_a_piece_at_a_time(M, n, V, dtype):
+    # more than 512 MB of them, in both passes
+    check(*make(M, n, V, dtype))

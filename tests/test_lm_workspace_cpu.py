@@ -1,0 +1,29 @@
+"""What the loss's passes ask for: pieces of the vocabulary, not the whole of it."""
+import pytest
+
+import paper_2312_06881_amd as dy
+
+MB = 2 ** 20
+SIZES = [(129, 4096, 128256), (512, 4096, 50000), (512, 4100, 50000), (4096, 4096, 32768), (1024, 16384, 128256), (64, 768, 2 ** 22),
+         (16384, 768, 50000), (300, 1000, 777)]
+
+
+@pytest.mark.parametrize("dtype", [dy.F32, dy.BF16])
+@pytest.mark.parametrize("M,n,V", SIZES)
+def test_workspaces_do_not_grow_with_the_vocabulary(M, n, V, dtype):
+    if dtype == dy.F32 and M < 129:
+        pytest.skip("no weights are laid out")
+    value = 6 if dtype == dy.F32 else 2
+    # a piece of W laid out otherwise: 512 MB.  The tokens: X, X times dloss and their places, rows padded to 64; by
+    # them their tiles' statistics.
+    rows = M * (n + 64) * (value + 2) + 64 * (M + 512)
+    forward = dy.dyad_linear_ce_workspace_bytes(dy.CE_FORWARD, M, n, V, dtype)
+    assert 0 < forward <= 512 * MB + rows + 8 * M * (V // 128 + 1) + MB
+    # W^T, G^T: 512 MB each.  dX's sums: 256 MB over those of one split.
+    backward = dy.dyad_linear_ce_workspace_bytes(dy.CE_BACKWARD, M, n, V, dtype)
+    assert 0 < backward <= (512 + 512 + 256) * MB + rows + 4 * (M + 64) * n + 16 * n + MB
+
+
+def test_pieces_of_very_long_rows_are_not_shorter_than_2048_columns():
+    n = 2 ** 20
+    assert dy.dyad_linear_ce_workspace_bytes(dy.CE_BACKWARD, 64, n, 2048, dy.BF16) >= 2 * 2048 * n
