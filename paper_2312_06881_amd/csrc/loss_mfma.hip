@@ -14,6 +14,10 @@
 // 2^15 for G (values from 2^-29 on keep all bits), and one a column for the other two, which
 // takes the column's largest magnitude to 2^14 .. 2^15 and goes out again with the sums.
 //
+// An entry that every token finds improbable has a row of G, and of dW, below that range.  Rows whose
+// largest |G| is under 2^-24 are formed again, gathered, each at a power of two of its own (kGrad and kDw with
+// RARE).  From 2^-24 on fp16's smallest step, 2^-39, is at most 2^-15 of the row's largest value.
+//
 // fp32 operands (from kSplitFrom tokens) are split in three bf16 values, x = h + m + l with 8 bits
 // each, exact to 2^-27, and six of the nine products h h, h m, m h, h l, l h, m m are summed in
 // fp32; the others are below 2^-26 of the whole.  The reduction is six times as long at eight
@@ -89,6 +93,10 @@ struct Args {
     LossEpi e;
     Token tok;
     const uint32_t *col_top;     // kDw: of the columns of dloss X
+    float *row_top;              // kGrad: each row's largest |G| 2^15 of a tile's tokens, [tiles][ldt]; null: not wanted
+    int64_t ldt;
+    // RARE: how many rows, and for each its vocabulary entry in the piece and its exponent beside kGExp
+    const int *rare, *rare_row, *rare_exp;
     int64_t v0;                  // the piece's first vocabulary column
     void *out;
     float *acc;
@@ -126,8 +134,9 @@ __device__ __forceinline__ uint4 pack_pair(const float (&x)[8], Pack pack) {
 }
 __device__ __forceinline__ int lane_piece(int lg) { return (lg & 1) * 16 + (lg >> 1) * 8; }
 
-template <int BM, int BN, int WGM, int WGN, bool TB, Kind KIND, bool F32>
-__global__ void __launch_bounds__(kPPThreads, 1) loss_pp_kernel(Args g) {
+// One tile of one split.
+template <int BM, int BN, int WGM, int WGN, bool TB, Kind KIND, bool F32, bool RARE>
+__device__ __forceinline__ void loss_tile(const Args &g, int block, int tiles_i, int tiles_j) {
     using C = Cfg<BM, BN, WGM, WGN, TB>;
     using SA = typename C::A;
     using SB = typename C::B;
@@ -136,20 +145,10 @@ __global__ void __launch_bounds__(kPPThreads, 1) loss_pp_kernel(Args g) {
     lds_u8 *lds = (lds_u8 *)smem;
     const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (g.count) {
-        const int64_t tokens = *g.count;
-        if (KIND == kStats) g.I = tokens;
-        if (KIND == kGrad || KIND == kDx) g.J = tokens;
-        if (KIND == kDw) {
-            g.K = (tokens + kPPK - 1) / kPPK * kPPK;
-            g.rows_b = tokens;
-        }
-    }
-    const int tiles_i = (int)((g.I + BM - 1) / BM), tiles_j = (int)((g.J + BN - 1) / BN), tiles = tiles_i * tiles_j;
-    if ((int)blockIdx.x >= tiles * g.splits) return;
+    const int tiles = tiles_i * tiles_j;
     // runs of `group` panels of side A, side A fastest: the workgroups that run together on an
     // XCD share both sides
-    int item = xcd_tile(blockIdx.x, tiles * g.splits);
+    int item = RARE ? block : xcd_tile(block, tiles * g.splits);
     const int split = KIND == kDx ? item / tiles : 0;
     item -= split * tiles;
     const int run = g.group * tiles_j, first = item / run * g.group;
@@ -234,7 +233,16 @@ __global__ void __launch_bounds__(kPPThreads, 1) loss_pp_kernel(Args g) {
     if constexpr (KIND == kStats) {
         loss_stats<SM, SN, BM, WGN>(g.e, acc, i0, g.I, g.v0 + j0, (int)(g.v0 / BN) + tile_j, wm0, wn0, wave % WGN, reinterpret_cast<float2 *>(smem));
     } else if constexpr (KIND == kGrad) {
-        const int v_lane = (int)(g.v0 + i0) + wm0 + lr;
+        int v_of[SM], up_by[SM];     // the lane's rows: their vocabulary entries, and exponents
+        float top[SM];               // of what the lane has of them, the largest
+#pragma unroll
+        for (int i = 0; i < SM; ++i) {
+            int row = (int)i0 + wm0 + 16 * i + lr;
+            if constexpr (RARE) row = row < g.I ? row : 0;
+            v_of[i] = (int)g.v0 + (RARE ? g.rare_row[row] : row);
+            up_by[i] = kGExp + (RARE ? g.rare_exp[row] : 0);
+            top[i] = 0.f;
+        }
 #pragma unroll
         for (int jp = 0; jp < SN / 2; ++jp) {
             float scale[8], lse[8];
@@ -254,8 +262,9 @@ __global__ void __launch_bounds__(kPPThreads, 1) loss_pp_kernel(Args g) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float z = acc[i][2 * jp + (e >> 2)][e & 3];
-                    const float p = __builtin_amdgcn_exp2f(F32 ? (z - lse[e]) * kLog2e : fmaf(z, kLog2e, -lse[e])) - (target[e] == v_lane + 16 * i ? 1.f : 0.f);
-                    x[e] = scale[e] != 0.f ? p * (F32 ? scale[e] : (float)(1 << kGExp)) : 0.f;   // zero whatever p is
+                    const float p = __builtin_amdgcn_exp2f(F32 ? (z - lse[e]) * kLog2e : fmaf(z, kLog2e, -lse[e])) - (target[e] == v_of[i] ? 1.f : 0.f);
+                    x[e] = scale[e] != 0.f ? F32 ? p * scale[e] : RARE ? ldexpf(p, up_by[i]) : p * (float)(1 << kGExp) : 0.f;   // zero whatever p is
+                    if constexpr (!F32 && !RARE) top[i] = fmaxf(top[i], fabsf(x[e]));
                 }
                 const bool in = col < g.ldo && i0 + wm0 + 16 * i + lr < g.I;
                 if constexpr (F32) {
@@ -270,6 +279,24 @@ __global__ void __launch_bounds__(kPPThreads, 1) loss_pp_kernel(Args g) {
                 } else {
                     const uint4 w = pack_pair(x, pack_f16);
                     if (in) *reinterpret_cast<uint4 *>(o + (int64_t)(16 * i) * g.ldo) = w;
+                }
+            }
+        }
+        if constexpr (!F32 && !RARE) {
+            if (g.row_top) {
+                float *red = reinterpret_cast<float *>(smem);      // [WGN][BM]
+#pragma unroll
+                for (int i = 0; i < SM; ++i) {
+                    top[i] = fmaxf(top[i], __shfl_xor(top[i], 16));
+                    top[i] = fmaxf(top[i], __shfl_xor(top[i], 32));
+                    if (lg == 0) red[(wave % WGN) * BM + wm0 + 16 * i + lr] = top[i];
+                }
+                __syncthreads();
+                for (int r = threadIdx.x; r < left_i; r += kPPThreads) {
+                    float t = red[r];
+#pragma unroll
+                    for (int w = 1; w < WGN; ++w) t = fmaxf(t, red[w * BM + r]);
+                    g.row_top[(int64_t)tile_j * g.ldt + i0 + r] = t;
                 }
             }
         }
@@ -306,12 +333,14 @@ __global__ void __launch_bounds__(kPPThreads, 1) loss_pp_kernel(Args g) {
 #pragma unroll
             for (int i = 0; i < SM; ++i) {
                 const int64_t row = i0 + wm0 + 16 * i + lr;
+                const int64_t own = row < g.I ? row : 0;
+                const int down = RARE ? g.rare_exp[own] : 0;
                 float x[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = ldexpf(acc[i][2 * jp + (e >> 2)][e & 3], back[e]);
+                for (int e = 0; e < 8; ++e) x[e] = ldexpf(acc[i][2 * jp + (e >> 2)][e & 3], back[e] - down);
                 const uint4 w = pack_pair(x, pack_bf16);
                 if (row >= g.I) continue;
-                uint16_t *o = static_cast<uint16_t *>(g.out) + row * g.ldo + col;
+                uint16_t *o = static_cast<uint16_t *>(g.out) + (RARE ? g.rare_row[own] : row) * g.ldo + col;
                 if (col + 8 <= g.J) {
                     __builtin_memcpy(o, &w, 16);
                 } else {
@@ -339,6 +368,28 @@ __global__ void __launch_bounds__(kPPThreads, 1) loss_pp_kernel(Args g) {
                 *o = s;
             }
         }
+    }
+}
+
+// RARE: the grid is smaller than the tiles may be many, and a workgroup takes several.
+template <int BM, int BN, int WGM, int WGN, bool TB, Kind KIND, bool F32, bool RARE = false>
+__global__ void __launch_bounds__(kPPThreads, 1) loss_pp_kernel(Args g) {
+    if (g.count) {
+        const int64_t tokens = *g.count;
+        if (KIND == kStats) g.I = tokens;
+        if (KIND == kGrad || KIND == kDx) g.J = tokens;
+        if (KIND == kDw) {
+            g.K = (tokens + kPPK - 1) / kPPK * kPPK;
+            g.rows_b = tokens;
+        }
+    }
+    if constexpr (RARE) g.I = *g.rare;
+    const int tiles_i = (int)((g.I + BM - 1) / BM), tiles_j = (int)((g.J + BN - 1) / BN), items = tiles_i * tiles_j * g.splits;
+    if constexpr (RARE) {
+        for (int block = blockIdx.x; block < items; block += gridDim.x)
+            loss_tile<BM, BN, WGM, WGN, TB, KIND, F32, RARE>(g, block, tiles_i, tiles_j);
+    } else if ((int)blockIdx.x < items) {
+        loss_tile<BM, BN, WGM, WGN, TB, KIND, F32, RARE>(g, blockIdx.x, tiles_i, tiles_j);
     }
 }
 
@@ -499,6 +550,28 @@ __global__ void __launch_bounds__(256) column_top_kernel(const uint16_t *src, co
     for (int k = 0; k < 8; ++k) b = t[k][threadIdx.x] > b ? t[k][threadIdx.x] : b;
     // the order of these does not matter
     if (blockIdx.y * 256 + threadIdx.x < n && b) atomicMax(top + blockIdx.y * 256 + threadIdx.x, b);
+}
+
+// The rows of G, held times 2^15, whose largest value over the tiles of the tokens is under 2^-24: how
+// many, which, and the exponents that take them to 2^14 .. 2^15.  In any order, which the rows do not
+// depend on; *rare starts at zero.
+__global__ void __launch_bounds__(256) rare_kernel(const float *row_top, int64_t ldt, int64_t M, const int *count, int bn,
+                                                   int64_t rows, int *rare, int *rare_row, int *rare_exp) {
+    const int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int lane = threadIdx.x & 63;
+    if (count) M = *count;
+    float top = 0.f;
+    if (v < rows)
+        for (int64_t j = 0; j * bn < M; ++j) top = fmaxf(top, row_top[j * ldt + v]);
+    const bool is = top > 0.f && top < 0x1p-9f;
+    const uint64_t all = __ballot(is);
+    if (all == 0) return;
+    int at = 0;
+    if (lane == 0) at = atomicAdd(rare, __popcll(all));
+    at = __shfl(at, 0) + __popcll(all & (((uint64_t)1 << lane) - 1));
+    if (!is) return;
+    rare_row[at] = (int)v;
+    rare_exp[at] = 14 + 127 - (int)(__float_as_uint(top) >> 23);
 }
 
 // dst[m][c] = src[m][c] scale[m] in fp16 at the column's scale, rows of np columns.
@@ -682,6 +755,18 @@ hipError_t launch(Args g, const Choice &c, bool f32, hipStream_t s) {
     return f32 ? launch_as<TB, KIND, true>(g, c, s) : launch_as<TB, KIND, false>(g, c, s);
 }
 
+// The rare rows' products, of at most `rows`: two workgroups a CU of tiles that two share, as many
+// rounds as the rows then are.
+template <bool TB, Kind KIND>
+hipError_t launch_rare(Args g, int64_t rows, hipStream_t s) {
+    const int64_t tiles = ((rows + 127) / 128) * ((g.J + 127) / 128);
+    if (tiles >= (int64_t)1 << 31) return hipErrorNotSupported;
+    g.group = 4;
+    g.splits = 1;
+    loss_pp_kernel<128, 128, 2, 4, TB, KIND, false, true><<<(unsigned)(tiles < 512 ? tiles : 512), kPPThreads, 0, s>>>(g);
+    return hipGetLastError();
+}
+
 // Below this the launches that gather would take longer than what they save.
 constexpr int64_t kCompactFrom = 257;
 
@@ -790,7 +875,8 @@ struct Layout {
     Operands ops;
     int64_t Mp, Mq, nq, vp;
     Choice dx;
-    size_t tokens, tops, xs, wt, gt, acc, total;
+    size_t tokens, tops, xs, wt, gt, row_top, rare_row, rare_exp, acc, total;
+    int64_t pieces;
 };
 Layout layout_of(int64_t M, int64_t n, int64_t V, bool f32) {
     Layout l;
@@ -800,7 +886,7 @@ Layout layout_of(int64_t M, int64_t n, int64_t V, bool f32) {
     l.Mq = up(M, 256) + 256;     // the last tile's tokens, whatever its width
     l.nq = up(n, 256) + 256;
     // G^T of a piece within kPieceBytes, and W^T with W where it is laid out
-    const int64_t longer = n + (lays_out_w(n, f32) ? up(n, kPPK) : 0);
+    const int64_t np = up(n, kPPK), longer = lays_out_w(n, f32) ? 2 * np : np;
     l.vp = piece_of(V, kPieceBytes / ((int64_t)value * (l.Mp > longer ? l.Mp : longer)));
     // at least 16 units a split, and the splits' sums within 256 MB
     int64_t splits = l.vp / kPPK * (f32 ? kProducts : 1) / 16;
@@ -811,10 +897,14 @@ Layout layout_of(int64_t M, int64_t n, int64_t V, bool f32) {
     if (l.vp > longest) l.vp = piece_of(V, longest);
     l.ops = operands_of(space, M, n, l.vp, f32);
     l.tokens = space.take((size_t)l.Mq * 12);
-    l.tops = space.take(f32 ? 0 : (size_t)l.nq * 8);
+    l.pieces = (V + l.vp - 1) / l.vp;
+    l.tops = space.take(f32 ? 0 : (size_t)(2 * l.nq + l.pieces) * 4);   // and a piece's number of rare rows
     l.xs = space.take(f32 ? 0 : (size_t)(M * l.ops.np) * 2);
-    l.wt = space.take((size_t)(n * l.vp) * value);
+    l.wt = space.take((size_t)(np * l.vp) * value);    // W^T of a piece, then its rare rows of W
     l.gt = space.take((size_t)(l.vp * l.Mp) * value);
+    l.row_top = space.take(f32 ? 0 : (size_t)(up(M, 128) / 128 * l.vp) * 4);
+    l.rare_row = space.take(f32 ? 0 : (size_t)l.vp * 4);
+    l.rare_exp = space.take(f32 ? 0 : (size_t)l.vp * 4);
     l.acc = space.take((size_t)(l.dx.splits * n * l.Mp) * 4);
     l.total = space.total;
     return l;
@@ -878,7 +968,7 @@ hipError_t launch_loss_mfma_grad(const LossPass &p, const LossEpi &e, hipStream_
     tok.target = reinterpret_cast<int *>(tok.lse + l.Mq);
     uint32_t *const x_top = reinterpret_cast<uint32_t *>(ws + l.tops), *const w_top = x_top + l.nq;
     token_kernel<<<(unsigned)(l.Mq / 256), 256, 0, s>>>(e, tok, p.M, l.Mq, r.idx, r.count, f32 ? 1.f : kLog2e, x_top,
-                                                        f32 ? 0 : 2 * l.nq);
+                                                        f32 ? 0 : 2 * l.nq + l.pieces);
     err = hipGetLastError();
     const int np = (int)l.ops.np, n = (int)p.n;
     const auto top_grid = [&](int64_t rows) {
@@ -920,7 +1010,13 @@ hipError_t launch_loss_mfma_grad(const LossPass &p, const LossEpi &e, hipStream_
         g.out = at(l.gt);
         g.plane_out = plane_gt;
         g.ldo = l.Mp;
-        err = launch<false, kGrad>(g, choose(g.I, g.J), f32, s);
+        const Choice tile = choose(g.I, g.J);
+        if (p.dW && !f32) {
+            g.row_top = reinterpret_cast<float *>(ws + l.row_top);
+            g.ldt = l.vp;
+        }
+        Args grad = g;
+        err = launch<false, kGrad>(g, tile, f32, s);
         if (err == hipSuccess && p.dW) {
             g.A = at(l.gt);
             g.plane_a = plane_gt;
@@ -932,6 +1028,7 @@ hipError_t launch_loss_mfma_grad(const LossPass &p, const LossEpi &e, hipStream_
             g.out = static_cast<char *>(p.dW) + v0 * p.n * (f32 ? 4 : 2);
             err = launch<true, kDw>(g, choose(g.I, g.J), f32, s);
         }
+        Args dw = g;
         if (err == hipSuccess && p.dX) {
             const dim3 grid((unsigned)((vn + 63) / 64), (unsigned)(np / 64));
             if (f32)
@@ -954,6 +1051,24 @@ hipError_t launch_loss_mfma_grad(const LossPass &p, const LossEpi &e, hipStream_
             g.acc = acc;
             g.first = v0 == 0;
             err = launch<true, kDx>(g, l.dx, f32, s);
+        }
+        if (err == hipSuccess && p.dW && !f32) {
+            int *rare = reinterpret_cast<int *>(w_top + l.nq) + v0 / l.vp, *rare_row = reinterpret_cast<int *>(ws + l.rare_row),
+                *rare_exp = reinterpret_cast<int *>(ws + l.rare_exp);
+            rare_kernel<<<(unsigned)((vn + 255) / 256), 256, 0, s>>>(grad.row_top, l.vp, p.M, r.count, kTiles[tile.tile].bn, vn, rare,
+                                                                    rare_row, rare_exp);
+            const int64_t blocks = (vn * (np / 8) + 255) / 256;
+            gather_kernel<<<(unsigned)(blocks < 2048 ? blocks : 2048), 256, 0, s>>>(static_cast<const uint16_t *>(p.W) + v0 * n,
+                                                                                    at(l.wt), vn, n, np, rare_row, rare);
+            err = hipGetLastError();
+            for (Args *again : {&grad, &dw}) {
+                again->rare = rare;
+                again->rare_row = rare_row;
+                again->rare_exp = rare_exp;
+            }
+            grad.A = at(l.wt);
+            if (err == hipSuccess) err = launch_rare<false, kGrad>(grad, vn, s);
+            if (err == hipSuccess) err = launch_rare<true, kDw>(dw, vn, s);
         }
     }
     if (err == hipSuccess && p.dX) {
