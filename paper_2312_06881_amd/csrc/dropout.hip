@@ -18,7 +18,7 @@ __global__ void __launch_bounds__(kThreads) dropout_kernel(const T *x, T *y, int
         const int64_t row = total >> 32 ? o / octets : (int64_t)((uint32_t)o / (uint32_t)octets);
         const int c = (int)(o - row * octets) * 8;
         float v[8];
-        load_cols<true>(x + row * n, c, n, v);
+        load_cols(x + row * n, c, n, v);
         apply_drop(v, keep_bits(philox(d.seed, offset, (uint64_t)o), d.thr), d.scale);
         store_cols<true>(y + row * n, c, n, v);
     }

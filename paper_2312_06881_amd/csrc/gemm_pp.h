@@ -45,14 +45,6 @@ struct PPCfg {
     static_assert(kSubN % 2 == 0, "the epilogue pairs column blocks");
 };
 
-// Swaps the odd 16-lane rows of a with the even ones of b.
-__device__ __forceinline__ void swap_rows(uint32_t &a, uint32_t &b) {
-    typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
-    const u32x2_t r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
-    a = r.x;
-    b = r.y;
-}
-
 // Zero columns in front of padded block g of b real columns.
 __host__ __device__ constexpr int pp_pad_shift(int64_t g, int64_t b) { return (int)(g * b & 7); }
 

@@ -8,6 +8,8 @@ namespace dyad {
 
 struct DropArgs;   // philox.h
 
+inline int64_t up(int64_t v, int64_t q) { return (v + q - 1) / q * q; }   // to a multiple of q
+
 hipError_t launch_dropout(int64_t rows, int64_t cols, int dtype, const void *x, const DropArgs &d, void *y, hipStream_t s);
 
 // ---- h = x_scale x + y_scale gate * drop(post(y)),  out = norm(h) -------------------

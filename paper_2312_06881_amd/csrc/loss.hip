@@ -2,9 +2,9 @@
 // Forward: tiles of logits leave (largest, sum of exponentials) per token, joined here.
 // Backward, a piece of the vocabulary at a time: the tiles' logits again, as
 // G = dloss (exp(z - lse) - onehot), then dX += G W and dW = G^T X of the piece.  Forming z
-// twice is 8 M n V operations for the four products where 6 M n V would do with z kept, which
-// takes M V values written and read at 4 bytes (as long, at the rates of this card, as the
-// product) and the memory for them.
+// twice is 8 M n V operations for the four products where 6 M n V would do with z kept.  That
+// takes the memory for M V values, and writing and reading them at 4 bytes: 1.5 ps each at a large
+// copy's rate, where forming one takes 1.1 ps at 768 columns and 6 at 4096.
 #include "lm_internal.h"
 
 namespace dyad {
@@ -65,8 +65,6 @@ __global__ void __launch_bounds__(1024) loss_sum_kernel(LossEpi e, int64_t M, co
 __global__ void __launch_bounds__(256) zero_kernel(uint16_t *p, int64_t n) {
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = 0;
 }
-
-int64_t up(int64_t v, int64_t q) { return (v + q - 1) / q * q; }
 
 // Which fp32 calls run on fp32 matrix instructions.
 bool plain_f32(int64_t M, int dtype) { return dtype == kF32 && M < kSplitFrom; }

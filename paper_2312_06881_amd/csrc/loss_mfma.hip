@@ -16,7 +16,9 @@
 //
 // An entry that every token finds improbable has a row of G, and of dW, below that range.  Rows whose
 // largest |G| is under 2^-24 are formed again, gathered, each at a power of two of its own (kGrad and kDw with
-// RARE).  From 2^-24 on fp16's smallest step, 2^-39, is at most 2^-15 of the row's largest value.
+// RARE).  From 2^-24 on fp16's smallest step, 2^-39, is at most 2^-15 of the row's largest value.  A step
+// without such rows takes up to 3 % longer for it, one where half of them are 16 to 29 % (4096 tokens of 1024 and
+// 16384 of 768 over 50000).
 //
 // fp32 operands (from kSplitFrom tokens) are split in three bf16 values, x = h + m + l with 8 bits
 // each, exact to 2^-27, and six of the nine products h h, h m, m h, h l, l h, m m are summed in
@@ -115,21 +117,13 @@ struct Cfg {
     static_assert(WGM * WGN == kPPWaves && kLds <= 160 * 1024, "eight waves, LDS budget");
 };
 
-// Swaps the odd 16-lane rows of a with the even ones of b.
-__device__ __forceinline__ void swap_lane_rows(uint32_t &a, uint32_t &b) {
-    typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
-    const u32x2_t r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
-    a = r.x;
-    b = r.y;
-}
-
 // x: a lane's four sums of column block 2 jp and of the next.  After the swap it holds 8
 // consecutive columns, from lane_piece() of the pair on.
 template <class Pack>
 __device__ __forceinline__ uint4 pack_pair(const float (&x)[8], Pack pack) {
     uint32_t d0 = pack(x[0], x[1]), d1 = pack(x[2], x[3]), s0 = pack(x[4], x[5]), s1 = pack(x[6], x[7]);
-    swap_lane_rows(d0, s0);
-    swap_lane_rows(d1, s1);
+    swap_rows(d0, s0);
+    swap_rows(d1, s1);
     return make_uint4(d0, d1, s0, s1);
 }
 __device__ __forceinline__ int lane_piece(int lg) { return (lg & 1) * 16 + (lg >> 1) * 8; }
@@ -272,8 +266,8 @@ __device__ __forceinline__ void loss_tile(const Args &g, int block, int tiles_i,
                     split8(x, p);
 #pragma unroll
                     for (int k = 0; k < 3; ++k) {
-                        swap_lane_rows(p[k].x, p[k].z);
-                        swap_lane_rows(p[k].y, p[k].w);
+                        swap_rows(p[k].x, p[k].z);
+                        swap_rows(p[k].y, p[k].w);
                         if (in) *reinterpret_cast<uint4 *>(o + k * g.plane_out + (int64_t)(16 * i) * g.ldo) = p[k];
                     }
                 } else {
@@ -457,7 +451,7 @@ __global__ void __launch_bounds__(256) gather_kernel(const uint16_t *src, uint16
         int c;
         octet_at(i, total, np, r, c);
         float v[8];
-        load_cols<true>(src + (idx ? idx[r] : r) * n, c, n, v);
+        load_cols(src + (idx ? idx[r] : r) * n, c, n, v);
         store8(dst + r * np + c, v);
     }
 }
@@ -473,7 +467,7 @@ __global__ void __launch_bounds__(256) gather_split_kernel(const float *src, uin
         int c;
         octet_at(i, total, np, r, c);
         float v[8];
-        load_cols<true>(src + (idx ? idx[r] : r) * n, c, n, v);
+        load_cols(src + (idx ? idx[r] : r) * n, c, n, v);
         if (e.targets && !loss_counts(e, e.targets[r]))
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] = 0.f;
@@ -494,7 +488,7 @@ __global__ void __launch_bounds__(256) transpose_split_kernel(const float *src, 
     for (int q = 0; q < 2; ++q) {
         const int r = (tid + 256 * q) / 8, c = (tid + 256 * q) % 8 * 8;
         float v[8] = {};
-        if (r0 + r < rows) load_cols<true>(src + (r0 + r) * n, c0 + c, n, v);
+        if (r0 + r < rows) load_cols(src + (r0 + r) * n, c0 + c, n, v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) t[c + e][r] = v[e];
     }
@@ -533,7 +527,7 @@ __global__ void __launch_bounds__(256) column_top_kernel(const uint16_t *src, co
     if (c < n) {
         for (int64_t m = (int64_t)blockIdx.x * 8 + r; m < rows; m += (int64_t)gridDim.x * 8) {
             float v[8];
-            load_cols<true>(src + m * ld, c, n, v);
+            load_cols(src + m * ld, c, n, v);
             const float s = scale ? scale[m] : 1.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -770,8 +764,6 @@ hipError_t launch_rare(Args g, int64_t rows, hipStream_t s) {
 // Below this the launches that gather would take longer than what they save.
 constexpr int64_t kCompactFrom = 257;
 
-int64_t up(int64_t v, int64_t q) { return (v + q - 1) / q * q; }
-size_t part(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
 // Where things lie in the workspace; a size of 0 for what a call does not need.
 struct Space {
@@ -867,7 +859,7 @@ int64_t forward_piece(int64_t n, int64_t V, bool f32) {
 
 // dX's reduction units in one accumulator at most (split fp32: 16384 vocabulary columns; bf16: 98304).  Each unit is two
 // additions, and each may lose half of the last bit of a sum that a target's term has made as large as the whole
-// gradient: 1e-4 of it at worst, where 43520 columns of small terms of one sign had lost 3.6e-5 in place of 1.2e-5.
+// gradient: 1e-4 of it at worst.  (fp32, 43520 columns of small terms of one sign: 4e-6 of dX, in one sum 3.6e-5.)
 constexpr int64_t kMostUnits = 1536;
 
 // Vocabulary columns of a piece, and the workspace of a backward pass.

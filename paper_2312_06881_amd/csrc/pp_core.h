@@ -193,6 +193,14 @@ __device__ __forceinline__ void pp_read(uint32_t pa, const uint32_t (&pb)[TB ? S
     }
 }
 
+// Swaps the odd 16-lane rows of a with the even ones of b.
+__device__ __forceinline__ void swap_rows(uint32_t &a, uint32_t &b) {
+    typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
+    const u32x2_t r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+    a = r.x;
+    b = r.y;
+}
+
 // The loop over `units` units (at least one).  issue_a(d) / issue_b(d) start
 // the wave's NVA / NVB loads of unit d's sides into slots d % SLOTA and
 // d % SLOTB (for d >= units they load a valid unit again: its slot is never

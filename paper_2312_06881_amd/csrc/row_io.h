@@ -22,18 +22,17 @@ __device__ __forceinline__ void store8(uint16_t *p, const float (&v)[8]) {
     __builtin_memcpy(p, w, 16);
 }
 
-// Columns c .. c + 7 of a row of n; columns past it read zero and are not written.  RAG:
-// n may end inside the eight (the element-wise ends double a kernel's registers, so
-// rows of whole vectors have instances without them).
-template <bool RAG, class T>
+// Columns c .. c + 7 of a row of n; columns past it read zero and are not written.
+template <class T>
 __device__ __forceinline__ void load_cols(const T *row, int c, int n, float (&v)[8]) {
     if (c + 8 <= n) {
         load8(row + c, v);
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = RAG && c + e < n ? load_f32(row, c + e) : 0.f;
+        for (int e = 0; e < 8; ++e) v[e] = c + e < n ? load_f32(row, c + e) : 0.f;
     }
 }
+// RAG: n may end inside the eight (element by element; rows of whole vectors have instances without).
 template <bool RAG, class T>
 __device__ __forceinline__ void store_cols(T *row, int c, int n, const float (&v)[8]) {
     if (c + 8 <= n) {
