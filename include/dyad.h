@@ -367,12 +367,18 @@ int dyad_add_norm_backward(const dyad_add_norm_args *args, const dyad_add_norm_g
  *
  * Backward: dloss, of loss's length, is the gradient that reaches it; dX [M][n] and
  * dW [V][n], either of which may be NULL, are the gradients.  The logits are formed
- * again, a piece of the vocabulary at a time.  With bf16 operands their gradient, and
- * X times dloss, enter the products with W and X in fp16 (at powers of two that meet
- * its range); the sums are fp32.
+ * again, a piece of the vocabulary at a time.  With bf16 operands their gradient G, W
+ * and X times dloss enter the products in fp16 at powers of two: one a column for W and for
+ * X times dloss, whose values below 2^-39 of the column's largest become zero; 2^15 for G,
+ * whose values below 2^-39 become zero in dX, and in dW only beside larger ones in their row
+ * (a row whose largest is under 2^-24 has a power of its own).  The sums are fp32.
  *
  * M, V <= 2^22, M V <= 2^38 and n <= 2^20, else DYAD_ERR_SHAPE.  The workspace holds
- * dyad_linear_ce_workspace_bytes() bytes for the pass (0 for invalid arguments).
+ * dyad_linear_ce_workspace_bytes() bytes for the pass (0 for invalid arguments): about
+ * M n values twice, and for the pieces up to 512 MB of G, as much as 256 MB of sums and
+ * 768 MB of W laid out otherwise (more for up to 1024 tokens: 65536 / ceil(M / 256) rows of
+ * W, of 2 bytes a value in bf16 and 6 in fp32).  For few tokens that is more than their
+ * logits would take.
  */
 typedef enum { DYAD_REDUCE_NONE = 0, DYAD_REDUCE_SUM = 1, DYAD_REDUCE_MEAN = 2 } dyad_reduction;
 typedef enum { DYAD_CE_FORWARD = 0, DYAD_CE_BACKWARD = 1 } dyad_ce_pass;

@@ -156,7 +156,7 @@ hipError_t launch_loss_f32_piece(const LossPass &p, const LossEpi &e, int64_t v0
 
 // bf16, and fp32 from kSplitFrom tokens (loss_mfma.hip).  The statistics (ws: forward_bytes), and the whole backward pass (the
 // call's workspace: backward_bytes).
-int loss_mfma_tiles(int64_t M, int64_t V);
+int loss_mfma_tiles(int64_t M, int64_t n, int64_t V, bool f32);
 size_t loss_mfma_forward_bytes(int64_t M, int64_t n, int64_t V, bool f32);
 size_t loss_mfma_backward_bytes(int64_t M, int64_t n, int64_t V, bool f32);
 // Which token row c of the statistics is, and how many rows there are; null: c, and all.

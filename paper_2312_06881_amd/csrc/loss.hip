@@ -96,7 +96,7 @@ size_t loss_workspace(bool backward, int64_t M, int64_t n, int64_t V, int dtype)
     const bool f32 = dtype == kF32, plain = plain_f32(M, dtype);
     if (backward) return plain ? (size_t)(M * f32_piece(V)) * 4 : loss_mfma_backward_bytes(M, n, V, f32);
     return plain ? stats_bytes(M, loss_f32_tiles(M, V))
-                 : stats_bytes(M, loss_mfma_tiles(M, V)) + loss_mfma_forward_bytes(M, n, V, f32);
+                 : stats_bytes(M, loss_mfma_tiles(M, n, V, f32)) + loss_mfma_forward_bytes(M, n, V, f32);
 }
 
 hipError_t launch_loss_forward(const LossPass &p, hipStream_t s) {
@@ -107,7 +107,7 @@ hipError_t launch_loss_forward(const LossPass &p, hipStream_t s) {
         e.part = reinterpret_cast<float2 *>(e.at_target + up(p.M, 4));
         if (p.reduction == kReduceNone) each = p.loss;
         const bool plain = plain_f32(p.M, p.dtype);
-        e.tiles = plain ? loss_f32_tiles(p.M, p.V) : loss_mfma_tiles(p.M, p.V);
+        e.tiles = plain ? loss_f32_tiles(p.M, p.V) : loss_mfma_tiles(p.M, p.n, p.V, p.dtype == kF32);
         LossTokens tokens{};
         const hipError_t err = plain ? launch_loss_f32_stats(p, e, s)
                                      : launch_loss_mfma_stats(p, e, static_cast<char *>(p.ws) + stats_bytes(p.M, e.tiles),

@@ -17,8 +17,8 @@
 // An entry that every token finds improbable has a row of G, and of dW, below that range.  Rows whose
 // largest |G| is under 2^-24 are formed again, gathered, each at a power of two of its own (kGrad and kDw with
 // RARE).  From 2^-24 on fp16's smallest step, 2^-39, is at most 2^-15 of the row's largest value.  A step
-// without such rows takes up to 3 % longer for it, one where half of them are 16 to 29 % (4096 tokens of 1024 and
-// 16384 of 768 over 50000).
+// without such rows takes up to 3 % longer for it, one where half of them are 9 to 30 % (512 and 16384
+// tokens of 768 over 50000).
 //
 // fp32 operands (from kSplitFrom tokens) are split in three bf16 values, x = h + m + l with 8 bits
 // each, exact to 2^-27, and six of the nine products h h, h m, m h, h l, l h, m m are summed in
@@ -547,25 +547,49 @@ __global__ void __launch_bounds__(256) column_top_kernel(const uint16_t *src, co
 }
 
 // The rows of G, held times 2^15, whose largest value over the tiles of the tokens is under 2^-24: how
-// many, which, and the exponents that take them to 2^14 .. 2^15.  In any order, which the rows do not
-// depend on; *rare starts at zero.
+// many, which, the exponents that take them to 2^14 .. 2^15, and their rows of W, in any order,
+// which the results do not depend on.  *rare starts at zero.
 __global__ void __launch_bounds__(256) rare_kernel(const float *row_top, int64_t ldt, int64_t M, const int *count, int bn,
-                                                   int64_t rows, int *rare, int *rare_row, int *rare_exp) {
-    const int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int lane = threadIdx.x & 63;
+                                                   int64_t rows, const uint16_t *W, int n, int np, int *rare, int *rare_row,
+                                                   int *rare_exp, uint16_t *dst) {
+    __shared__ float tops[4][64];
+    __shared__ int found[64], first, many;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t v = (int64_t)blockIdx.x * 64 + lane;
     if (count) M = *count;
+    const int tiles = (int)((M + bn - 1) / bn);
     float top = 0.f;
     if (v < rows)
-        for (int64_t j = 0; j * bn < M; ++j) top = fmaxf(top, row_top[j * ldt + v]);
-    const bool is = top > 0.f && top < 0x1p-9f;
-    const uint64_t all = __ballot(is);
-    if (all == 0) return;
-    int at = 0;
-    if (lane == 0) at = atomicAdd(rare, __popcll(all));
-    at = __shfl(at, 0) + __popcll(all & (((uint64_t)1 << lane) - 1));
-    if (!is) return;
-    rare_row[at] = (int)v;
-    rare_exp[at] = 14 + 127 - (int)(__float_as_uint(top) >> 23);
+#pragma unroll 8
+        for (int j = wave; j < tiles; j += 4) top = fmaxf(top, row_top[j * ldt + v]);
+    tops[wave][lane] = top;
+    __syncthreads();
+    if (wave == 0) {
+#pragma unroll
+        for (int w = 1; w < 4; ++w) top = fmaxf(top, tops[w][lane]);
+        const bool is = top > 0.f && top < 0x1p-9f;
+        const uint64_t all = __ballot(is);
+        int at = 0;
+        if (lane == 0 && all) at = atomicAdd(rare, __popcll(all));
+        at = __shfl(at, 0);
+        const int place = __popcll(all & (((uint64_t)1 << lane) - 1));
+        if (is) {
+            found[place] = (int)v;
+            rare_row[at + place] = (int)v;
+            rare_exp[at + place] = 14 + 127 - (int)(__float_as_uint(top) >> 23);
+        }
+        if (lane == 0) {
+            first = at;
+            many = __popcll(all);
+        }
+    }
+    __syncthreads();
+    for (int k = wave; k < many; k += 4)
+        for (int c = lane * 8; c < np; c += 512) {
+            float w[8];
+            load_cols(W + (int64_t)found[k] * n, c, n, w);
+            store8(dst + (int64_t)(first + k) * np + c, w);
+        }
 }
 
 // dst[m][c] = src[m][c] scale[m] in fp16 at the column's scale, rows of np columns.
@@ -764,7 +788,6 @@ hipError_t launch_rare(Args g, int64_t rows, hipStream_t s) {
 // Below this the launches that gather would take longer than what they save.
 constexpr int64_t kCompactFrom = 257;
 
-
 // Where things lie in the workspace; a size of 0 for what a call does not need.
 struct Space {
     size_t total = 0;
@@ -850,16 +873,26 @@ int64_t piece_of(int64_t V, int64_t most) {
     const int64_t pieces = (V + most - 1) / most;
     return up((V + pieces - 1) / pieces, 256);
 }
-// What a piece of W laid out otherwise, and of G, may take.
-constexpr int64_t kPieceBytes = (int64_t)512 << 20;
-
-int64_t forward_piece(int64_t n, int64_t V, bool f32) {
-    return lays_out_w(n, f32) ? piece_of(V, kPieceBytes / ((f32 ? 6 : 2) * up(n, kPPK))) : V;
+// What a piece of G may take, and one of W laid out otherwise; of W as many columns all the same as
+// give each of 256 CUs a tile (129 tokens of 4096 over 50000 in fp32: forward 1532 us in three
+// pieces, 798 in one; the step 5005 in five).
+constexpr int64_t kGradBytes = (int64_t)512 << 20, kWeightBytes = (int64_t)768 << 20;
+int64_t weight_columns(int64_t M, int64_t n, bool f32) {
+    const int64_t by_bytes = kWeightBytes / ((f32 ? 6 : 2) * up(n, kPPK)), by_tiles = up(65536 / ((M + 255) / 256), 256);
+    return by_bytes > by_tiles ? by_bytes : by_tiles;
+}
+int64_t forward_piece(int64_t M, int64_t n, int64_t V, bool f32) {
+    return lays_out_w(n, f32) ? piece_of(V, weight_columns(M, n, f32)) : V;
+}
+// The tile that every piece of a forward pass takes.
+Choice forward_tile(int64_t M, int64_t n, int64_t V, bool f32) {
+    const int64_t piece = forward_piece(M, n, V, f32);
+    return choose(M, piece < V ? piece : V);
 }
 
 // dX's reduction units in one accumulator at most (split fp32: 16384 vocabulary columns; bf16: 98304).  Each unit is two
 // additions, and each may lose half of the last bit of a sum that a target's term has made as large as the whole
-// gradient: 1e-4 of it at worst.  (fp32, 43520 columns of small terms of one sign: 4e-6 of dX, in one sum 3.6e-5.)
+// gradient: 1e-4 of it at worst.  (fp32, 43520 columns of small terms of one sign: 1.2e-5 of dX, in one sum 3.6e-5.)
 constexpr int64_t kMostUnits = 1536;
 
 // Vocabulary columns of a piece, and the workspace of a backward pass.
@@ -877,9 +910,8 @@ Layout layout_of(int64_t M, int64_t n, int64_t V, bool f32) {
     l.Mp = up(M, kPPK);
     l.Mq = up(M, 256) + 256;     // the last tile's tokens, whatever its width
     l.nq = up(n, 256) + 256;
-    // G^T of a piece within kPieceBytes, and W^T with W where it is laid out
-    const int64_t np = up(n, kPPK), longer = lays_out_w(n, f32) ? 2 * np : np;
-    l.vp = piece_of(V, kPieceBytes / ((int64_t)value * (l.Mp > longer ? l.Mp : longer)));
+    const int64_t np = up(n, kPPK), most = kGradBytes / ((int64_t)value * l.Mp), columns = weight_columns(M, n, f32);
+    l.vp = piece_of(V, most < columns ? most : columns);
     // at least 16 units a split, and the splits' sums within 256 MB
     int64_t splits = l.vp / kPPK * (f32 ? kProducts : 1) / 16;
     const int64_t room = ((int64_t)64 << 20) / (n * l.Mp);
@@ -887,12 +919,13 @@ Layout layout_of(int64_t M, int64_t n, int64_t V, bool f32) {
     l.dx = choose(n, M, splits < 1 ? 1 : splits);
     const int64_t longest = l.dx.splits * kMostUnits / (f32 ? kProducts : 1) * kPPK;
     if (l.vp > longest) l.vp = piece_of(V, longest);
-    l.ops = operands_of(space, M, n, l.vp, f32);
+    l.ops = operands_of(space, M, n, 0, f32);
     l.tokens = space.take((size_t)l.Mq * 12);
     l.pieces = (V + l.vp - 1) / l.vp;
     l.tops = space.take(f32 ? 0 : (size_t)(2 * l.nq + l.pieces) * 4);   // and a piece's number of rare rows
     l.xs = space.take(f32 ? 0 : (size_t)(M * l.ops.np) * 2);
-    l.wt = space.take((size_t)(np * l.vp) * value);    // W^T of a piece, then its rare rows of W
+    // W of a piece for its logits, then W^T of it, then its rare rows
+    l.wt = l.ops.w = space.take((size_t)(np * l.vp) * value);
     l.gt = space.take((size_t)(l.vp * l.Mp) * value);
     l.row_top = space.take(f32 ? 0 : (size_t)(up(M, 128) / 128 * l.vp) * 4);
     l.rare_row = space.take(f32 ? 0 : (size_t)l.vp * 4);
@@ -904,14 +937,14 @@ Layout layout_of(int64_t M, int64_t n, int64_t V, bool f32) {
 
 }  // namespace
 
-int loss_mfma_tiles(int64_t M, int64_t V) {
-    const int bn = kTiles[choose(M, V).tile].bn;
+int loss_mfma_tiles(int64_t M, int64_t n, int64_t V, bool f32) {
+    const int bn = kTiles[forward_tile(M, n, V, f32).tile].bn;
     return (int)((V + bn - 1) / bn);
 }
 
 size_t loss_mfma_forward_bytes(int64_t M, int64_t n, int64_t V, bool f32) {
     Space space;
-    operands_of(space, M, n, forward_piece(n, V, f32), f32);
+    operands_of(space, M, n, forward_piece(M, n, V, f32), f32);
     return space.total;
 }
 
@@ -921,9 +954,9 @@ hipError_t launch_loss_mfma_stats(const LossPass &p, const LossEpi &e, void *ws,
                                   hipStream_t s) {
     Space space;
     const bool f32 = p.dtype == kF32;
-    const int64_t piece = forward_piece(p.n, p.V, f32);
+    const int64_t piece = forward_piece(p.M, p.n, p.V, f32);
     const Operands o = operands_of(space, p.M, p.n, piece, f32);
-    const Choice tile = choose(p.M, p.V);
+    const Choice tile = forward_tile(p.M, p.n, p.V, f32);
     Prepared r;
     hipError_t err = prepare(o, p, e, static_cast<char *>(ws), each, p.lse, r, s);
     if (err != hipSuccess) return err;
@@ -1047,11 +1080,9 @@ hipError_t launch_loss_mfma_grad(const LossPass &p, const LossEpi &e, hipStream_
         if (err == hipSuccess && p.dW && !f32) {
             int *rare = reinterpret_cast<int *>(w_top + l.nq) + v0 / l.vp, *rare_row = reinterpret_cast<int *>(ws + l.rare_row),
                 *rare_exp = reinterpret_cast<int *>(ws + l.rare_exp);
-            rare_kernel<<<(unsigned)((vn + 255) / 256), 256, 0, s>>>(grad.row_top, l.vp, p.M, r.count, kTiles[tile.tile].bn, vn, rare,
-                                                                    rare_row, rare_exp);
-            const int64_t blocks = (vn * (np / 8) + 255) / 256;
-            gather_kernel<<<(unsigned)(blocks < 2048 ? blocks : 2048), 256, 0, s>>>(static_cast<const uint16_t *>(p.W) + v0 * n,
-                                                                                    at(l.wt), vn, n, np, rare_row, rare);
+            rare_kernel<<<(unsigned)((vn + 63) / 64), 256, 0, s>>>(grad.row_top, l.vp, p.M, r.count, kTiles[tile.tile].bn, vn,
+                                                                  static_cast<const uint16_t *>(p.W) + v0 * n, n, np, rare,
+                                                                  rare_row, rare_exp, at(l.wt));
             err = hipGetLastError();
             for (Args *again : {&grad, &dw}) {
                 again->rare = rare;

@@ -14,14 +14,18 @@ def test_workspaces_do_not_grow_with_the_vocabulary(M, n, V, dtype):
     if dtype == dy.F32 and M < 129:
         pytest.skip("no weights are laid out")
     value = 6 if dtype == dy.F32 else 2
-    # a piece of W laid out otherwise: 512 MB.  The tokens: X, X times dloss and their places, rows padded to 64; by
-    # them their tiles' statistics.
+    # a piece of W laid out otherwise: 768 MB, or the columns of one tile of 256 on each of 256 CUs
+    np = -(-n // 64) * 64
+    weights = max(768 * MB, (65536 // -(-M // 256) + 512) * np * value)
+    # X, X times dloss and the tokens' places, rows padded to 64; by them their tiles' statistics
     rows = M * (n + 64) * (value + 2) + 64 * (M + 512)
     forward = dy.dyad_linear_ce_workspace_bytes(dy.CE_FORWARD, M, n, V, dtype)
-    assert 0 < forward <= 512 * MB + rows + 8 * M * (V // 128 + 1) + MB
-    # W^T, G^T: 512 MB each.  dX's sums: 256 MB over those of one split.
+    assert 0 < forward <= weights + rows + 8 * M * (V // 128 + 1) + MB
+    # G: 512 MB, and 1 / 64 of it for its rows' largest values.  dX's sums: 256 MB over those of one split.
     backward = dy.dyad_linear_ce_workspace_bytes(dy.CE_BACKWARD, M, n, V, dtype)
-    assert 0 < backward <= (512 + 512 + 256) * MB + rows + 4 * (M + 64) * n + 16 * n + MB
+    assert 0 < backward <= weights + (512 + 8 + 256) * MB + rows + 4 * (M + 64) * n + 16 * n + MB
+    # one copy of W at a time, for its logits or turned round
+    assert backward <= V * np * value + (512 + 8 + 256) * MB + rows + 4 * (M + 64) * n + 512 * np * value + 16 * n + MB
 
 
 def test_pieces_of_very_long_rows_are_not_shorter_than_2048_columns():
