@@ -375,10 +375,9 @@ int dyad_add_norm_backward(const dyad_add_norm_args *args, const dyad_add_norm_g
  *
  * M, V <= 2^22, M V <= 2^38 and n <= 2^20, else DYAD_ERR_SHAPE.  The workspace holds
  * dyad_linear_ce_workspace_bytes() bytes for the pass (0 for invalid arguments): about
- * M n values twice, and for the pieces up to 512 MB of G, as much as 256 MB of sums and
- * 768 MB of W laid out otherwise (more for up to 1024 tokens: 65536 / ceil(M / 256) rows of
- * W, of 2 bytes a value in bf16 and 6 in fp32).  For few tokens that is more than their
- * logits would take.
+ * M n values twice, and for the pieces up to 512 MB of G, 256 MB of sums and 768 MB of W
+ * laid out otherwise (or 65536 / ceil(M / 256) rows of W, at 2 bytes a value in bf16 and 6 in
+ * fp32, where that is more).  For few tokens that is more than their logits would take.
  */
 typedef enum { DYAD_REDUCE_NONE = 0, DYAD_REDUCE_SUM = 1, DYAD_REDUCE_MEAN = 2 } dyad_reduction;
 typedef enum { DYAD_CE_FORWARD = 0, DYAD_CE_BACKWARD = 1 } dyad_ce_pass;
