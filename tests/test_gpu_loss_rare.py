@@ -62,3 +62,36 @@ def test_rows_keep_their_relative_precision(M, n, V, first, reduction, dtype):
     assert (off <= tol).all(), float((off / tol).max())
     if len(used):
         assert dw[first:].any(1).float().mean() > 0.9
+
+
+def test_captured_steps_with_rare_rows():
+    from paper_2312_06881_amd import lm
+
+    def step(s):
+        loss, lse, count = lm.linear_cross_entropy(*s, keep=True)
+        return [loss, *lm.linear_cross_entropy_backward(torch.ones_like(loss), *s, lse, count)]
+
+    a, b = ([t.cuda() for t in rare(700, 64, 2000, BF, first, seed=first)] for first in (300, 1500))
+    s = [t.clone() for t in a]
+    step(s)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(s)
+    for new in (b, a, b, b):
+        for t, u in zip(s, new):
+            t.copy_(u)
+        graph.replay()
+        for x, y in zip(got, step(new)):
+            assert torch.equal(x, y)
+
+
+def test_rare_rows_without_the_tokens_gradient():
+    x, w, t = rare(400, 72, 900, BF, 200)
+    b = w.cuda().requires_grad_(True)
+    dw, = torch.autograd.grad(nn.linear_cross_entropy(x.cuda(), b, t.cuda()), b)
+    a = x.cuda().requires_grad_(True)
+    both = torch.autograd.grad(nn.linear_cross_entropy(a, b, t.cuda()), (a, b))
+    assert torch.equal(dw, both[1])
+    dx, = torch.autograd.grad(nn.linear_cross_entropy(a, w.cuda(), t.cuda()), a)
+    assert torch.equal(dx, both[0])
